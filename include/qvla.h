@@ -372,8 +372,111 @@ qvla_status qvla_w4a8_linear(const qvla_layer* layer, const void* x, int M, int 
 qvla_status qvla_gemm_w4a8(const qvla_layer* layer, const int8_t* xq, const float* xscale, int M, void* y,
                            int32_t* acc, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Synchronise `stream`, then report (and clear) the device-side error word: QVLA_OK, or
- * QVLA_ERR_TIMEOUT if a kernel gave up waiting since the last check. */
+/* ------------------------------------------------------------------------------------------
+ * Attention between the quantised linears, and a key/value cache of 4-bit codes.
+ *
+ * The paper quantises the linears of the language backbone and of the DiT action head (Sec. 5.1);
+ * what runs between the fused Q/K/V linear and the output linear is the model's softmax attention
+ *     o_i = sum_j p_ij v_j,   p_ij = exp(scale q_i.k_j) / sum_j' exp(scale q_i.k_j'),
+ * j over the keys that query i sees.  Conventions of the calls below:
+ *  - A token's heads are contiguous: element (t, h, c) of q is q[t * q_stride + h * head_dim + c],
+ *    so q, k and v may be slices of the fused linear's output (q_stride its row length).  Strides
+ *    are in elements, multiples of 8 and at least heads * head_dim (kv_heads * head_dim); pointers
+ *    are 16-byte aligned.  Outputs are dense: o[t][heads][head_dim].
+ *  - dt is QVLA_F16 or QVLA_BF16, for queries, keys, values and outputs alike.  head_dim is 64, 128
+ *    or 256; kv_heads divides heads, and query head h reads key/value head h / (heads / kv_heads).
+ *  - Sequences are packed: sequence b's queries are rows [cu_q[b], cu_q[b+1]) (device int32
+ *    [batch + 1], not decreasing).  Lengths may be zero and may change between replays of a CUDA
+ *    graph within total_q / total_k.
+ *  - causal != 0: with n queries and m keys, query i of its sequence sees keys 0 .. m - n + i (the last
+ *    query stands at the last key).  A query that sees no key (m == 0, or m - n + i < 0) gets zeros.
+ *    A key or value that a query does not see has no effect on it, whatever its bits (NaN, Inf).
+ *  - scale is positive and finite (1 / sqrt(head_dim) as a rule).  Scores, the softmax's maximum
+ *    and sum, and the sum over the values are held in float32.
+ *  - Indices in device memory (cu_q, cu_k, page tables, lengths) that leave the buffers they index are
+ *    caught on the device: the tokens concerned are skipped, and qvla_check_device() reports
+ *    QVLA_ERR_INVALID_ARG.  Offsets beyond total_q / total_k are cut off.
+ * ------------------------------------------------------------------------------------------ */
+
+/* Attention over packed prompts.
+ *   q [total_q], k and v [total_k] tokens as above; cu_k device int32 [batch + 1], may be cu_q.
+ *   o device out [total_q][heads][head_dim]; rows outside every sequence are not written.
+ * batch >= 0, total_q and total_k in [0, 2^24], heads <= 1024.
+ * The probabilities are rounded to dt for the product with the values. */
+qvla_status qvla_attention_prompt(const void* q, const void* k, const void* v, qvla_dtype dt, int heads, int kv_heads,
+                                  int head_dim, int64_t q_stride, int64_t k_stride, int64_t v_stride, int batch,
+                                  const int32_t* cu_q, int total_q, const int32_t* cu_k, int total_k, float scale,
+                                  int causal, void* o, void* stream);
+
+/* A paged key/value cache of 4-bit codes in one device buffer of the caller (the pool).
+ *   pool      device, 16-byte aligned, qvla_kv4_pool_bytes(...) bytes: num_pages x kv_heads blocks of
+ *             page_size * (head_dim + 8) bytes, each holding, for one head's tokens of the page, the key
+ *             codes [page_size][head_dim / 2], the value codes (the same), the key scales float32
+ *             [page_size] and the value scales.  Byte j of a token's codes holds channel 2j in its
+ *             low nibble and 2j + 1 in its high nibble, two's complement in [-7, 7].
+ *   page_size 16, 32, 64, 128 or 256 tokens.
+ *   rotate    nonzero: every head is multiplied by H / sqrt(head_dim) (H the Sylvester Hadamard matrix)
+ *             ahead of the quantiser, which spreads a head's large channels (Sec. 4.1 Eq. 3, applied
+ *             to the cached heads).  Queries are rotated alike, and outputs rotated back.
+ * A token's head has one scale, Delta = max |y| / 7, and codes clamp(round(y / Delta), -7, 7), round
+ * half to even on the exact quotient (Sec. 4.2 Eq. 5-6 per token and head); Delta = 0 gives codes 0.
+ * A head with a NaN or an infinity reads back as NaN.
+ * A sequence's tokens lie at positions 0, 1, 2, ...; position p of sequence b is slot p % page_size of
+ * page page_table[b * max_pages + p / page_size] (device int32 [batch][max_pages]). */
+typedef struct {
+  void* pool;
+  int num_pages;
+  int page_size;
+  int kv_heads;
+  int head_dim;
+  int rotate;
+} qvla_kv4_cache;
+
+/* Bytes of a pool; 0 for a geometry that the calls below refuse. */
+size_t qvla_kv4_pool_bytes(int num_pages, int page_size, int kv_heads, int head_dim);
+
+/* Quantise new tokens' keys and values into the cache: token t of sequence b, at row cu_new[b] + t of k
+ * and v, goes to position start[b] + t (start device int32 [batch]: the tokens cached before; NULL: 0).
+ * Two rows of one call must not name the same slot. */
+qvla_status qvla_kv4_append(const qvla_kv4_cache* cache, const void* k, const void* v, qvla_dtype dt, int64_t k_stride,
+                            int64_t v_stride, int batch, const int32_t* cu_new, int total_new,
+                            const int32_t* page_table, int max_pages, const int32_t* start, void* stream);
+
+/* Read cached tokens back, in the model's basis (rotated back) and rounded to dt: position start[b] + t
+ * (start NULL: 0) of sequence b to row cu[b] + t of k and v (device out [total][kv_heads][head_dim]),
+ * for example as the first part of a prompt's keys and values for qvla_attention_prompt.  A position
+ * without a page gives zeros. */
+qvla_status qvla_kv4_gather(const qvla_kv4_cache* cache, int batch, const int32_t* cu, int total,
+                            const int32_t* page_table, int max_pages, const int32_t* start, void* k, void* v,
+                            qvla_dtype dt, void* stream);
+
+/* Bytes of workspace that let qvla_attention_kv4 split the keys of each sequence as far as is useful on the
+ * current device (a multiple of 256; 0 when no split would be made). */
+size_t qvla_attention_kv4_workspace_bytes(int heads, int kv_heads, int head_dim, int batch, int total_q, int max_q,
+                                          int max_len);
+
+/* Attention of a few query tokens of every sequence over its cached keys and values: one token while
+ * decoding, a chunk of action tokens, a few speculated tokens.  The codes are multiplied as they are and
+ * the scales applied to scores and probabilities; nothing is written back to memory as values.
+ *   q          [total_q] tokens;  max_q >= the queries of any sequence
+ *   kv_len     device int32 [batch]: cached tokens of each sequence (with causal != 0 the queries' own
+ *              tokens, appended before, are the last of them);  max_len >= every kv_len.  max_q and
+ *              max_len shape the launch: a sequence that exceeds them is skipped, and reported by
+ *              qvla_check_device().
+ *   o          device out [total_q][heads][head_dim]
+ *   workspace  device, 256-byte aligned, or NULL with 0 bytes: room for the partial results of a split
+ *              over the keys (qvla_attention_kv4_workspace_bytes; a smaller one allows a smaller split).
+ *              Used only during the call's kernels on `stream`.
+ * The probabilities, times the value scales, are rounded to bfloat16 for the product with the codes
+ * (their range is a float32's); queries are scaled by a power of two and rounded to float16. */
+qvla_status qvla_attention_kv4(const qvla_kv4_cache* cache, const void* q, qvla_dtype dt, int heads, int64_t q_stride,
+                               int batch, const int32_t* cu_q, int total_q, int max_q, const int32_t* page_table,
+                               int max_pages, const int32_t* kv_len, int max_len, float scale, int causal, void* o,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Synchronise `stream`, then report (and clear) the device-side error words: QVLA_OK,
+ * QVLA_ERR_TIMEOUT if a kernel gave up waiting since the last check, or QVLA_ERR_INVALID_ARG if an
+ * attention or cache kernel met an index in device memory that it had to skip. */
 qvla_status qvla_check_device(void* stream);
 
 #ifdef __cplusplus

@@ -13,6 +13,7 @@
 
 #include "../../include/qvla.h"
 #include "../../include/qvla_debug.h"
+#include "api_status.h"
 #include "kernels.h"
 #include "pack.h"
 
@@ -37,8 +38,12 @@ struct qvla_layer {
 };
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
+
+namespace qvla {
+
+void clear_error() { g_last_error.clear(); }
 
 qvla_status fail(qvla_status s, const char* fmt, ...) {
   char buf[512];
@@ -54,32 +59,6 @@ qvla_status cuda_fail(cudaError_t e, const char* what) {
   return fail(e == cudaErrorMemoryAllocation ? QVLA_ERR_OOM : QVLA_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-#define QVLA_CUDA(call, what)                        \
-  do {                                               \
-    cudaError_t e_ = (call);                         \
-    if (e_ != cudaSuccess) return cuda_fail(e_, what); \
-  } while (0)
-
-int ilog2_exact(int v) {
-  if (v < 1 || (v & (v - 1))) return -1;
-  int l = 0;
-  while ((1 << l) < v) ++l;
-  return l;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-qvla_status check_shape(int N, int K, int had_block) {
-  if (K <= 0 || K % 128 != 0) return fail(QVLA_ERR_INVALID_ARG, "K=%d must be a positive multiple of 128", K);
-  if (K > 16384) return fail(QVLA_ERR_UNSUPPORTED, "K=%d exceeds 16384 (exact float32 accumulation bound)", K);
-  if (N <= 0 || N % 16 != 0) return fail(QVLA_ERR_INVALID_ARG, "N=%d must be a positive multiple of 16", N);
-  const int lb = ilog2_exact(had_block);
-  if (lb < 0) return fail(QVLA_ERR_INVALID_ARG, "had_block=%d is not a power of two", had_block);
-  if (had_block > 4096) return fail(QVLA_ERR_UNSUPPORTED, "had_block=%d exceeds 4096", had_block);
-  if (K % had_block != 0) return fail(QVLA_ERR_INVALID_ARG, "K=%d is not a multiple of had_block=%d", K, had_block);
-  return QVLA_OK;
-}
-
 int num_sms(int device) {
   static std::mutex mu;
   static std::vector<int> cache;
@@ -91,6 +70,33 @@ int num_sms(int device) {
     cache[device] = v;
   }
   return cache[device];
+}
+
+}  // namespace qvla
+
+using qvla::aligned16;
+using qvla::cuda_fail;
+using qvla::fail;
+using qvla::num_sms;
+
+namespace {
+
+int ilog2_exact(int v) {
+  if (v < 1 || (v & (v - 1))) return -1;
+  int l = 0;
+  while ((1 << l) < v) ++l;
+  return l;
+}
+
+qvla_status check_shape(int N, int K, int had_block) {
+  if (K <= 0 || K % 128 != 0) return fail(QVLA_ERR_INVALID_ARG, "K=%d must be a positive multiple of 128", K);
+  if (K > 16384) return fail(QVLA_ERR_UNSUPPORTED, "K=%d exceeds 16384 (exact float32 accumulation bound)", K);
+  if (N <= 0 || N % 16 != 0) return fail(QVLA_ERR_INVALID_ARG, "N=%d must be a positive multiple of 16", N);
+  const int lb = ilog2_exact(had_block);
+  if (lb < 0) return fail(QVLA_ERR_INVALID_ARG, "had_block=%d is not a power of two", had_block);
+  if (had_block > 4096) return fail(QVLA_ERR_UNSUPPORTED, "had_block=%d exceeds 4096", had_block);
+  if (K % had_block != 0) return fail(QVLA_ERR_INVALID_ARG, "K=%d is not a multiple of had_block=%d", K, had_block);
+  return QVLA_OK;
 }
 
 size_t round256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
@@ -1045,14 +1051,19 @@ qvla_status qvla_debug_gemm_plan_codes(int codes, int M, int K, int N, int gated
 
 qvla_status qvla_check_device(void* stream) {
   g_last_error.clear();
-  unsigned int word = 0, word_tmem = 0, word_fused = 0, word_gemv = 0, word_rqp = 0;
+  unsigned int word = 0, word_tmem = 0, word_fused = 0, word_gemv = 0, word_rqp = 0, word_prompt = 0, word_kv4 = 0, word_akv4 = 0;
   QVLA_CUDA(qvla::read_and_clear_error_word(&word, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_tmem(&word_tmem, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_fused(&word_fused, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_gemv(&word_gemv, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_rqp(&word_rqp, static_cast<cudaStream_t>(stream)), "device check");
-  if ((word | word_tmem | word_fused | word_gemv | word_rqp) & 1u)
-    return fail(QVLA_ERR_TIMEOUT, "a kernel wait ran out of its time limit");
+  QVLA_CUDA(qvla::read_and_clear_error_word_prompt(&word_prompt, static_cast<cudaStream_t>(stream)), "device check");
+  QVLA_CUDA(qvla::read_and_clear_error_word_kv4(&word_kv4, static_cast<cudaStream_t>(stream)), "device check");
+  QVLA_CUDA(qvla::read_and_clear_error_word_attention_kv4(&word_akv4, static_cast<cudaStream_t>(stream)), "device check");
+  const unsigned int all = word | word_tmem | word_fused | word_gemv | word_rqp | word_prompt | word_kv4 | word_akv4;
+  if (all & 1u) return fail(QVLA_ERR_TIMEOUT, "a kernel wait ran out of its time limit");
+  if (all & 2u)
+    return fail(QVLA_ERR_INVALID_ARG, "an offset, length or page index in device memory was out of range; its tokens were skipped");
   return QVLA_OK;
 }
 

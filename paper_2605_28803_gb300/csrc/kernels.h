@@ -143,4 +143,72 @@ cudaError_t set_debug_hooks_fused(unsigned long long wait_limit_ns, int hold_loa
 cudaError_t set_debug_hooks_gemv(unsigned long long wait_limit_ns, int hold_loads);
 cudaError_t read_and_clear_error_word_gemv(unsigned int* out, cudaStream_t stream);
 
+// ---- attention over packed prompts (attention_prompt.cu) ----
+struct PromptArgs {
+  const void* q;           // device [total_q] tokens, element (t, h, c) at t * q_stride + h * head_dim + c
+  const void* k;
+  const void* v;
+  int dt;                  // 0 f16, 1 bf16
+  int heads, kv_heads, head_dim;
+  int64_t q_stride, k_stride, v_stride;  // elements
+  int batch;
+  const int32_t* cu_q;     // device [batch + 1]
+  const int32_t* cu_k;
+  int total_q, total_k;
+  float scale;
+  int causal;
+  void* o;                 // device [total_q][heads][head_dim]
+  int num_sms;
+  cudaStream_t stream;
+};
+cudaError_t launch_attention_prompt(const PromptArgs& a);
+cudaError_t read_and_clear_error_word_prompt(unsigned int* out, cudaStream_t stream);
+
+// ---- the 4-bit key/value cache (kv4_cache.cu) and attention over it (attention_kv4.cu) ----
+struct Kv4Pool {
+  uint8_t* base;           // [num_pages][kv_heads] blocks, see qvla_kv4_cache
+  int num_pages, log_page, kv_heads, head_dim, rotate;
+};
+struct Kv4RowsArgs {
+  Kv4Pool pool;
+  void* k;                 // append: device in, element (t, h, c) at t * k_stride + h * head_dim + c;
+  void* v;                 // gather: device out
+  int64_t k_stride, v_stride;
+  int dt;                  // 0 f16, 1 bf16
+  int batch;
+  const int32_t* cu;       // device [batch + 1]
+  int total;
+  const int32_t* table;    // device [batch][max_pages]
+  int max_pages;
+  const int32_t* start;    // device [batch] or null (0)
+  cudaStream_t stream;
+};
+cudaError_t launch_kv4_append(const Kv4RowsArgs& a);
+cudaError_t launch_kv4_gather(const Kv4RowsArgs& a);
+cudaError_t read_and_clear_error_word_kv4(unsigned int* out, cudaStream_t stream);
+
+struct Kv4AttentionArgs {
+  Kv4Pool pool;
+  const void* q;
+  int dt, heads;
+  int64_t q_stride;
+  int batch;
+  const int32_t* cu_q;
+  int total_q, max_q;
+  const int32_t* table;
+  int max_pages;
+  const int32_t* kv_len;   // device [batch]
+  int max_len;
+  float scale;
+  int causal;
+  void* o;
+  void* ws;                // room for the partial results of a split over the keys, or null
+  size_t ws_bytes;
+  int num_sms;
+  cudaStream_t stream;
+};
+size_t attention_kv4_workspace(const Kv4AttentionArgs& a);
+cudaError_t launch_attention_kv4(const Kv4AttentionArgs& a);
+cudaError_t read_and_clear_error_word_attention_kv4(unsigned int* out, cudaStream_t stream);
+
 }  // namespace qvla

@@ -1,0 +1,117 @@
+// Device helpers of the attention operators: packed sequences, the 4-bit cache's pages, rotated heads.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace qvla {
+
+// The sequence of packed row t: the last b with cu[b] <= t, found by the whole warp, 32 offsets a round.  False when t lies in
+// no sequence.  Any contents of cu are safe: b stays in [0, batch).
+__device__ __forceinline__ bool find_sequence(const int32_t* __restrict__ cu, int batch, int t, int& b, int& first) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = batch;
+  while (n > 1) {
+    const int step = (n + 31) >> 5;
+    const bool at_or_before = lane * step < n && __ldg(cu + lo + lane * step) <= t;
+    const int c = max(1, __popc(__ballot_sync(0xffffffffu, at_or_before)));
+    lo += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  b = lo;
+  first = __ldg(cu + lo);
+  return first <= t && t < __ldg(cu + lo + 1);
+}
+
+__device__ __forceinline__ void report_index() { atomicOr(&g_error_word, kErrIndex); }
+
+// Bytes of one head's tokens of a page, and the place of its parts.
+__device__ __forceinline__ size_t kv4_block_bytes(const Kv4Pool& p) { return static_cast<size_t>(p.head_dim + 8) << p.log_page; }
+
+// The block that holds position pos of sequence b for a head; null (and reported) when the table or the page is left.
+__device__ __forceinline__ uint8_t* kv4_block(const Kv4Pool& p, const int32_t* __restrict__ table, int max_pages, int b, int64_t pos,
+                                              int head) {
+  if (pos < 0 || (pos >> p.log_page) >= max_pages) {
+    report_index();
+    return nullptr;
+  }
+  const int page = __ldg(table + static_cast<size_t>(b) * max_pages + (pos >> p.log_page));
+  if (page < 0 || page >= p.num_pages) {
+    report_index();
+    return nullptr;
+  }
+  return p.base + (static_cast<size_t>(page) * p.kv_heads + head) * kv4_block_bytes(p);
+}
+
+// x . H for a head spread over a team of kTeam adjacent lanes, 8 consecutive channels a lane: butterflies of distance 1, 2, 4
+// in registers, then 8, 16, ... between lanes, each output a + b or a - b (so any order of evaluation gives the same
+// bits), and the factor 1 / sqrt(8 kTeam) last.
+template <int kTeam>
+__device__ __forceinline__ void rotate_head(float (&y)[8]) {
+#pragma unroll
+  for (int h = 1; h < 8; h *= 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if ((i & h) == 0) {
+        const float a = y[i], b = y[i + h];
+        y[i] = a + b;
+        y[i + h] = a - b;
+      }
+    }
+  }
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 1; h < kTeam; h *= 2) {
+    const bool high = (lane & h) != 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float o = __shfl_xor_sync(0xffffffffu, y[i], h);
+      y[i] = high ? o - y[i] : y[i] + o;
+    }
+  }
+  constexpr float f = kTeam == 8 ? 0.125f : kTeam == 16 ? 0.08838834764831845f : 0.0625f;  // float32(1 / sqrt(8 kTeam))
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] *= f;
+}
+
+template <typename T>
+struct Pair;
+template <>
+struct Pair<__half> {
+  using V = __half2;
+  static __device__ __forceinline__ float2 to_float(V v) { return __half22float2(v); }
+  static __device__ __forceinline__ V from_float(float a, float b) { return __floats2half2_rn(a, b); }
+};
+template <>
+struct Pair<__nv_bfloat16> {
+  using V = __nv_bfloat162;
+  static __device__ __forceinline__ float2 to_float(V v) { return __bfloat1622float2(v); }
+  static __device__ __forceinline__ V from_float(float a, float b) { return __floats2bfloat162_rn(a, b); }
+};
+
+// 8 consecutive 16-bit values at a 16-byte aligned address.
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint4& v, float (&y)[8]) {
+  const typename Pair<T>::V* h = reinterpret_cast<const typename Pair<T>::V*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = Pair<T>::to_float(h[i]);
+    y[2 * i] = f.x;
+    y[2 * i + 1] = f.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
+  uint4 v;
+  typename Pair<T>::V* h = reinterpret_cast<typename Pair<T>::V*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = Pair<T>::from_float(y[2 * i], y[2 * i + 1]);
+  return v;
+}
+
+}  // namespace qvla

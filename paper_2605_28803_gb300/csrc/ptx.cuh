@@ -6,11 +6,13 @@
 
 namespace qvla {
 
-// Device-side error word: bit 0 = a bounded wait ran out of time.  Each translation unit
-// that waits has its own copy; the host reads and clears it through qvla_check_device().
+// Device-side error word: bit 0 = a bounded wait ran out of time, bit 1 = an index in device memory
+// left the buffer that it indexes (and was skipped).  Each translation unit that can set it has
+// its own copy; the host reads and clears it through qvla_check_device().
 static __device__ unsigned int g_error_word;
 
 constexpr unsigned int kErrTimeout = 1u;
+constexpr unsigned int kErrIndex = 2u;
 // A wait gives up after this many nanoseconds of the global timer (a healthy wait in these
 // kernels lasts microseconds).  g_wait_limit_ns holds the limit in force (per translation unit,
 // like the error word); only a test hook lowers it.

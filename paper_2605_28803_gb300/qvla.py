@@ -23,6 +23,7 @@ STATUS = {0: "QVLA_OK", 1: "QVLA_ERR_INVALID_ARG", 2: "QVLA_ERR_UNSUPPORTED", 3:
 
 # every symbol include/*.h declares, with (restype, argtypes)
 _P, _I, _S, _D = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_double
+_L, _F = ctypes.c_int64, ctypes.c_float
 SIGNATURES = {
     "qvla_last_error": (ctypes.c_char_p, []),
     "qvla_abi_version": (_I, []),
@@ -57,6 +58,12 @@ SIGNATURES = {
     "qvla_check_device": (_I, [_P]),
     "qvla_debug_set_hooks": (_I, [ctypes.c_ulonglong, _I]),
     "qvla_debug_gemm_plan": (_I, [_I, _I, _I, _I, _I, _I, _P, _P]),
+    "qvla_attention_prompt": (_I, [_P, _P, _P, _I, _I, _I, _I, _L, _L, _L, _I, _P, _I, _P, _I, _F, _I, _P, _P]),
+    "qvla_kv4_pool_bytes": (_S, [_I, _I, _I, _I]),
+    "qvla_kv4_append": (_I, [_P, _P, _P, _I, _L, _L, _I, _P, _I, _P, _I, _P, _P]),
+    "qvla_kv4_gather": (_I, [_P, _I, _P, _I, _P, _I, _P, _P, _P, _I, _P]),
+    "qvla_attention_kv4_workspace_bytes": (_S, [_I, _I, _I, _I, _I, _I, _I]),
+    "qvla_attention_kv4": (_I, [_P, _P, _I, _I, _L, _I, _P, _I, _I, _P, _I, _P, _I, _F, _I, _P, _P, _S, _P]),
     "qvla_debug_gemm_plan_codes": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P]),
 }
 
@@ -293,6 +300,61 @@ def qvla_w4a8_linear(layer: Layer, x, M: int, step: int, y, workspace, workspace
 def qvla_gemm_w4a8(layer: Layer, xq, xscale, M: int, y, acc, workspace, workspace_bytes: int, stream=None) -> None:
     _check(_lib.qvla_gemm_w4a8(layer.handle, _ptr(xq), _ptr(xscale), M, _ptr(y), _ptr(acc), _ptr(workspace),
                                workspace_bytes, _stream(stream)))
+
+
+def qvla_attention_prompt(q, k, v, dt: int, heads: int, kv_heads: int, head_dim: int, q_stride: int, k_stride: int,
+                          v_stride: int, batch: int, cu_q, total_q: int, cu_k, total_k: int, scale: float, causal: bool,
+                          o, stream=None) -> None:
+    """Softmax attention over packed prompts; strides in elements between tokens."""
+    _check(_lib.qvla_attention_prompt(_ptr(q), _ptr(k), _ptr(v), dt, heads, kv_heads, head_dim, q_stride, k_stride,
+                                      v_stride, batch, _ptr(cu_q), total_q, _ptr(cu_k), total_k, scale,
+                                      1 if causal else 0, _ptr(o), _stream(stream)))
+
+
+class _Kv4Struct(ctypes.Structure):
+    _fields_ = [("pool", _P), ("num_pages", _I), ("page_size", _I), ("kv_heads", _I), ("head_dim", _I), ("rotate", _I)]
+
+
+class Kv4Cache:
+    """A 4-bit key/value cache (qvla_kv4_cache) over `pool`, a device buffer of qvla_kv4_pool_bytes(...) bytes that the
+    caller owns and this object keeps alive."""
+
+    def __init__(self, pool, num_pages: int, page_size: int, kv_heads: int, head_dim: int, rotate: bool = True):
+        if pool is not None and pool.numel() * pool.element_size() < qvla_kv4_pool_bytes(num_pages, page_size, kv_heads,
+                                                                                         head_dim):
+            raise ValueError("the pool is smaller than qvla_kv4_pool_bytes(...)")
+        self.pool = pool
+        self.struct = _Kv4Struct(_ptr(pool), num_pages, page_size, kv_heads, head_dim, 1 if rotate else 0)
+        self.ref = ctypes.addressof(self.struct)
+
+
+def qvla_kv4_pool_bytes(num_pages: int, page_size: int, kv_heads: int, head_dim: int) -> int:
+    return int(_lib.qvla_kv4_pool_bytes(num_pages, page_size, kv_heads, head_dim))
+
+
+def qvla_kv4_append(cache: Kv4Cache, k, v, dt: int, k_stride: int, v_stride: int, batch: int, cu_new, total_new: int,
+                    page_table, max_pages: int, start, stream=None) -> None:
+    _check(_lib.qvla_kv4_append(cache.ref, _ptr(k), _ptr(v), dt, k_stride, v_stride, batch, _ptr(cu_new), total_new,
+                                _ptr(page_table), max_pages, _ptr(start), _stream(stream)))
+
+
+def qvla_kv4_gather(cache: Kv4Cache, batch: int, cu, total: int, page_table, max_pages: int, start, k, v, dt: int,
+                    stream=None) -> None:
+    _check(_lib.qvla_kv4_gather(cache.ref, batch, _ptr(cu), total, _ptr(page_table), max_pages, _ptr(start), _ptr(k),
+                                _ptr(v), dt, _stream(stream)))
+
+
+def qvla_attention_kv4_workspace_bytes(heads: int, kv_heads: int, head_dim: int, batch: int, total_q: int, max_q: int,
+                                       max_len: int) -> int:
+    return int(_lib.qvla_attention_kv4_workspace_bytes(heads, kv_heads, head_dim, batch, total_q, max_q, max_len))
+
+
+def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, batch: int, cu_q, total_q: int, max_q: int,
+                       page_table, max_pages: int, kv_len, max_len: int, scale: float, causal: bool, o, workspace=None,
+                       workspace_bytes: int = 0, stream=None) -> None:
+    _check(_lib.qvla_attention_kv4(cache.ref, _ptr(q), dt, heads, q_stride, batch, _ptr(cu_q), total_q, max_q,
+                                   _ptr(page_table), max_pages, _ptr(kv_len), max_len, scale, 1 if causal else 0, _ptr(o),
+                                   _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def qvla_check_device(stream=None) -> None:
