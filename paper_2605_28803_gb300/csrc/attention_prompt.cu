@@ -1,80 +1,599 @@
 // Softmax attention over packed prompts: o_i = sum_j p_ij v_j, p_ij = exp(scale q_i.k_j) / sum exp, in one pass over the keys
-// with a running maximum and sum.  A block takes one query head of one token; its warps take every kWarps-th key and
-// are joined at the end.
+// with a running maximum and sum, on the tensor cores.
+//
+// A CTA takes kTiles tiles of 128 query rows of one key/value head and runs them over the keys in blocks of kBlock.  A tile's
+// rows are tokens x the query heads that share the key/value head, so grouped heads fill a tile that one head's tokens would
+// leave half empty, and read K and V once.  Per block and tile:
+//   S = Q K^T        tcgen05, operands from shared memory (TMA, 128-byte swizzle), S in TMEM
+//   P = exp2(S c - m), rounded to 16 bits, over S's own columns in TMEM: a thread a row, no exchange between threads
+//   O += P V         tcgen05 with A = P from TMEM and B = V as it lies (MN-major), O in TMEM
+// While a warpgroup works out one tile's P, the tensor cores run the other tile's products; with 256 channels O takes half of
+// TMEM, so there is one tile with two S buffers instead, and its next S is made while P is worked out.
+// The maximum that P is taken against moves only when a row's maximum has grown by more than 2^8 (p <= 256 is harmless in
+// both types, and numerator and denominator use the same one), so O is rarely read back to be rescaled.
+//
+// Keys that some row of the CTA does not see (the diagonal's blocks, a sequence's last block) need care on the value side, where
+// 0 * NaN would spread: two warps zero the rows behind the sequence's end and take NaN and infinities out of such
+// blocks; a row that does see one of those gets it back, exactly, when it is written out.
+#include <cuda.h>
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include <mutex>
+#include <set>
+#include <utility>
+
+#include "griddep.cuh"
 #include "kv4.cuh"
 
 namespace qvla {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr float kLog2e = 1.4426950408889634f;
+// Test hook: nonzero makes the load warp issue no copy (see qvla_debug.h).
+static __device__ int g_debug_hold_loads;
 
-template <typename T, int kDim>
-__global__ void __launch_bounds__(32 * kWarps) attention_prompt_kernel(const PromptArgs a) {
-  constexpr int kPer = kDim / 32;
-  __shared__ float s_acc[kWarps][kDim], s_m[kWarps], s_l[kWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t = blockIdx.x, h = blockIdx.y, kvh = h / (a.heads / a.kv_heads);
-  int b, q0;
-  if (!find_sequence(a.cu_q, a.batch, t, b, q0)) return;
-  const int n = min(a.cu_q[b + 1], a.total_q) - q0;
-  const int k0 = min(max(a.cu_k[b], 0), a.total_k), k1 = min(max(a.cu_k[b + 1], k0), a.total_k);
-  const int keys = k1 - k0, seen = a.causal ? min(keys, keys - n + (t - q0) + 1) : keys;
-  float q[kPer], acc[kPer];
-  const T* qp = static_cast<const T*>(a.q) + t * a.q_stride + h * kDim + lane * kPer;
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) {
-    q[c] = static_cast<float>(qp[c]) * (a.scale * kLog2e);
-    acc[c] = 0.0f;
-  }
-  float m = -INFINITY, l = 0.0f;
-  for (int j = warp; j < seen; j += kWarps) {
-    const T* kp = static_cast<const T*>(a.k) + (k0 + j) * a.k_stride + kvh * kDim + lane * kPer;
-    const T* vp = static_cast<const T*>(a.v) + (k0 + j) * a.v_stride + kvh * kDim + lane * kPer;
-    float s = 0.0f;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) s = fmaf(q[c], static_cast<float>(kp[c]), s);
-#pragma unroll
-    for (int x = 16; x > 0; x /= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
-    const float top = fmaxf(m, s), keep = m == top ? 1.0f : exp2f(m - top), p = exp2f(s - top);
-    m = top;
-    l = l * keep + p;
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) acc[c] = fmaf(p, static_cast<float>(vp[c]), acc[c] * keep);
-  }
-  if (lane == 0) {
-    s_m[warp] = m;
-    s_l[warp] = l;
-  }
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) s_acc[warp][lane * kPer + c] = acc[c];
-  __syncthreads();
-  float top = -INFINITY, sum = 0.0f;
-  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w]);
-  for (int w = 0; w < kWarps; ++w) sum += s_l[w] == 0.0f ? 0.0f : s_l[w] * exp2f(s_m[w] - top);
-  for (int c = threadIdx.x; c < kDim; c += 32 * kWarps) {
-    float o = 0.0f;
-    for (int w = 0; w < kWarps; ++w) o += s_l[w] == 0.0f ? 0.0f : s_acc[w][c] * exp2f(s_m[w] - top);
-    static_cast<T*>(a.o)[(static_cast<size_t>(t) * a.heads + h) * kDim + c] = static_cast<T>(sum == 0.0f ? 0.0f : o / sum);
-  }
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRowsPerTile = 128;
+constexpr float kGrowth = 8.0f;  // log2 of what a row's maximum may grow by before its O is rescaled
+constexpr int kWarpLoad = 0, kWarpMma = 1, kWarpGuard = 2, kGuardWarps = 2, kWarpSoftmax = 4;
+
+template <int kDim>
+struct Shape {
+  static constexpr int kTiles = kDim == 256 ? 1 : 2;
+  static constexpr int kBlock = kDim == 256 ? 64 : 128;
+  static constexpr int kStages = kDim == 64 ? 4 : 2;          // of K, and of V
+  static constexpr int kThreads = 32 * (kWarpSoftmax + 4 * kTiles);
+  static constexpr int kQBytes = kRowsPerTile * kDim * 2;     // one tile
+  static constexpr int kKvBytes = kBlock * kDim * 2;          // one block of K or V
+  static constexpr int kSmem = kTiles * kQBytes + 2 * kStages * kKvBytes + 1024;
+  static constexpr int kOCol = kDim == 256 ? 256 : 2 * kBlock;  // TMEM: two S buffers, then O of each tile
+};
+
+struct PromptParams {
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  void* o;
+  const void* v;
+  int64_t v_stride;
+  int batch, total_q, total_k;
+  int heads, kv_heads, group;  // group: query heads on a key/value head
+  int chunk_heads, chunks;     // of them in one tile; tiles' head chunks
+  int tokens;                  // tokens in one tile
+  int causal;
+  float c;                     // scale * log2(e)
+};
+
+struct Work {
+  int q0, n, k0, keys;  // the sequence's first row, queries, first key and keys
+  int token;            // first token of the CTA's first tile
+  int kvh, head;        // key/value head; first query head
+  int heads;            // query heads in the tile
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 template <typename T>
-void launch(const PromptArgs& a) {
-  const dim3 grid(a.total_q, a.heads);
-  if (a.head_dim == 64) attention_prompt_kernel<T, 64><<<grid, 32 * kWarps, 0, a.stream>>>(a);
-  if (a.head_dim == 128) attention_prompt_kernel<T, 128><<<grid, 32 * kWarps, 0, a.stream>>>(a);
-  if (a.head_dim == 256) attention_prompt_kernel<T, 256><<<grid, 32 * kWarps, 0, a.stream>>>(a);
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typename Pair<T>::V v = Pair<T>::from_float(a, b);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// Two 16-bit values of type T: the bits of those that are not finite, the others zero.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  constexpr uint32_t e = sizeof(T) == 2 && std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+  uint32_t m = 0;
+  if ((w & e) == e) m |= 0xffffu;
+  if (((w >> 16) & e) == e) m |= 0xffff0000u;
+  return w & m;
+}
+template <typename T>
+__device__ __forceinline__ bool any_not_finite(uint32_t w) {
+  constexpr uint32_t e = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
+  constexpr uint32_t one = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+  return (((w & e) + one) & 0x80008000u) != 0;  // an exponent of all ones carries into the sign's place
+}
+
+// Keys that query token i of its sequence sees.
+__device__ __forceinline__ int seen_by(const Work& w, int causal, int i) {
+  return causal ? max(0, min(w.keys, w.keys - w.n + i + 1)) : w.keys;
+}
+
+template <typename T, int kDim>
+__global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
+    attention_prompt_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                            const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ PromptParams p) {
+  using C = Shape<kDim>;
+  constexpr int kTiles = C::kTiles, kBlock = C::kBlock, kStages = C::kStages;
+  constexpr int kBoxes = kDim / 64;            // 64-channel boxes of a row
+  constexpr int kQBox = kRowsPerTile * 128, kKvBox = kBlock * 128;
+  constexpr int kBf16 = std::is_same<T, __half>::value ? 0 : 1;
+
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_q[2], bar_kfull[kStages], bar_kempty[kStages], bar_vfull[kStages], bar_vok[kStages],
+      bar_vempty[kStages], bar_s[2], bar_p[2], bar_o[2], bar_done;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_found, s_bad;
+  __shared__ Work s_work;
+  uint8_t* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  uint8_t* const smem_k = smem + kTiles * C::kQBytes;
+  uint8_t* const smem_v = smem_k + kStages * C::kKvBytes;
+
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  if (warp == kWarpMma) tmem_alloc<512>(smem_u32(&s_tmem));
+  if (threadIdx.x == 32 * kWarpGuard) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bar_q[i]), 1);
+      mbar_init(smem_u32(&bar_s[i]), 1);
+      mbar_init(smem_u32(&bar_p[i]), 4);
+      mbar_init(smem_u32(&bar_o[i]), 1);
+    }
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_u32(&bar_kfull[i]), 1);
+      mbar_init(smem_u32(&bar_kempty[i]), 1);
+      mbar_init(smem_u32(&bar_vfull[i]), 1);
+      mbar_init(smem_u32(&bar_vok[i]), kGuardWarps);
+      mbar_init(smem_u32(&bar_vempty[i]), 1);
+    }
+    mbar_init(smem_u32(&bar_done), 1);
+    mbar_init_fence();
+    s_bad = 0;
+  }
+  griddep_wait();  // the offsets, q, k and v may come from the previous kernel, which may still read o
+  if (warp == 0) {  // the sequence and tile of this CTA: 32 sequences a round, the last tiles of a sequence first
+    const int per = p.kv_heads * p.chunks;
+    int tile = static_cast<int>(blockIdx.x / per);
+    const int rest = static_cast<int>(blockIdx.x % per);
+    bool found = false;
+    for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {
+      const int b = b0 + lane;
+      int first = 0, n = 0;
+      if (b < p.batch) {
+        first = min(max(p.cu_q[b], 0), p.total_q);
+        n = min(max(p.cu_q[b + 1], first), p.total_q) - first;
+      }
+      const int tiles = (n + kTiles * p.tokens - 1) / (kTiles * p.tokens);
+      int upto = tiles;
+      for (int s = 1; s < 32; s *= 2) {
+        const int o = __shfl_up_sync(0xffffffffu, upto, s);
+        if (lane >= s) upto += o;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, tile < upto);
+      if (hit == 0) {
+        tile -= __shfl_sync(0xffffffffu, upto, 31);
+        continue;
+      }
+      found = true;
+      if (lane == __ffs(hit) - 1) {
+        Work w;
+        w.q0 = first;
+        w.n = n;
+        w.k0 = min(max(p.cu_k[b], 0), p.total_k);
+        w.keys = min(max(p.cu_k[b + 1], w.k0), p.total_k) - w.k0;
+        w.token = (upto - 1 - tile) * kTiles * p.tokens;
+        w.kvh = rest / p.chunks;
+        w.head = w.kvh * p.group + (rest % p.chunks) * p.chunk_heads;
+        w.heads = min(p.chunk_heads, (w.kvh + 1) * p.group - w.head);
+        s_work = w;
+      }
+    }
+    if (lane == 0) s_found = found ? 1 : 0;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  griddep_launch_dependents();
+  const uint32_t tmem = s_tmem;
+  if (s_found) {
+    const Work w = s_work;
+    // per tile: blocks to run, and the first of them that some row does not see whole
+    int blocks[kTiles], partial[kTiles], most = 0, guard_from = 1 << 30;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const int first = w.token + t * p.tokens, last = min(first + p.tokens, w.n) - 1;
+      blocks[t] = first < w.n ? (seen_by(w, p.causal, last) + kBlock - 1) / kBlock : 0;
+      partial[t] = seen_by(w, p.causal, first) / kBlock;
+      most = max(most, blocks[t]);
+      if (blocks[t] > 0) guard_from = min(guard_from, partial[t]);
+    }
+
+    if (warp == kWarpLoad) {
+      // ------------------------------------------------------------------ TMA
+      if constexpr (kTiles == 2) setmaxnreg_dec<64>();
+      bool ok = *const_cast<volatile int*>(&g_debug_hold_loads) == 0;
+      int issued = 0;
+      if (ok && most > 0) {
+        if (elect_one()) {
+          tma_prefetch_desc(&tmap_k);
+          tma_prefetch_desc(&tmap_v);
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            if (blocks[t] == 0) continue;
+            const uint32_t bar = smem_u32(&bar_q[t]);
+            mbar_arrive_expect_tx(bar, static_cast<uint32_t>(p.chunk_heads * p.tokens * kDim * 2));
+            for (int c = 0; c < kBoxes; ++c)
+              tma_load_3d(smem_u32(smem + t * C::kQBytes + c * kQBox), &tmap_q, c * 64, w.head, w.q0 + w.token + t * p.tokens, bar);
+          }
+        }
+        __syncwarp();
+        for (int j = 0; j < most; ++j) {
+          const int s = j % kStages;
+          const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_kempty[s]), ph ^ 1u))) break;
+          if (elect_one()) {
+            const uint32_t bar = smem_u32(&bar_kfull[s]);
+            mbar_arrive_expect_tx(bar, C::kKvBytes);
+            for (int c = 0; c < kBoxes; ++c)
+              tma_load_3d(smem_u32(smem_k + s * C::kKvBytes + c * kKvBox), &tmap_k, c * 64, w.kvh, w.k0 + j * kBlock, bar);
+          }
+          __syncwarp();
+          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_vempty[s]), ph ^ 1u))) {
+            mbar_wait(smem_u32(&bar_kfull[s]), ph);
+            break;
+          }
+          if (elect_one()) {
+            const uint32_t bar = smem_u32(&bar_vfull[s]);
+            mbar_arrive_expect_tx(bar, C::kKvBytes);
+            for (int c = 0; c < kBoxes; ++c)
+              tma_load_3d(smem_u32(smem_v + s * C::kKvBytes + c * kKvBox), &tmap_v, c * 64, w.kvh, w.k0 + j * kBlock, bar);
+          }
+          __syncwarp();
+          issued = j + 1;
+        }
+        // before leaving, let every load land
+        for (int t = 0; t < kTiles; ++t)
+          if (blocks[t] > 0) mbar_wait(smem_u32(&bar_q[t]), 0);
+        for (int j = max(0, issued - kStages); j < issued; ++j) {
+          const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
+          mbar_wait(smem_u32(&bar_kfull[j % kStages]), ph);
+          mbar_wait(smem_u32(&bar_vfull[j % kStages]), ph);
+        }
+      }
+      __syncwarp();
+    } else if (warp == kWarpMma) {
+      // ------------------------------------------------------------------ MMA
+      if constexpr (kTiles == 2) setmaxnreg_dec<64>();
+      constexpr uint32_t idesc_s = idesc_f16_f32(kBf16, kRowsPerTile, kBlock, 0);
+      constexpr uint32_t idesc_o = idesc_f16_f32(kBf16, kRowsPerTile, kDim, 1);
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, int n) {  // completion n of a barrier
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), static_cast<uint32_t>(n) & 1u));
+        return ok;
+      };
+      // S of tile t (buffer b) from K's stage s
+      auto scores = [&](int t, int b, int s) {
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t d = tmem + static_cast<uint32_t>(b * kBlock);
+#pragma unroll
+          for (int i = 0; i < kDim / 16; ++i) {
+            const uint32_t at = (i / 4) * kQBox + (i % 4) * 32, bt = (i / 4) * kKvBox + (i % 4) * 32;
+            mma_f16_ss(d, smem_desc_sw128(smem_u32(smem + t * C::kQBytes) + at), smem_desc_sw128(smem_u32(smem_k + s * C::kKvBytes) + bt),
+                       idesc_s, i != 0);
+          }
+          mma_commit(smem_u32(&bar_s[b]));
+        }
+        __syncwarp();
+      };
+      // O of tile t += P (buffer b) V (stage s)
+      auto values = [&](int t, int b, int s, bool first) {
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t d = tmem + static_cast<uint32_t>(C::kOCol + t * kDim), a = tmem + static_cast<uint32_t>(b * kBlock);
+#pragma unroll
+          for (int i = 0; i < kBlock / 16; ++i)
+            mma_f16_ts(d, a + static_cast<uint32_t>(i * 8), smem_desc_sw128_mn(smem_u32(smem_v + s * C::kKvBytes) + i * 2048, kKvBox), idesc_o,
+                       !(first && i == 0));
+          mma_commit(smem_u32(&bar_o[t]));
+        }
+        __syncwarp();
+      };
+      auto release = [&](uint64_t* bar) {  // free once every product issued so far is done
+        if (elect_one()) mma_commit(smem_u32(bar));
+        __syncwarp();
+      };
+      if constexpr (kTiles == 2) {
+        if (most > 0 && wait(&bar_kfull[0], 0)) {
+          for (int t = 0; t < 2 && ok; ++t)
+            if (blocks[t] > 0 && wait(&bar_q[t], 0)) scores(t, t, 0);
+          if (ok) release(&bar_kempty[0]);
+        }
+        for (int j = 0; j < most && ok; ++j) {
+          const int s = j % kStages, s1 = (j + 1) % kStages;
+          if (!wait(&bar_vok[s], j / kStages)) break;
+          if (j + 1 < most && !wait(&bar_kfull[s1], (j + 1) / kStages)) break;
+          for (int t = 0; t < 2 && ok; ++t) {
+            if (j >= blocks[t] || !wait(&bar_p[t], j)) continue;
+            values(t, t, s, j == 0);
+            if (j + 1 < blocks[t]) scores(t, t, s1);  // over P, which the product before it has read
+          }
+          if (!ok) break;
+          release(&bar_vempty[s]);
+          if (j + 1 < most) release(&bar_kempty[s1]);
+        }
+      } else {
+        if (most > 0 && wait(&bar_kfull[0], 0) && wait(&bar_q[0], 0)) {
+          scores(0, 0, 0);
+          release(&bar_kempty[0]);
+        }
+        for (int j = 0; j < most && ok; ++j) {
+          const int s = j % kStages, s1 = (j + 1) % kStages;
+          if (j + 1 < most) {  // the next S, over the P that the product before last has read
+            if (!wait(&bar_kfull[s1], (j + 1) / kStages)) break;
+            scores(0, (j + 1) & 1, s1);
+            release(&bar_kempty[s1]);
+          }
+          if (!wait(&bar_vok[s], j / kStages) || !wait(&bar_p[j & 1], j >> 1)) break;
+          values(0, j & 1, s, j == 0);
+          release(&bar_vempty[s]);
+        }
+      }
+      if (elect_one()) {
+        mma_commit(smem_u32(&bar_done));  // every product issued above has completed once this flips
+        mbar_wait(smem_u32(&bar_done), 0);
+      }
+      __syncwarp();
+    } else if (warp < kWarpSoftmax) {
+      // ------------------------------------------------------------------ the guard of V
+      if constexpr (kTiles == 2) setmaxnreg_dec<64>();
+      for (int j = 0; j < most; ++j) {
+        const int s = j % kStages;
+        const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_vfull[s]), ph))) break;
+        const int inside = min(kBlock, w.keys - j * kBlock);  // rows of the sequence; the rest is its neighbour's
+        const bool look = p.causal && j >= guard_from;
+        if (look || inside < kBlock) {
+          bool bad = false;
+#pragma unroll 4
+          for (int i = (warp - kWarpGuard) * 32 + lane; i < kBoxes * kBlock * 8; i += 32 * kGuardWarps) {
+            const int row = (i >> 3) % kBlock;
+            uint4* at = reinterpret_cast<uint4*>(smem_v + s * C::kKvBytes + i * 16);
+            if (row >= inside) {
+              *at = make_uint4(0, 0, 0, 0);
+            } else if (look) {
+              const uint4 x = *at;
+              if (any_not_finite<T>(x.x) | any_not_finite<T>(x.y) | any_not_finite<T>(x.z) | any_not_finite<T>(x.w)) {
+                *at = make_uint4(x.x ^ not_finite<T>(x.x), x.y ^ not_finite<T>(x.y), x.z ^ not_finite<T>(x.z), x.w ^ not_finite<T>(x.w));
+                bad = true;
+              }
+            }
+          }
+          if (bad) *const_cast<volatile int*>(&s_bad) = 1;
+          fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar_vok[s]));
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------------ softmax and output: a thread a row
+      if constexpr (kTiles == 2) setmaxnreg_inc<216>();  // 128 x 64 + 256 x 216 of the launch's 384 x 168
+      const int t = kTiles == 2 ? (warp - kWarpSoftmax) >> 2 : 0;
+      const int row = (warp & 3) * 32 + lane;
+      const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+      const int token = w.token + t * p.tokens + row / p.chunk_heads, head = row % p.chunk_heads;
+      const bool live = row < p.tokens * p.chunk_heads && token < w.n && head < w.heads;
+      const int seen = live ? seen_by(w, p.causal, token) : w.keys;
+      const int n = blocks[t], from = partial[t];
+      const uint32_t o_at = tmem + lanes + static_cast<uint32_t>(C::kOCol + t * kDim);
+      float m = -INFINITY, sum = 0.0f;
+      bool ok = true;
+      for (int j = 0; j < n; ++j) {
+        const int b = kTiles == 2 ? t : j & 1, visit = kTiles == 2 ? j : j >> 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s[b]), static_cast<uint32_t>(visit) & 1u))) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t s_at = tmem + lanes + static_cast<uint32_t>(b * kBlock);
+        uint32_t x[kBlock / 32][32];
+#pragma unroll
+        for (int i = 0; i < kBlock / 32; ++i) tmem_ld32(s_at + i * 32, x[i]);
+        tmem_ld_wait();
+        if (j >= from) {  // some row of the tile does not see all of this block
+          const int left = seen - j * kBlock;
+#pragma unroll
+          for (int i = 0; i < kBlock; ++i)
+            if (i >= left) x[i / 32][i % 32] = __float_as_uint(-INFINITY);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i) top = fmaxf(top, __uint_as_float(x[i / 32][i % 32]));
+        top *= p.c;
+        const bool grown = top > m + kGrowth || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xffffffffu, grown)) {
+          const float keep = grown ? ex2(m - top) : 1.0f;
+          if (grown) m = top;
+          sum *= keep;
+          if (j > 0) {
+            // the product of block j - 1 has to be in O (with two tiles S's completion shows that already)
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_o[t]), static_cast<uint32_t>(j - 1) & 1u))) { ok = false; break; }
+            tc_fence_after();
+#pragma unroll 1
+            for (int i = 0; i < kDim / 32; ++i) {
+              uint32_t y[32];
+              tmem_ld32(o_at + i * 32, y);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * keep);
+              tmem_st32(o_at + i * 32, y);
+            }
+            tmem_st_wait();
+          }
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;  // (a row that has seen nothing yet)
+        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < kBlock / 32; ++i) {
+          uint32_t y[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float a = ex2(fmaf(__uint_as_float(x[i][e]), p.c, -ref)), d = ex2(fmaf(__uint_as_float(x[i][e + 1]), p.c, -ref));
+            part[e & 2] += a;
+            part[(e & 2) + 1] += d;
+            y[e / 2] = pack2<T>(a, d);
+          }
+          tmem_st16(s_at + i * 16, y);
+        }
+        sum += (part[0] + part[1]) + (part[2] + part[3]);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar_p[b]));
+      }
+      if (ok && n > 0) {
+        // with one tile the last two products may both be outstanding (the last S was made ahead of the first of them), and a
+        // barrier's phases are waited for one by one
+        if (kTiles == 1 && n > 1) mbar_wait(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 2) & 1u);
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 1) & 1u));
+        tc_fence_after();
+      }
+      if (ok) {
+        const bool bad = *const_cast<volatile int*>(&s_bad) != 0;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        T* const dst = static_cast<T*>(p.o) + (static_cast<size_t>(w.q0 + token) * p.heads + w.head + head) * kDim;
+#pragma unroll 1
+        for (int i = 0; i < kDim / 32; ++i) {
+          float y[32];
+          uint32_t r[32];
+          if (n > 0) {
+            tmem_ld32(o_at + i * 32, r);
+            tmem_ld_wait();
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) y[e] = n > 0 ? __uint_as_float(r[e]) * inv : 0.0f;
+          if (bad && live) {  // the NaN and infinities that the guard took out and this row sees
+            for (int key = guard_from * kBlock; key < seen; ++key) {
+              const T* src = static_cast<const T*>(p.v) + (w.k0 + key) * p.v_stride + w.kvh * kDim + i * 32;
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const float x = static_cast<float>(src[e]);
+                if (!(fabsf(x) < INFINITY)) y[e] += x;
+              }
+            }
+          }
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              uint4 q;
+              q.x = pack2<T>(y[e], y[e + 1]);
+              q.y = pack2<T>(y[e + 2], y[e + 3]);
+              q.z = pack2<T>(y[e + 4], y[e + 5]);
+              q.w = pack2<T>(y[e + 6], y[e + 7]);
+              *reinterpret_cast<uint4*>(dst + i * 32 + e) = q;
+            }
+          }
+        }
+      }
+      tc_fence_before();
+    }
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kWarpMma) tmem_dealloc<512>(tmem);
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+  static std::once_flag once;
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+  });
+  return fn;
+}
+
+// Packed tokens of `heads` heads as 64 channels x box_heads x box_tokens, under the 128-byte swizzle.
+cudaError_t make_tmap_heads(CUtensorMap* m, const void* base, int bf16, int dim, int heads, int tokens, int64_t stride, int box_heads,
+                            int box_tokens) {
+  PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
+  if (!enc) return cudaErrorNotSupported;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(dim) * 2, static_cast<cuuint64_t>(stride) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_tokens)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box,
+                   estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// Raise a kernel's dynamic shared-memory limit, once per kernel and device.
+cudaError_t prepare_kernel(const void* kern, int smem) {
+  static std::mutex mu;
+  static std::set<std::pair<const void*, int>> done;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> lock(mu);
+  if (done.count({kern, dev})) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) done.insert({kern, dev});
+  return e;
+}
+
+template <typename T, int kDim>
+cudaError_t launch(const PromptArgs& a) {
+  using C = Shape<kDim>;
+  auto kern = attention_prompt_kernel<T, kDim>;
+  cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kern), C::kSmem);
+  if (e != cudaSuccess) return e;
+  PromptParams p;
+  p.cu_q = a.cu_q;
+  p.cu_k = a.cu_k;
+  p.o = a.o;
+  p.v = a.v;
+  p.v_stride = a.v_stride;
+  p.batch = a.batch;
+  p.total_q = a.total_q;
+  p.total_k = a.total_k;
+  p.heads = a.heads;
+  p.kv_heads = a.kv_heads;
+  p.group = a.heads / a.kv_heads;
+  // more than 128 query heads on a key/value head: equal chunks of them, a token a tile
+  p.chunks = (p.group + kRowsPerTile - 1) / kRowsPerTile;
+  p.chunk_heads = (p.group + p.chunks - 1) / p.chunks;
+  p.tokens = kRowsPerTile / p.chunk_heads;
+  p.causal = a.causal;
+  p.c = a.scale * kLog2e;
+  // without keys nothing is loaded; the maps still need a valid base
+  const int bf16 = std::is_same<T, __half>::value ? 0 : 1, keys = a.total_k > 0 ? a.total_k : 1;
+  CUtensorMap tq = {}, tk = {}, tv = {};
+  e = make_tmap_heads(&tq, a.q, bf16, kDim, a.heads, a.total_q, a.q_stride, p.chunk_heads, p.tokens);
+  if (e == cudaSuccess) e = make_tmap_heads(&tk, a.total_k > 0 ? a.k : a.q, bf16, kDim, a.kv_heads, keys, a.k_stride, 1, C::kBlock);
+  if (e == cudaSuccess) e = make_tmap_heads(&tv, a.total_k > 0 ? a.v : a.q, bf16, kDim, a.kv_heads, keys, a.v_stride, 1, C::kBlock);
+  if (e != cudaSuccess) return e;
+  // at most this many groups of tiles, however the tokens are spread over the sequences
+  const int64_t per = static_cast<int64_t>(C::kTiles) * p.tokens;
+  const int64_t groups = (a.total_q + static_cast<int64_t>(a.batch) * (per - 1)) / per;
+  const int64_t ctas = groups * a.kv_heads * p.chunks;
+  if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = a.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, kern, tq, tk, tv, p);
+  if (e != cudaSuccess) return e;
+  return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_attention_prompt(const PromptArgs& a) {
-  if (a.dt == 0) launch<__half>(a);
-  else launch<__nv_bfloat16>(a);
-  return cudaGetLastError();
+  if (a.dt == 0)
+    return a.head_dim == 64 ? launch<__half, 64>(a) : a.head_dim == 128 ? launch<__half, 128>(a) : launch<__half, 256>(a);
+  return a.head_dim == 64 ? launch<__nv_bfloat16, 64>(a)
+                          : a.head_dim == 128 ? launch<__nv_bfloat16, 128>(a) : launch<__nv_bfloat16, 256>(a);
 }
 
 cudaError_t read_and_clear_error_word_prompt(unsigned int* out, cudaStream_t stream) {
@@ -84,6 +603,14 @@ cudaError_t read_and_clear_error_word_prompt(unsigned int* out, cudaStream_t str
   if (e != cudaSuccess) return e;
   const unsigned int zero = 0;
   return cudaMemcpyToSymbol(g_error_word, &zero, sizeof(unsigned int));
+}
+
+cudaError_t set_debug_hooks_prompt(unsigned long long wait_limit_ns, int hold_loads) {
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return e;
+  e = cudaMemcpyToSymbol(g_wait_limit_ns, &wait_limit_ns, sizeof(wait_limit_ns));
+  if (e != cudaSuccess) return e;
+  return cudaMemcpyToSymbol(g_debug_hold_loads, &hold_loads, sizeof(hold_loads));
 }
 
 }  // namespace qvla

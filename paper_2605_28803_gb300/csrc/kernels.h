@@ -163,6 +163,7 @@ struct PromptArgs {
 };
 cudaError_t launch_attention_prompt(const PromptArgs& a);
 cudaError_t read_and_clear_error_word_prompt(unsigned int* out, cudaStream_t stream);
+cudaError_t set_debug_hooks_prompt(unsigned long long wait_limit_ns, int hold_loads);
 
 // ---- the 4-bit key/value cache (kv4_cache.cu) and attention over it (attention_kv4.cu) ----
 struct Kv4Pool {

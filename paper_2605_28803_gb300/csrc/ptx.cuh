@@ -332,6 +332,37 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar, uint16_t mask) {
                : "memory");
 }
 
+// ---------------------------------------------------------------------------------------
+// tcgen05.mma, kind::f16: 16-bit operands (A and B of one type), FP32 accumulator in TMEM
+// ---------------------------------------------------------------------------------------
+// Instruction descriptor: D = F32, A = B = F16 (bf16 0) or BF16 (1), shape M x N; B K-major or (b_mn) MN-major.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int bf16, int m, int n, int b_mn) {
+  return (1u << 4) | (static_cast<uint32_t>(bf16) << 7) | (static_cast<uint32_t>(bf16) << 10) | (static_cast<uint32_t>(b_mn) << 16) |
+         (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+// Descriptor of an MN-major tile under the 128-byte swizzle: rows of one k with 64 MN elements (128 bytes), 8-row groups
+// 1024 bytes apart, the next 64 MN elements lbo bytes on.
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t lbo) {
+  uint64_t d = smem_desc_sw128(saddr) & ~(static_cast<uint64_t>(0x3FFF) << 16);
+  return d | (static_cast<uint64_t>(lbo >> 4) << 16);
+}
+// A and B in shared memory.
+__device__ __forceinline__ void mma_f16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// A in TMEM (two consecutive k of a row in each 32-bit column), B in shared memory.
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
 // Arrive once on an mbarrier when every tcgen05.mma issued so far by this thread completes.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
