@@ -467,8 +467,8 @@ size_t qvla_attention_kv4_workspace_bytes(int heads, int kv_heads, int head_dim,
  *   workspace  device, 256-byte aligned, or NULL with 0 bytes: room for the partial results of a split
  *              over the keys (qvla_attention_kv4_workspace_bytes; a smaller one allows a smaller split).
  *              Used only during the call's kernels on `stream`.
- * The probabilities, times the value scales, are rounded to bfloat16 for the product with the codes
- * (their range is a float32's); queries are scaled by a power of two and rounded to float16. */
+ * Each probability times its value scale is rounded to float16 against a power of two that follows the
+ * row's largest (11 bits whatever the scales' size); queries are rounded to float16 likewise. */
 qvla_status qvla_attention_kv4(const qvla_kv4_cache* cache, const void* q, qvla_dtype dt, int heads, int64_t q_stride,
                                int batch, const int32_t* cu_q, int total_q, int max_q, const int32_t* page_table,
                                int max_pages, const int32_t* kv_len, int max_len, float scale, int causal, void* o,

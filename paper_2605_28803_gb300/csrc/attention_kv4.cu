@@ -1,7 +1,28 @@
-// Attention of a few query tokens over the 4-bit key/value cache.  A block takes one query head of one token; its warps take
-// every kWarps-th cached token and are joined at the end.
+// Attention of a few query tokens over the 4-bit key/value cache:
+//   s_j = scale Dk_j (q' . ck_j),   o = sum_j p_j Dv_j cv_j / sum_j p_j,   p_j = exp(s_j - max s)
+// with codes ck, cv, scales Dk, Dv and, for a rotated cache, q' = q H / sqrt(D) and the output o H / sqrt(D).
+//
+// For single tokens the codes' bytes (D + 8 for a token and head) are the bound, for chunks the launch and the matrix
+// instructions.  A warp takes 16 cached tokens at a time, straight from global memory into the registers of mma.m16n8k16
+// fragments: the contraction over channels and the rows of O may be permuted at will, so a lane's share of a key is D / 8
+// contiguous bytes and of a value D / 16, and no byte crosses shared memory.
+//   S^T = K Q^T      A = key codes (16 keys x 16 channels), B = queries (8 rows): grouped heads' single tokens fill 8 columns
+//   O^T += V^T P^T   A = value codes (16 channels x 16 keys), B = P^T, from S^T's accumulators by an 8 x 8 transpose
+// A code becomes float16 by one logic operation and one exact addition on two at a time (the bits 0x6408 ^ code read 1032 +
+// code, 0x5480 ^ (code << 4) read 72 + code).
+//   Dk_j multiplies the score.  Dv_j joins the exponent: the weight that is rounded to float16 for the second product is
+// w_j = exp2(s_j + log2 Dv_j - r) against a running reference r of its own, so it has float16's 11 bits whatever the scales'
+// size, while sum_j p_j is kept in float32 against max s.  References move when a weight would pass 2^8.
+//   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
+// float16.
+//
+// The keys of a sequence are split into chunks of equal length over CTAs, of kWarps warps with every kWarps-th 16 tokens; the
+// chunks' results are joined by a second kernel where a sequence has more than one.
 #include <cuda_runtime.h>
 
+#include <cfloat>
+
+#include "griddep.cuh"
 #include "kv4.cuh"
 
 namespace qvla {
@@ -9,91 +30,528 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kGrowth = 8.0f;  // log2 of the largest weight
+constexpr int kStep = 16;        // cached tokens a warp takes at once
 
-template <typename T, int kDim>
-__global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const Kv4AttentionArgs a) {
-  constexpr int kTeam = kDim / 8, kTeams = 32 / kTeam;
-  __shared__ float s_acc[kWarps * kTeams][kDim], s_m[kWarps * kTeams], s_l[kWarps * kTeams];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = lane / kTeam, tl = lane % kTeam;
-  const int t = blockIdx.x, h = blockIdx.y, kvh = h / (a.heads / a.pool.kv_heads);
-  int b, q0;
-  if (!find_sequence(a.cu_q, a.batch, t, b, q0)) return;
-  const int n = min(a.cu_q[b + 1], a.total_q) - q0, keys = a.kv_len[b];
-  if (n > a.max_q || keys < 0 || keys > a.max_len) {
-    report_index();
-    return;
-  }
-  const int seen = a.causal ? min(keys, keys - n + (t - q0) + 1) : keys;
-  float q[8], acc[8] = {};
-  unpack8<T>(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + t * a.q_stride + h * kDim + tl * 8), q);
-  if (a.pool.rotate) rotate_head<kTeam>(q);
-  const int plane = (kDim / 2) << a.pool.log_page;
-  const int part = warp * kTeams + team;
-  float m = -INFINITY, l = 0.0f;
-  for (int j0 = 0; j0 < seen; j0 += kWarps * kTeams) {
-    const int j = j0 + part;
-    uint8_t* page = j < seen ? kv4_block(a.pool, a.table, a.max_pages, b, j, kvh) : nullptr;
-    const int slot = j & ((1 << a.pool.log_page) - 1);
-    uint32_t kc = 0, vc = 0;
-    float ks = 0.0f, vs = 0.0f;
-    if (page) {
-      kc = *reinterpret_cast<const uint32_t*>(page + slot * (kDim / 2) + tl * 4);
-      vc = *reinterpret_cast<const uint32_t*>(page + plane + slot * (kDim / 2) + tl * 4);
-      ks = reinterpret_cast<const float*>(page + 2 * plane)[slot];
-      vs = reinterpret_cast<const float*>(page + 2 * plane)[(1 << a.pool.log_page) + slot];
-    }
-    float s = 0.0f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) s = fmaf(q[c], static_cast<float>(static_cast<int>(kc << (28 - 4 * c)) >> 28), s);
-#pragma unroll
-    for (int x = 1; x < kTeam; x *= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
-    if (!page) continue;
-    s *= ks * a.scale * kLog2e;
-    const float top = fmaxf(m, s), keep = m == top ? 1.0f : exp2f(m - top), p = exp2f(s - top);
-    m = top;
-    l = l * keep + p;
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-      acc[c] = fmaf(p * vs, static_cast<float>(static_cast<int>(vc << (28 - 4 * c)) >> 28), acc[c] * keep);
-  }
-  if (tl == 0) {
-    s_m[part] = m;
-    s_l[part] = l;
-  }
-#pragma unroll
-  for (int c = 0; c < 8; ++c) s_acc[part][tl * 8 + c] = acc[c];
-  __syncthreads();
-  if (warp > 0) return;
-  float top = -INFINITY, sum = 0.0f, o[8] = {};
-  for (int w = 0; w < kWarps * kTeams; ++w) top = fmaxf(top, s_m[w]);
-  for (int w = 0; w < kWarps * kTeams; ++w) {
-    if (s_l[w] == 0.0f) continue;
-    const float f = exp2f(s_m[w] - top);
-    sum += s_l[w] * f;
-    for (int c = 0; c < 8; ++c) o[c] += s_acc[w][tl * 8 + c] * f;
-  }
-  for (int c = 0; c < 8; ++c) o[c] = sum == 0.0f ? 0.0f : o[c] / sum;
-  if (a.pool.rotate) rotate_head<kTeam>(o);
-  if (team == 0)
-    *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(t) * a.heads + h) * kDim + tl * 8) = pack8<T>(o);
+struct Kv4Params {
+  Kv4AttentionArgs a;
+  int group;         // query heads on a key/value head
+  int rows;          // query rows of a CTA (8 or 16): (token, head of the group), tokens outer
+  int row_tiles;     // for max_q queries
+  int chunk, chunks; // cached tokens of a CTA; CTAs for max_len
+  float* part;       // [unit][chunks][rows][head_dim + 2]: sums over the values, then max s, sum p
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-template <typename T>
-void launch(const Kv4AttentionArgs& a) {
-  const dim3 grid(a.total_q, a.heads);
-  if (a.pool.head_dim == 64) attention_kv4_kernel<T, 64><<<grid, 32 * kWarps, 0, a.stream>>>(a);
-  if (a.pool.head_dim == 128) attention_kv4_kernel<T, 128><<<grid, 32 * kWarps, 0, a.stream>>>(a);
-  if (a.pool.head_dim == 256) attention_kv4_kernel<T, 256><<<grid, 32 * kWarps, 0, a.stream>>>(a);
+// Of a word of 8 codes: the codes at nibbles 0 and 4, and at 1 and 5, as float16 pairs.
+__device__ __forceinline__ uint32_t codes_04(uint32_t w) {
+  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&(w = (w & 0x000f000fu) ^ 0x64086408u)), __half2half2(__float2half(-1032.0f)));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t codes_15(uint32_t w) {
+  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&(w = (w & 0x00f000f0u) ^ 0x54805480u)), __half2half2(__float2half(-72.0f)));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+template <int kWords>
+__device__ __forceinline__ void load_words(uint32_t (&r)[kWords], const uint8_t* p) {
+  if constexpr (kWords == 1) {
+    r[0] = __ldg(reinterpret_cast<const unsigned int*>(p));
+  } else if constexpr (kWords == 2) {
+    const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+    r[0] = v.x;
+    r[1] = v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + i * 4));
+      r[i] = v.x;
+      r[i + 1] = v.y;
+      r[i + 2] = v.z;
+      r[i + 3] = v.w;
+    }
+  }
+}
+
+// One sequence as the launch's bounds admit it; false where it is to be skipped.
+struct Sequence {
+  int q0, n, len;
+};
+__device__ __forceinline__ bool load_sequence(const Kv4AttentionArgs& a, int b, Sequence& s) {
+  s.q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q);
+  s.n = min(max(__ldg(a.cu_q + b + 1), s.q0), a.total_q) - s.q0;
+  s.len = __ldg(a.kv_len + b);
+  return s.n <= a.max_q && s.len >= 0 && s.len <= a.max_len;
+}
+// Cached tokens that query token i sees.
+__device__ __forceinline__ int seen_by(const Sequence& s, int causal, int i) { return causal ? max(0, s.len - s.n + i + 1) : s.len; }
+
+template <int kDim>
+struct Cfg {
+  static constexpr int kKeyWords = kDim / 32, kValueWords = kDim / 64;  // a lane's words of a key, of a value
+  static constexpr int kStages = kDim == 64 ? 4 : 2;                    // 16-token steps in flight
+  static constexpr int kTeam = kDim / 8;                                // lanes that hold a head, 8 channels each
+  static constexpr int kQStride = kDim + 8;                             // float16 of a staged query row
+};
+
+template <typename T, int kDim, int kTiles>
+__global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid_constant__ Kv4Params p) {
+  using C = Cfg<kDim>;
+  constexpr int kRows = 8 * kTiles, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam;
+  constexpr bool kQInRegs = kTiles * kDim <= 256;
+  const Kv4AttentionArgs& a = p.a;
+  extern __shared__ float s_o[];                                   // [kWarps][kRows][kDim] at the end
+  __half* const s_q = reinterpret_cast<__half*>(s_o);              // [kRows][kQStride] until then (where Q is in registers)
+  __shared__ float s_f[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
+  __shared__ __align__(16) __half s_q2[kQInRegs ? 8 : kRows * C::kQStride];
+  __half* const q_at = kQInRegs ? s_q : s_q2;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  int u = blockIdx.x;
+  const int ch = u % p.chunks;
+  const int unit = u /= p.chunks;
+  const int tile = u % p.row_tiles;
+  u /= p.row_tiles;
+  const int kvh = u % a.pool.kv_heads, b = u / a.pool.kv_heads;
+  griddep_wait();  // the queries, lengths and the cache may come from the previous kernel, which may still read o
+  griddep_launch_dependents();
+  Sequence seq;
+  if (!load_sequence(a, b, seq)) {
+    if (threadIdx.x == 0) report_index();
+    return;
+  }
+  const int row0 = tile * kRows, rows = min(kRows, seq.n * p.group - row0);
+  if (rows <= 0) return;
+  const int most = seen_by(seq, a.causal, (row0 + rows - 1) / p.group);  // tokens that the last row sees
+  const int k0 = ch * p.chunk, k1 = min(most, k0 + p.chunk);
+  if (ch > 0 && k0 >= most) return;
+
+  // ---- the first cached tokens are asked for before the queries are worked on
+  const size_t block = kv4_block_bytes(a.pool);
+  const int plane = (kDim / 2) << a.pool.log_page, slots = (1 << a.pool.log_page) - 1;
+  struct Stage {
+    uint32_t k[2][C::kKeyWords];    // tokens g and g + 8, this lane's quarter of the channels
+    uint32_t v[4][C::kValueWords];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, this lane's eighth
+    float scale;                    // lane i < 16: the key scale of token i; else the value scale of token i - 16
+    int end;                        // first token that nobody may use
+  } st[C::kStages];
+  const int steps = k1 > k0 + kStep * warp ? (k1 - k0 - kStep * warp + kStep * kWarps - 1) / (kStep * kWarps) : 0;
+  int pages = 0;  // of 32 steps, one a lane
+  auto load = [&](int i, Stage& s) {
+    if (i >= steps) return;
+    if ((i & 31) == 0) {
+      const int at = k0 + kStep * (warp + kWarps * (i + lane));
+      pages = at < k1 ? __ldg(a.table + static_cast<size_t>(b) * a.max_pages + (at >> a.pool.log_page)) : 0;
+    }
+    int page = __shfl_sync(0xffffffffu, pages, i & 31);
+    const int at = k0 + kStep * (warp + kWarps * i);
+    s.end = k1;
+    if (page < 0 || page >= a.pool.num_pages) {
+      if (lane == 0) report_index();
+      page = 0;
+      s.end = 0;
+    }
+    const uint8_t* src = a.pool.base + (static_cast<size_t>(page) * a.pool.kv_heads + kvh) * block;
+    const int slot = at & slots;
+    const uint8_t* ks = src + (slot + g) * (kDim / 2) + t * (kDim / 8);
+    const uint8_t* vs = src + plane + (slot + 2 * t) * (kDim / 2) + g * (kDim / 16);
+    load_words(s.k[0], ks);
+    load_words(s.k[1], ks + 8 * (kDim / 2));
+    load_words(s.v[0], vs);
+    load_words(s.v[1], vs + kDim / 2);
+    load_words(s.v[2], vs + 8 * (kDim / 2));
+    load_words(s.v[3], vs + 9 * (kDim / 2));
+    s.scale = __ldg(reinterpret_cast<const float*>(src + 2 * plane) + ((lane >> 4) << a.pool.log_page) + slot + (lane & 15));
+  };
+#pragma unroll
+  for (int i = 0; i < C::kStages; ++i) load(i, st[i]);
+
+  // ---- queries: rotated, scaled by a power of two, float16, in the order of the codes' pairs
+#pragma unroll
+  for (int r0 = 0; r0 < kRows; r0 += kTeams) {
+    const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
+    float y[8] = {};
+    if (r < rows) {
+      const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
+      unpack8<T>(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + token * a.q_stride + head * kDim + tl * 8)), y);
+    }
+    if (a.pool.rotate) rotate_head<kTeam>(y);
+    float top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(y[c]));
+#pragma unroll
+    for (int h = 1; h < kTeam; h *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
+    const int e = min(126, max(-126, static_cast<int>(__float_as_uint(top) >> 23) - 126));
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+    if (r < kRows) {
+      uint4 v;
+      v.x = __half_as_ushort(__float2half_rn(y[0] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[4] * down))) << 16;
+      v.y = __half_as_ushort(__float2half_rn(y[1] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[5] * down))) << 16;
+      v.z = __half_as_ushort(__float2half_rn(y[2] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[6] * down))) << 16;
+      v.w = __half_as_ushort(__float2half_rn(y[3] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[7] * down))) << 16;
+      *reinterpret_cast<uint4*>(q_at + r * C::kQStride + tl * 8) = v;
+      if (tl == 0) s_f[r] = a.scale * kLog2e * up;
+    }
+  }
+  __syncthreads();
+  uint32_t q[kQInRegs ? kTiles : 1][kQInRegs ? kDim / 8 : 1];
+  if constexpr (kQInRegs) {
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int w = 0; w < kDim / 32; ++w) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w);
+        q[n][4 * w] = v.x;
+        q[n][4 * w + 1] = v.y;
+        q[n][4 * w + 2] = v.z;
+        q[n][4 * w + 3] = v.w;
+      }
+    __syncthreads();  // (s_o takes the queries' place)
+  }
+  // this lane's rows of S^T and O^T: 8 n + 2 t and the next
+  float f[kTiles][2], m[kTiles][2], mv[kTiles][2], l[kTiles][2], o[kDim / 16][kTiles][4];
+  int seen[kTiles][2], least = most;
+#pragma unroll
+  for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 8 * n + 2 * t + e;
+      f[n][e] = s_f[r];
+      seen[n][e] = seen_by(seq, a.causal, min(row0 + r, row0 + rows - 1) / p.group);
+      m[n][e] = mv[n][e] = -FLT_MAX;
+      l[n][e] = 0.0f;
+    }
+  if (a.causal) least = seen_by(seq, 1, row0 / p.group);  // of the first row
+#pragma unroll
+  for (int i = 0; i < kDim / 16; ++i)
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.0f;
+
+  auto step = [&](int i, const Stage& s) {
+    const int at = k0 + kStep * (warp + kWarps * i);
+    float x[kTiles][4] = {};
+#pragma unroll
+    for (int w = 0; w < C::kKeyWords; ++w) {
+      uint32_t k0w = s.k[0][w], k1w = s.k[1][w];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t a0 = codes_04(k0w), a1 = codes_04(k1w), a2 = codes_15(k0w), a3 = codes_15(k1w);
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+          if constexpr (kQInRegs) {
+            mma16816(x[n], a0, a1, a2, a3, q[n][4 * w + 2 * h], q[n][4 * w + 2 * h + 1]);
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w + 4 * h);
+            mma16816(x[n], a0, a1, a2, a3, v.x, v.y);
+          }
+        }
+        k0w >>= 8;
+        k1w >>= 8;
+      }
+    }
+    const float own = lane < 16 ? s.scale : lg2(s.scale);
+    const float dk0 = __shfl_sync(0xffffffffu, own, g), dk1 = __shfl_sync(0xffffffffu, own, g + 8);
+    const float lv0 = __shfl_sync(0xffffffffu, own, g + 16), lv1 = __shfl_sync(0xffffffffu, own, g + 24);
+    float y[kTiles][4];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[n][e] *= (e < 2 ? dk0 : dk1) * f[n][e & 1];
+        y[n][e] = x[n][e] + (e < 2 ? lv0 : lv1);
+      }
+    if (at + kStep > min(least, s.end)) {  // some row does not see all of these tokens
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at + g + (e < 2 ? 0 : 8) >= min(seen[n][e & 1], s.end)) x[n][e] = y[n][e] = -INFINITY;
+    }
+    bool grown = false;
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) grown |= x[n][e] > m[n][e & 1] + kGrowth || y[n][e] > mv[n][e & 1] + kGrowth;
+    if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(m[n][e], fmaxf(x[n][e], x[n][e + 2])), topv = fmaxf(mv[n][e], fmaxf(y[n][e], y[n][e + 2]));
+#pragma unroll
+          for (int h = 4; h < 32; h *= 2) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
+            topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, h));
+          }
+          l[n][e] *= ex2(m[n][e] - top);
+          const float keep = ex2(mv[n][e] - topv);
+          m[n][e] = top;
+          mv[n][e] = topv;
+#pragma unroll
+          for (int c = 0; c < kDim / 16; ++c) {
+            o[c][n][e] *= keep;
+            o[c][n][e + 2] *= keep;
+          }
+        }
+    }
+    uint32_t b0[kTiles], b1[kTiles];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        l[n][e & 1] += ex2(x[n][e] - m[n][e & 1]);
+        y[n][e] = ex2(y[n][e] - mv[n][e & 1]);
+      }
+      const __half2 lo = __floats2half2_rn(y[n][0], y[n][1]), hi = __floats2half2_rn(y[n][2], y[n][3]);
+      b0[n] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
+      b1[n] = transpose8(*reinterpret_cast<const uint32_t*>(&hi));
+    }
+#pragma unroll
+    for (int w = 0; w < C::kValueWords; ++w)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // channels 4 h .. 4 h + 3 of the word, two tokens in each register
+        uint32_t v0 = __byte_perm(s.v[0][w], s.v[1][w], h ? 0x7632 : 0x5410), v1 = __byte_perm(s.v[2][w], s.v[3][w], h ? 0x7632 : 0x5410);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t a0 = codes_04(v0), a1 = codes_15(v0), a2 = codes_04(v1), a3 = codes_15(v1);
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) mma16816(o[4 * w + 2 * h + c][n], a0, a1, a2, a3, b0[n], b1[n]);
+          v0 >>= 8;
+          v1 >>= 8;
+        }
+      }
+  };
+  for (int i = 0; i < steps; i += C::kStages) {
+#pragma unroll
+    for (int e = 0; e < C::kStages; ++e) {
+      if (i + e < steps) {
+        step(i + e, st[e]);
+        load(i + e + C::kStages, st[e]);
+      }
+    }
+  }
+
+  // ---- join the warps; sums over the values are brought to the reference of the sum of p
+#pragma unroll
+  for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int h = 4; h < 32; h *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], h);
+      const int r = 8 * n + 2 * t + e;
+      if (g == 0) {
+        s_m[warp][r] = m[n][e];
+        s_l[warp][r] = l[n][e];
+      }
+      const float back = ex2(mv[n][e] - m[n][e]);
+      float* const dst = s_o + (warp * kRows + r) * kDim + g * (kDim / 8);
+#pragma unroll
+      for (int c = 0; c < kDim / 16; ++c) {
+        dst[2 * c] = o[c][n][e] * back;
+        dst[2 * c + 1] = o[c][n][e + 2] * back;
+      }
+    }
+  __syncthreads();
+  const bool whole = most <= p.chunk;
+#pragma unroll
+  for (int r0 = 0; r0 < kRows; r0 += kTeams) {
+    const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
+    const int rr = min(r, kRows - 1);
+    float top = s_m[0][rr], sum = 0.0f, y[8] = {};
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_m[w][rr]);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float k = ex2(s_m[w][rr] - top);
+      sum += s_l[w][rr] * k;
+      const float4* src = reinterpret_cast<const float4*>(s_o + (w * kRows + rr) * kDim + tl * 8);
+      const float4 lo = src[0], hi = src[1];
+      y[0] += lo.x * k;
+      y[1] += lo.y * k;
+      y[2] += lo.z * k;
+      y[3] += lo.w * k;
+      y[4] += hi.x * k;
+      y[5] += hi.y * k;
+      y[6] += hi.z * k;
+      y[7] += hi.w * k;
+    }
+    if (whole) {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) y[c] *= inv;
+      if (a.pool.rotate) rotate_head<kTeam>(y);
+      if (r < rows) {
+        const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+      }
+    } else if (r < rows) {
+      float* const dst = p.part + ((static_cast<size_t>(unit) * p.chunks + ch) * kRows + r) * (kDim + 2);
+#pragma unroll
+      for (int c = 0; c < 8; c += 2) *reinterpret_cast<float2*>(dst + tl * 8 + c) = make_float2(y[c], y[c + 1]);
+      if (tl == 0) *reinterpret_cast<float2*>(dst + kDim) = make_float2(top, sum);
+    }
+  }
+}
+
+// The chunks of every query row joined: a team of D / 8 lanes a row.
+template <typename T, int kDim>
+__global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const __grid_constant__ Kv4Params p) {
+  constexpr int kTeam = kDim / 8;
+  const Kv4AttentionArgs& a = p.a;
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t row_id = (static_cast<int64_t>(blockIdx.x) * (32 * kWarps) + threadIdx.x) / kTeam;
+  const int tl = threadIdx.x % kTeam;
+  // (a warp's rows may lie in two sequences: the search is made for each of them by the whole warp)
+  int token = static_cast<int>(min(row_id / a.heads, static_cast<int64_t>(a.total_q) - 1));
+  const int head = static_cast<int>(row_id % a.heads);
+  int b = -1, first = 0;
+  for (int s = 0; s < 32 / kTeam; ++s) {
+    int b1, f1;
+    const bool found = find_sequence(a.cu_q, a.batch, __shfl_sync(0xffffffffu, token, s * kTeam), b1, f1);
+    if (static_cast<int>(threadIdx.x & 31) / kTeam == s && found) {
+      b = b1;
+      first = f1;
+    }
+  }
+  Sequence seq = {0, 0, 0};
+  bool mine = b >= 0 && row_id < static_cast<int64_t>(a.total_q) * a.heads;
+  if (mine) mine = load_sequence(a, b, seq) && seq.q0 == first;
+  const int kvh = head / p.group, r = (token - seq.q0) * p.group + head % p.group;
+  const int tile = mine ? r / p.rows : 0;
+  const int most = mine ? seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group) : 0;
+  const int chunks = (most + p.chunk - 1) / p.chunk;
+  mine = mine && chunks > 1;  // (one chunk's result is written by its CTA)
+  const size_t unit = (static_cast<size_t>(max(b, 0)) * a.pool.kv_heads + kvh) * p.row_tiles + tile;
+  const float* const src = p.part + (unit * p.chunks * p.rows + r % p.rows) * (kDim + 2);
+  const size_t next = static_cast<size_t>(p.rows) * (kDim + 2);
+  float top = -FLT_MAX, sum = 0.0f, y[8] = {};
+  if (mine) {
+    for (int c = 0; c < chunks; ++c) top = fmaxf(top, src[c * next + kDim]);
+#pragma unroll 4
+    for (int c = 0; c < chunks; ++c) {
+      const float* at = src + c * next;
+      const float k = ex2(at[kDim] - top);
+      sum += at[kDim + 1] * k;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(at + tl * 8 + e);
+        y[e] += v.x * k;
+        y[e + 1] += v.y * k;
+      }
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) y[c] *= inv;
+  if (a.pool.rotate) rotate_head<kTeam>(y);
+  if (mine) *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+}
+
+int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * (a.heads / a.pool.kv_heads) <= 8 ? 8 : 16; }
+
+// The split over the keys: CTAs enough to fill the device several times over (sequences may be much shorter than max_len), of
+// at least 64 tokens, as far as the workspace has room for their results.
+constexpr int kLeastChunk = kStep * kWarps;
+constexpr int kCtasPerSm = 16;
+void plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p) {
+  p->group = a.heads / a.pool.kv_heads;
+  p->rows = rows_of(a);
+  p->row_tiles = static_cast<int>((static_cast<int64_t>(a.max_q) * p->group + p->rows - 1) / p->rows);
+  const int64_t units = static_cast<int64_t>(a.batch) * a.pool.kv_heads * p->row_tiles;
+  const int64_t target = static_cast<int64_t>(a.num_sms) * kCtasPerSm;
+  const int64_t part = static_cast<int64_t>(p->rows) * (a.pool.head_dim + 2) * 4;
+  const int64_t room = static_cast<int64_t>(ws_bytes) / (units * part);
+  const int64_t most = (static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk;
+  int64_t chunks = target / units;
+  if (chunks > room) chunks = room;
+  if (chunks > most) chunks = most;
+  if (chunks < 1) chunks = 1;
+  int64_t len = (a.max_len + chunks - 1) / chunks;
+  len = (len + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
+  if (len < kLeastChunk) len = kLeastChunk;
+  p->chunk = static_cast<int>(len > 0x7fffffff - kLeastChunk ? 0x7fffffff - kLeastChunk : len);
+  p->chunks = static_cast<int>((a.max_len + len - 1) / len);
+  if (p->chunks < 1) p->chunks = 1;
+}
+
+template <typename T, int kDim, int kTiles>
+cudaError_t launch(const Kv4AttentionArgs& a) {
+  Kv4Params p;
+  p.a = a;
+  plan_split(a, a.ws ? a.ws_bytes : 0, &p);
+  p.part = static_cast<float*>(a.ws);
+  const int64_t ctas = static_cast<int64_t>(a.batch) * a.pool.kv_heads * p.row_tiles * p.chunks;
+  const int64_t joins = (static_cast<int64_t>(a.total_q) * a.heads * (kDim / 8) + 32 * kWarps - 1) / (32 * kWarps);
+  if (ctas > 0x7fffffff || joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  constexpr int kSmem = kWarps * 8 * kTiles * kDim * 4;
+  auto kern = attention_kv4_kernel<T, kDim, kTiles>;
+  if (kSmem > 48 * 1024) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.blockDim = dim3(32 * kWarps);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = a.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
+  if (e != cudaSuccess) return e;
+  if (p.chunks > 1) {
+    cfg.gridDim = dim3(static_cast<unsigned>(joins));
+    cfg.dynamicSmemBytes = 0;
+    e = cudaLaunchKernelEx(&cfg, attention_kv4_join_kernel<T, kDim>, p);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaGetLastError();
+}
+
+template <typename T, int kDim>
+cudaError_t launch(const Kv4AttentionArgs& a) {
+  return rows_of(a) == 8 ? launch<T, kDim, 1>(a) : launch<T, kDim, 2>(a);
 }
 
 }  // namespace
 
-size_t attention_kv4_workspace(const Kv4AttentionArgs&) { return 0; }
+size_t attention_kv4_workspace(const Kv4AttentionArgs& a) {
+  Kv4Params p;
+  plan_split(a, ~static_cast<size_t>(0) >> 1, &p);
+  if (p.chunks < 2) return 0;
+  const size_t n = static_cast<size_t>(a.batch) * a.pool.kv_heads * p.row_tiles * p.chunks * p.rows * (a.pool.head_dim + 2) * 4;
+  return (n + 255) & ~static_cast<size_t>(255);
+}
 
 cudaError_t launch_attention_kv4(const Kv4AttentionArgs& a) {
-  if (a.dt == 0) launch<__half>(a);
-  else launch<__nv_bfloat16>(a);
-  return cudaGetLastError();
+  if (a.dt == 0)
+    return a.pool.head_dim == 64 ? launch<__half, 64>(a) : a.pool.head_dim == 128 ? launch<__half, 128>(a) : launch<__half, 256>(a);
+  return a.pool.head_dim == 64 ? launch<__nv_bfloat16, 64>(a)
+                               : a.pool.head_dim == 128 ? launch<__nv_bfloat16, 128>(a) : launch<__nv_bfloat16, 256>(a);
 }
 
 cudaError_t read_and_clear_error_word_attention_kv4(unsigned int* out, cudaStream_t stream) {

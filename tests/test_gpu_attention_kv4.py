@@ -16,7 +16,7 @@ def check(p, q, lens_q, lens_k, causal, scale=None, **kw):
     got = H.f64(H.kv4(p, q.to(H.DEV), lens_q, lens_k, causal, scale, **kw))
     Q.qvla_check_device(H.stream())
     ref, mag, top, terms = H.kv4_reference(p, q, lens_q, lens_k, causal, scale)
-    # probabilities in bfloat16, queries in float16; a rotated output is a float32 sum of dim terms more
+    # probabilities rounded to 16 bits (bfloat16's at worst), queries to float16; a rotated output is a float32 sum of dim terms more
     tol = H.bound(ref, mag, top, terms, p.dim, dt, H.UNIT["bf16"] + (p.dim * 2.0 ** -23 if p.rotate else 0.0), H.UNIT["f16"], 0.0)
     assert not np.isnan(got).any()
     worst = np.max(np.abs(got - ref) - tol) if got.size else 0.0
