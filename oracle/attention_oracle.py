@@ -68,6 +68,24 @@ def cached_heads(pool, page, dim, table_row, n, first=0):
     return k, v
 
 
+def read_back(codes, scales, rotate):
+    """Heads as the cache gives them back, float32: the integers codes . H (exact) times float32(scale / sqrt(D)) -- one
+    float32 product with the factor float32(1 / sqrt(D)), one with the integer; without rotation, code times scale."""
+    if not rotate:
+        return codes.astype(np.float32) * scales[..., None]
+    dim = codes.shape[-1]
+    sums = np.rint(codes.astype(np.float64) @ (hadamard(dim) * np.sqrt(dim)))
+    return sums.astype(np.float32) * (scales * np.float32(1.0 / np.sqrt(dim)))[..., None]
+
+
+def cached_read_back(pool, page, dim, table_row, n, first, rotate):
+    """read_back of the n tokens from position `first` of one sequence: keys and values [n, kv_heads, dim]."""
+    kc, vc, ks, vs = pool_parts(pool, page, dim)
+    pos = np.arange(first, first + n)
+    at, slot = np.asarray(table_row)[pos // page], pos % page
+    return tuple(read_back(unpack_nibbles(c[at, :, slot]), s[at, :, slot], rotate) for c, s in ((kc, ks), (vc, vs)))
+
+
 def attention(q, k, v, scale, causal):
     """One sequence, float64: q [n, heads, D], k and v [m, kv_heads, D].  Returns o and, for error bounds, the largest |score|
     and the largest sum of |terms| of a score, per query and head, and sum_j p_j |v_j|."""

@@ -113,8 +113,9 @@ qvla_status qvla_kv4_append(const qvla_kv4_cache* cache, const void* k, const vo
   if (qvla_status s = check_tokens("v", v, total_new, v_stride, width)) return s;
   if (qvla_status s = check_batch(batch, cu_new, page_table, max_pages)) return s;
   if (batch == 0 || total_new == 0) return QVLA_OK;
-  const qvla::Kv4RowsArgs a = {pool, const_cast<void*>(k), const_cast<void*>(v), k_stride, v_stride, static_cast<int>(dt), batch,
-                               cu_new, total_new, page_table, max_pages, start, static_cast<cudaStream_t>(stream)};
+  qvla::Kv4RowsArgs a = {pool, const_cast<void*>(k), const_cast<void*>(v), k_stride, v_stride, static_cast<int>(dt), batch,
+                         cu_new, total_new, page_table, max_pages, start, 0, static_cast<cudaStream_t>(stream)};
+  if (qvla_status s = current_sms(&a.num_sms)) return s;
   QVLA_CUDA(qvla::launch_kv4_append(a), "kv4_append launch");
   return QVLA_OK;
 }
@@ -130,8 +131,9 @@ qvla_status qvla_kv4_gather(const qvla_kv4_cache* cache, int batch, const int32_
   if (qvla_status s = check_tokens("v", v, total, width, width)) return s;
   if (qvla_status s = check_batch(batch, cu, page_table, max_pages)) return s;
   if (batch == 0 || total == 0) return QVLA_OK;
-  const qvla::Kv4RowsArgs a = {pool, k, v, width, width, static_cast<int>(dt), batch, cu, total, page_table, max_pages, start,
-                               static_cast<cudaStream_t>(stream)};
+  qvla::Kv4RowsArgs a = {pool, k, v, width, width, static_cast<int>(dt), batch, cu, total, page_table, max_pages, start, 0,
+                         static_cast<cudaStream_t>(stream)};
+  if (qvla_status s = current_sms(&a.num_sms)) return s;
   QVLA_CUDA(qvla::launch_kv4_gather(a), "kv4_gather launch");
   return QVLA_OK;
 }

@@ -53,16 +53,6 @@ __device__ __forceinline__ float lg2(float x) {
   return y;
 }
 
-// Of a word of 8 codes: the codes at nibbles 0 and 4, and at 1 and 5, as float16 pairs.
-__device__ __forceinline__ uint32_t codes_04(uint32_t w) {
-  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&(w = (w & 0x000f000fu) ^ 0x64086408u)), __half2half2(__float2half(-1032.0f)));
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t codes_15(uint32_t w) {
-  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&(w = (w & 0x00f000f0u) ^ 0x54805480u)), __half2half2(__float2half(-72.0f)));
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])

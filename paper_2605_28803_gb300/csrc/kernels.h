@@ -182,6 +182,7 @@ struct Kv4RowsArgs {
   const int32_t* table;    // device [batch][max_pages]
   int max_pages;
   const int32_t* start;    // device [batch] or null (0)
+  int num_sms;
   cudaStream_t stream;
 };
 cudaError_t launch_kv4_append(const Kv4RowsArgs& a);

@@ -79,6 +79,19 @@ __device__ __forceinline__ void rotate_head(float (&y)[8]) {
   for (int i = 0; i < 8; ++i) y[i] *= f;
 }
 
+// Of a word of 8 codes: the codes at nibbles 0 and 4, and at 1 and 5, as float16 pairs.  The bits 0x6408 ^ code read 1032 + code
+// and 0x5480 ^ (code << 4) read 72 + code, from which one exact addition takes the offset.
+__device__ __forceinline__ uint32_t codes_04(uint32_t w) {
+  w = (w & 0x000f000fu) ^ 0x64086408u;
+  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0xe408)));  // -1032
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t codes_15(uint32_t w) {
+  w = (w & 0x00f000f0u) ^ 0x54805480u;
+  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0xd480)));  // -72
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 template <typename T>
 struct Pair;
 template <>

@@ -1,21 +1,138 @@
 // The 4-bit key/value cache: tokens in (rotate, quantise, store to their pages) and tokens out.
 //
 // Per token and key/value head: y = x . H / sqrt(D) (or x), Delta = max |y| / 7, codes clamp(round(y / Delta), -7, 7), round half
-// to even on the exact quotient; out again, x^ = (Delta q) . H / sqrt(D), rounded to the output's type.
+// to even on the exact quotient; out again, x^ = (Delta / sqrt(D)) (q . H), rounded to the output's type.  q . H is a vector of
+// integers of at most 7 D = 1792: exact in float16, so on the way out the rotation is float16 arithmetic, two channels an
+// instruction and a shuffle, without a rounding.
 //
-// Both are bound by HBM (read 2 D bytes, write D / 2 + 4, and the other way round); the rest hides behind it.  A head is
-// a team of D / 8 lanes with 8 channels (16 bytes in, 4 bytes of codes) each, so that loads and stores of a team are contiguous
-// and the rotation stays in registers and shuffles.  A warp takes kRows heads of one token per team, all loaded before
-// the first is used: the sequence search and the page lookup are made once for them.
+// Both move 2 D bytes of values one way and D / 2 + 4 of codes the other way per head, and HBM would be the bound; the rotation's
+// log2 D sums a channel and its exchanges between lanes come close to it.  So a head is a team of only D / 32 lanes with four
+// groups of 8 channels each, group k of lane l at channel 8 (k team + l): of the butterflies' distances 1, 2, 4 and the two
+// largest stay in registers, two channels an instruction, and 1 to 3 are shuffles; a team's 16-byte accesses are contiguous.
+// A warp takes `passes` sets of 32 / team heads in a row and loads the next set's data ahead of the present one's
+// arithmetic; the search for the first token's sequence is made once.
 #include <cuda_runtime.h>
 
+#include "griddep.cuh"
 #include "kv4.cuh"
 
 namespace qvla {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kRows = 4;  // heads a team holds at once
+constexpr int kPasses = 8;        // of a warp, at most
+constexpr int kWarpsPerSm = 32;   // below this many warps an SM, a warp takes fewer passes
+
+template <int kTeam>
+constexpr float kNorm = kTeam == 2 ? 0.125f : kTeam == 4 ? 0.08838834764831845f : 0.0625f;  // float32(1 / sqrt(32 kTeam))
+
+// Two float32 operations an instruction, each rounded like the single one.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)), "l"(reinterpret_cast<const uint64_t&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
+  return r;
+}
+
+// q . H for codes (or sums of them) spread over kTeam lanes as above: v[k] holds channels 0 and 4, 1 and 5, 2 and 6, 3 and 7 of
+// group k's eight.  Every sum is exact.
+template <int kTeam>
+__device__ __forceinline__ void rotate_codes(__half2 (&v)[4][4]) {
+  const int lane = threadIdx.x & 31;
+  const __half2 split = __halves2half2(__ushort_as_half(0x3c00), __ushort_as_half(0xbc00));  // 1, -1
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+#pragma unroll
+    for (int h = 1; h < 4; h *= 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((i & h) == 0) {
+          const __half2 a = v[k][i], b = v[k][i + h];
+          v[k][i] = __hadd2(a, b);
+          v[k][i + h] = __hsub2(a, b);
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[k][i] = __hfma2(v[k][i], split, __lowhigh2highlow(v[k][i]));
+  }
+#pragma unroll
+  for (int h = 1; h < kTeam; h *= 2) {
+    const __half2 sign = __half2half2(__ushort_as_half((lane & h) != 0 ? 0xbc00 : 0x3c00));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[k][i] = __hfma2(v[k][i], sign, __shfl_xor_sync(0xffffffffu, v[k][i], h));
+  }
+#pragma unroll
+  for (int h = 1; h < 4; h *= 2)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((k & h) == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __half2 a = v[k][i], b = v[k + h][i];
+          v[k][i] = __hadd2(a, b);
+          v[k + h][i] = __hsub2(a, b);
+        }
+}
+
+// x . H / sqrt(32 kTeam) for a head spread over kTeam lanes as above; the sums of rotate_head in its order, so the same bits.
+template <int kTeam>
+__device__ __forceinline__ void rotate_groups(float2 (&y)[4][4]) {
+  const float2 minus = make_float2(-1.0f, -1.0f);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[k][i] = make_float2(y[k][i].x + y[k][i].y, y[k][i].x - y[k][i].y);
+#pragma unroll
+    for (int h = 1; h < 4; h *= 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((i & h) == 0) {
+          const float2 a = y[k][i], b = y[k][i + h];
+          y[k][i] = add2(a, b);
+          y[k][i + h] = fma2(b, minus, a);
+        }
+  }
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 1; h < kTeam; h *= 2) {
+    const float sign = (lane & h) != 0 ? -1.0f : 1.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, y[k][i].x, h), __shfl_xor_sync(0xffffffffu, y[k][i].y, h));
+        y[k][i] = fma2(y[k][i], make_float2(sign, sign), o);  // a + b, or a - b in the upper lane
+      }
+  }
+  constexpr float f = kNorm<kTeam>;
+#pragma unroll
+  for (int h = 1; h < 4; h *= 2)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((k & h) == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 a = y[k][i], b = y[k + h][i];
+          y[k][i] = add2(a, b);
+          y[k + h][i] = fma2(b, minus, a);
+        }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[k][i] = mul2(y[k][i], make_float2(f, f));
+}
 
 // The code of y at scale d, r = 1 / d: round half to even on the exact quotient y / d.  y r is within 2 ulp of it, so away
 // from a half-integer both round alike; near one the rounded quotient t and the sign of the remainder y - t d decide.
@@ -35,100 +152,180 @@ __device__ __forceinline__ int code_of(float y, float d, float r) {
 }
 
 template <typename T, int kTeam, bool kAppend>
-__global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const Kv4RowsArgs a) {
-  constexpr int kDim = 8 * kTeam, kTeams = 32 / kTeam;
+__global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constant__ Kv4RowsArgs a, int passes) {
+  constexpr int kDim = 32 * kTeam, kHeads = 32 / kTeam;  // heads of a warp's pass
   const int lane = threadIdx.x & 31, team = lane / kTeam, tl = lane % kTeam;
   const int rows = 2 * a.pool.kv_heads;  // a token's heads: keys, then values
-  const int chunks = (rows + kTeams * kRows - 1) / (kTeams * kRows);
-  const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5;  // the same in a whole warp
-  if (item >= static_cast<int64_t>(a.total) * chunks) return;
-  const int t = static_cast<int>(item / chunks), row0 = static_cast<int>(item % chunks) * kTeams * kRows;
-  int b, first;
-  if (!find_sequence(a.cu, a.batch, t, b, first)) return;
-  const int64_t pos = static_cast<int64_t>(a.start ? __ldg(a.start + b) : 0) + (t - first);
-  uint8_t* const page = kv4_block(a.pool, a.table, a.max_pages, b, pos, 0);
-  const int slot = static_cast<int>(pos) & ((1 << a.pool.log_page) - 1);
-  if (kAppend && page == nullptr) return;
+  const int64_t all = static_cast<int64_t>(a.total) * rows;
+  const int64_t id0 = ((static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5) * passes * kHeads;
+  griddep_wait();  // tokens, cache, tables and offsets may come from the previous kernel, which may still read the outputs
+  griddep_launch_dependents();
+  if (id0 >= all) return;
+  int t0 = static_cast<int>(id0 / rows), row0 = static_cast<int>(id0 % rows);  // the pass's first head
+  int b, first, next;
+  find_sequence(a.cu, a.batch, t0, b, first);
+  next = __ldg(a.cu + b + 1);
   const size_t block = kv4_block_bytes(a.pool);
   const int plane = (kDim / 2) << a.pool.log_page;  // bytes of a block's key codes
 
-  uint4 x[kRows];
-  float scale[kRows];
+  struct Head {
+    uint8_t* at;    // its block in the cache, at the token's codes and scale; null: none
+    float* scale;
+    T* out;         // gather's output, append's input; null: nothing to do
+    uint4 x[4];     // append: the token's values; gather: the codes of group k in x[0].xyzw
+    float d;
+  };
+  auto load = [&](Head& h) {
+    h.out = nullptr;
+    h.at = nullptr;
+    h.d = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    const int row = row0 + i * kTeams + team;
-    x[i] = make_uint4(0, 0, 0, 0);
-    scale[i] = 0.0f;
-    if (row >= rows) continue;
-    const int value = row >= a.pool.kv_heads, head = row - value * a.pool.kv_heads;
-    if constexpr (kAppend) {
-      const T* src = static_cast<const T*>(value ? a.v : a.k) + t * (value ? a.v_stride : a.k_stride) + head * kDim + tl * 8;
-      x[i] = __ldg(reinterpret_cast<const uint4*>(src));
-    } else if (page != nullptr) {
-      const uint8_t* src = page + head * block;
-      x[i].x = __ldg(reinterpret_cast<const unsigned int*>(src + value * plane + slot * (kDim / 2) + tl * 4));
-      scale[i] = __ldg(reinterpret_cast<const float*>(src + 2 * plane) + (value << a.pool.log_page) + slot);
+    for (int k = 0; k < 4; ++k) h.x[k] = make_uint4(0, 0, 0, 0);
+    const int over = (row0 + team) / rows, t = t0 + over, row = row0 + team - over * rows;
+    row0 += kHeads;
+    t0 += row0 / rows;
+    row0 %= rows;
+    if (t >= a.total) return;
+    while (t >= next && b + 1 < a.batch) {  // (tokens come in order)
+      first = next;
+      ++b;
+      next = __ldg(a.cu + b + 1);
     }
-  }
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) {
-    if (row0 + i * kTeams >= rows) break;
-    const int row = row0 + i * kTeams + team;
-    const bool live = row < rows;  // (every lane takes the shuffles)
+    if (t < first || t >= next) return;
     const int value = row >= a.pool.kv_heads, head = row - value * a.pool.kv_heads;
-    float y[8];
+    h.out = static_cast<T*>(value ? a.v : a.k) + t * (value ? a.v_stride : a.k_stride) + head * kDim + tl * 8;
+    const int64_t pos = static_cast<int64_t>(a.start ? __ldg(a.start + b) : 0) + (t - first);
+    uint8_t* const at = kv4_block(a.pool, a.table, a.max_pages, b, pos, head);
+    if (at != nullptr) {
+      const int slot = static_cast<int>(pos) & ((1 << a.pool.log_page) - 1);
+      h.at = at + value * plane + slot * (kDim / 2) + tl * 4;
+      h.scale = reinterpret_cast<float*>(at + 2 * plane) + (value << a.pool.log_page) + slot;
+    }
     if constexpr (kAppend) {
-      unpack8<T>(x[i], y);
-      if (a.pool.rotate) rotate_head<kTeam>(y);
-      float m = 0.0f;
-      bool nan = false;
+      if (at == nullptr) return;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        m = fmaxf(m, fabsf(y[c]));
-        nan |= y[c] != y[c];
-      }
-      if (nan) m = __int_as_float(0x7fffffff);
+      for (int k = 0; k < 4; ++k) h.x[k] = __ldg(reinterpret_cast<const uint4*>(h.out + k * 8 * kTeam));
+    } else if (at != nullptr) {
+      h.x[0].x = __ldg(reinterpret_cast<const unsigned int*>(h.at));
+      h.x[0].y = __ldg(reinterpret_cast<const unsigned int*>(h.at + 4 * kTeam));
+      h.x[0].z = __ldg(reinterpret_cast<const unsigned int*>(h.at + 8 * kTeam));
+      h.x[0].w = __ldg(reinterpret_cast<const unsigned int*>(h.at + 12 * kTeam));
+      h.d = __ldg(h.scale);
+    }
+  };
+  auto finish = [&](const Head& h) {
+    float2 y[4][4];
+    if constexpr (kAppend) {
 #pragma unroll
-      for (int h = 1; h < kTeam; h *= 2) {  // the maximum of the bits: a NaN stands above every number
-        m = __uint_as_float(max(__float_as_uint(m), __shfl_xor_sync(0xffffffffu, __float_as_uint(m), h)));
-      }
-      const float d = __fdiv_rn(m, 7.0f);
-      uint32_t w = 0;
-      if (d > 0.0f && d < __int_as_float(0x7f800000)) {  // not zero, infinite or NaN
-        const bool tiny = d < 1e-28f;  // the remainder of a quotient could leave the numbers: decide on scaled values
-        const float ds = tiny ? d * 0x1p64f : d, r = __frcp_rn(ds);
+      for (int k = 0; k < 4; ++k) {
+        const typename Pair<T>::V* v = reinterpret_cast<const typename Pair<T>::V*>(&h.x[k]);
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-          w |= (static_cast<uint32_t>(code_of(tiny ? y[c] * 0x1p64f : y[c], ds, r)) & 15u) << (4 * c);
+        for (int i = 0; i < 4; ++i) y[k][i] = Pair<T>::to_float(v[i]);
       }
-      if (live) {
-        uint8_t* dst = page + head * block;
-        *reinterpret_cast<uint32_t*>(dst + value * plane + slot * (kDim / 2) + tl * 4) = w;
-        // an infinity reads back as NaN, like a NaN
-        if (tl == 0)
-          reinterpret_cast<float*>(dst + 2 * plane)[(value << a.pool.log_page) + slot] =
-              d < __int_as_float(0x7f800000) ? d : __int_as_float(0x7fffffff);
+      if (a.pool.rotate) rotate_groups<kTeam>(y);
+      uint32_t m = 0;  // the largest magnitude by its bits: a NaN stands above every number
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          m = max(m, max(__float_as_uint(y[k][i].x) & 0x7fffffffu, __float_as_uint(y[k][i].y) & 0x7fffffffu));
+#pragma unroll
+      for (int s = 1; s < kTeam; s *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
+      if (h.at == nullptr) return;
+      const float d = m < 0x7f800000u ? __fdiv_rn(__uint_as_float(m), 7.0f) : __uint_as_float(0x7fffffffu);
+      // y / d <= 7 by the choice of d, so codes need no clamp.  1.5 2^23 + y r rounds to half even in the last place, whose
+      // byte is the code; where that lies within 1e-5 of a tie (or r is no number to use) the exact decision is taken.
+      const float r = __frcp_rn(d);
+      const float2 r2 = make_float2(r, r), big = make_float2(12582912.0f, 12582912.0f), neg = make_float2(-12582912.0f, -12582912.0f);
+      float far = 0.0f;  // from the code, at most
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t e[4], o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 n = fma2(y[k][i], r2, big), c = add2(n, neg), rest = fma2(y[k][i], r2, make_float2(-c.x, -c.y));
+          far = fmaxf(far, fmaxf(fabsf(rest.x), fabsf(rest.y)));
+          e[i] = __float_as_uint(n.x);
+          o[i] = __float_as_uint(n.y);
+        }
+        const uint32_t even = __byte_perm(__byte_perm(e[0], e[1], 0x0040), __byte_perm(e[2], e[3], 0x0040), 0x5410);
+        const uint32_t odd = __byte_perm(__byte_perm(o[0], o[1], 0x0040), __byte_perm(o[2], o[3], 0x0040), 0x5410);
+        w[k] = (even & 0x0f0f0f0fu) | ((odd << 4) & 0xf0f0f0f0u);
       }
+      const bool tiny = d < 1e-28f;  // the remainder of a quotient could leave the numbers: decide on scaled values
+      if (!(far < 0.49999f) || tiny || !(d > 0.0f)) {
+        const float up = tiny ? 0x1p64f : 1.0f, ds = d * up, rs = __frcp_rn(ds);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          w[k] = 0;
+          if (d > 0.0f) {  // (not zero, not NaN)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              w[k] |= (static_cast<uint32_t>(code_of(y[k][i].x * up, ds, rs)) & 15u) << (8 * i);
+              w[k] |= (static_cast<uint32_t>(code_of(y[k][i].y * up, ds, rs)) & 15u) << (8 * i + 4);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *reinterpret_cast<uint32_t*>(h.at + k * 4 * kTeam) = w[k];
+      if (tl == 0) *h.scale = d;
     } else {
+      __half2 v[4][4];
 #pragma unroll
-      for (int c = 0; c < 8; ++c)  // (a product of its own: fused into the rotation's first sums it would not be rounded)
-        y[c] = __fmul_rn(static_cast<float>(static_cast<int>(x[i].x << (28 - 4 * c)) >> 28), scale[i]);
-      if (a.pool.rotate) rotate_head<kTeam>(y);
-      if (live) {
-        T* dst = static_cast<T*>(value ? a.v : a.k) + t * (value ? a.v_stride : a.k_stride) + head * kDim + tl * 8;
-        *reinterpret_cast<uint4*>(dst) = pack8<T>(y);
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t w = k == 0 ? h.x[0].x : k == 1 ? h.x[0].y : k == 2 ? h.x[0].z : h.x[0].w;
+        *reinterpret_cast<uint32_t*>(&v[k][0]) = codes_04(w);
+        *reinterpret_cast<uint32_t*>(&v[k][1]) = codes_15(w);
+        *reinterpret_cast<uint32_t*>(&v[k][2]) = codes_04(w >> 8);
+        *reinterpret_cast<uint32_t*>(&v[k][3]) = codes_15(w >> 8);
+      }
+      if (a.pool.rotate) rotate_codes<kTeam>(v);
+      if (h.out == nullptr) return;
+      const float f = a.pool.rotate ? h.d * kNorm<kTeam> : h.d;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 c = mul2(__half22float2(v[k][i]), make_float2(f, f));
+          y[i] = c.x;
+          y[i + 4] = c.y;
+        }
+        *reinterpret_cast<uint4*>(h.out + k * 8 * kTeam) = pack8<T>(y);
       }
     }
+  };
+  Head now, ahead;
+  load(now);
+  for (int i = 0; i < passes; ++i) {
+    if (id0 + static_cast<int64_t>(i) * kHeads >= all) break;  // (the whole warp)
+    if (i + 1 < passes) load(ahead);
+    finish(now);
+    now = ahead;
   }
 }
 
 template <typename T, int kTeam, bool kAppend>
 cudaError_t launch_rows(const Kv4RowsArgs& a) {
-  const int rows = 2 * a.pool.kv_heads, per = 32 / kTeam * kRows;
-  const int64_t items = static_cast<int64_t>(a.total) * ((rows + per - 1) / per);
-  const int64_t blocks = (items * 32 + kThreads - 1) / kThreads;
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  kv4_rows_kernel<T, kTeam, kAppend><<<static_cast<unsigned int>(blocks), kThreads, 0, a.stream>>>(a);
+  const int64_t sets = (static_cast<int64_t>(a.total) * 2 * a.pool.kv_heads + 32 / kTeam - 1) / (32 / kTeam);
+  const int64_t fill = static_cast<int64_t>(a.num_sms) * kWarpsPerSm;
+  const int passes = static_cast<int>(sets >= fill * kPasses ? kPasses : sets <= fill ? 1 : (sets + fill - 1) / fill);
+  const int64_t warps = (sets + passes - 1) / passes;
+  const int64_t blocks = (warps * 32 + kThreads - 1) / kThreads;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = a.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kv4_rows_kernel<T, kTeam, kAppend>, a, passes);
+  if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
 
@@ -136,10 +333,10 @@ template <bool kAppend>
 cudaError_t launch_rows(const Kv4RowsArgs& a) {
   const int d = a.pool.head_dim;
   if (a.dt == 0) {
-    return d == 64 ? launch_rows<__half, 8, kAppend>(a) : d == 128 ? launch_rows<__half, 16, kAppend>(a) : launch_rows<__half, 32, kAppend>(a);
+    return d == 64 ? launch_rows<__half, 2, kAppend>(a) : d == 128 ? launch_rows<__half, 4, kAppend>(a) : launch_rows<__half, 8, kAppend>(a);
   }
-  return d == 64 ? launch_rows<__nv_bfloat16, 8, kAppend>(a)
-                 : d == 128 ? launch_rows<__nv_bfloat16, 16, kAppend>(a) : launch_rows<__nv_bfloat16, 32, kAppend>(a);
+  return d == 64 ? launch_rows<__nv_bfloat16, 2, kAppend>(a)
+                 : d == 128 ? launch_rows<__nv_bfloat16, 4, kAppend>(a) : launch_rows<__nv_bfloat16, 8, kAppend>(a);
 }
 
 }  // namespace

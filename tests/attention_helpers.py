@@ -110,6 +110,12 @@ class Paged:
                  for b, n in enumerate(lens)]
         return tuple(np.concatenate([p[i] for p in parts]) for i in range(2))
 
+    def read_back(self, lens, first):
+        """What the cache gives back, packed, float32 in the model's basis."""
+        parts = [A.cached_read_back(self.pool, self.page, self.dim, self.table[b], n, first[b], self.rotate)
+                 for b, n in enumerate(lens)]
+        return tuple(np.concatenate([p[i] for p in parts]) for i in range(2))
+
 
 def kv4(p, q, lens_q, lens_k, causal, scale=None, ws_bytes=None, max_q=None, max_len=None, cu_q=None, kv_len=None):
     """qvla_attention_kv4; ws_bytes None: the library's own size."""

@@ -138,6 +138,15 @@ def test_codes_worked_by_hand():
     assert A.pack_nibbles(np.array([[1, -1]], np.int8)).tolist() == [[0xF1]]
 
 
+def test_read_back_is_the_rotation_of_code_times_scale():
+    rng = np.random.default_rng(2)
+    codes = rng.integers(-7, 8, (3, 2, 128)).astype(np.int8)
+    scales = rng.uniform(0.1, 1.0, (3, 2)).astype(np.float32)
+    want = (codes * scales[..., None].astype(np.float64)) @ A.hadamard(128)
+    assert np.allclose(A.read_back(codes, scales, True), want, atol=1e-6)
+    assert np.array_equal(A.read_back(codes, scales, False), codes.astype(np.float32) * scales[..., None])
+
+
 def test_attention_worked_by_hand():
     q = np.zeros((2, 1, 2))
     k = np.ones((3, 1, 2))
