@@ -8,8 +8,10 @@
 // contiguous bytes and of a value D / 16, and no byte crosses shared memory.
 //   S^T = K Q^T      A = key codes (16 keys x 16 channels), B = queries (8 rows): grouped heads' single tokens fill 8 columns
 //   O^T += V^T P^T   A = value codes (16 channels x 16 keys), B = P^T, from S^T's accumulators by an 8 x 8 transpose
-// A code becomes float16 by one logic operation and one exact addition on two at a time (the bits 0x6408 ^ code read 1032 +
-// code, 0x5480 ^ (code << 4) read 72 + code).
+// A value's code becomes float16 by one logic operation and one exact addition on two at a time.  A key's takes the logic
+// operation alone: code + 8 in the low bits of a float16 is the subnormal (code + 8) 2^-24 (2^-20 from the nibble above, whose
+// queries carry a factor 1/16), and 8 sum_c q'_c is taken from the row's scores.  (For values that offset would grow with
+// the number of tokens and cost the sum its last bits.)
 //   Dk_j multiplies the score.  Dv_j joins the exponent: the weight that is rounded to float16 for the second product is
 // w_j = exp2(s_j + log2 Dv_j - r) against a running reference r of its own, so it has float16's 11 bits whatever the scales'
 // size, while sum_j p_j is kept in float32 against max s.  References move when a weight would pass 2^8.
@@ -52,6 +54,10 @@ __device__ __forceinline__ float lg2(float x) {
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// Of a word of 8 codes: (code + 8) 2^-24 at nibbles 0 and 4, (code + 8) 2^-20 at 1 and 5.
+__device__ __forceinline__ uint32_t offsets_04(uint32_t w) { return (w & 0x000f000fu) ^ 0x00080008u; }
+__device__ __forceinline__ uint32_t offsets_15(uint32_t w) { return (w & 0x00f000f0u) ^ 0x00800080u; }
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -113,7 +119,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   const Kv4AttentionArgs& a = p.a;
   extern __shared__ float s_o[];                                   // [kWarps][kRows][kDim] at the end
   __half* const s_q = reinterpret_cast<__half*>(s_o);              // [kRows][kQStride] until then (where Q is in registers)
-  __shared__ float s_f[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
+  __shared__ float s_f[kRows], s_sum[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
   __shared__ __align__(16) __half s_q2[kQInRegs ? 8 : kRows * C::kQStride];
   __half* const q_at = kQInRegs ? s_q : s_q2;
 
@@ -138,8 +144,11 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   if (ch > 0 && k0 >= most) return;
 
   // ---- the first cached tokens are asked for before the queries are worked on
-  const size_t block = kv4_block_bytes(a.pool);
+  const uint32_t block = (kDim + 8u) << a.pool.log_page, stride = block * a.pool.kv_heads;  // of a head's page, of a page
+  const uint8_t* const base = a.pool.base + static_cast<uint64_t>(kvh) * block;
   const int plane = (kDim / 2) << a.pool.log_page, slots = (1 << a.pool.log_page) - 1;
+  const uint32_t k_lane = g * (kDim / 2) + t * (kDim / 8), v_lane = plane + 2 * t * (kDim / 2) + g * (kDim / 16);
+  const uint32_t s_lane = 2 * plane + (((lane >> 4) << a.pool.log_page) + (lane & 15)) * 4;
   struct Stage {
     uint32_t k[2][C::kKeyWords];    // tokens g and g + 8, this lane's quarter of the channels
     uint32_t v[4][C::kValueWords];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, this lane's eighth
@@ -162,17 +171,16 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
       page = 0;
       s.end = 0;
     }
-    const uint8_t* src = a.pool.base + (static_cast<size_t>(page) * a.pool.kv_heads + kvh) * block;
-    const int slot = at & slots;
-    const uint8_t* ks = src + (slot + g) * (kDim / 2) + t * (kDim / 8);
-    const uint8_t* vs = src + plane + (slot + 2 * t) * (kDim / 2) + g * (kDim / 16);
+    const uint8_t* const src = base + static_cast<uint64_t>(static_cast<uint32_t>(page)) * stride;
+    const uint8_t* const codes = src + (at & slots) * (kDim / 2);
+    const uint8_t *const ks = codes + k_lane, *const vs = codes + v_lane;
     load_words(s.k[0], ks);
     load_words(s.k[1], ks + 8 * (kDim / 2));
     load_words(s.v[0], vs);
     load_words(s.v[1], vs + kDim / 2);
     load_words(s.v[2], vs + 8 * (kDim / 2));
     load_words(s.v[3], vs + 9 * (kDim / 2));
-    s.scale = __ldg(reinterpret_cast<const float*>(src + 2 * plane) + ((lane >> 4) << a.pool.log_page) + slot + (lane & 15));
+    s.scale = __ldg(reinterpret_cast<const float*>(src + (at & slots) * 4 + s_lane));
   };
 #pragma unroll
   for (int i = 0; i < C::kStages; ++i) load(i, st[i]);
@@ -194,14 +202,25 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
     for (int h = 1; h < kTeam; h *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
     const int e = min(126, max(-126, static_cast<int>(__float_as_uint(top) >> 23) - 126));
     const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+    float sum = 0.0f;  // of the rounded queries
     if (r < kRows) {
-      uint4 v;
-      v.x = __half_as_ushort(__float2half_rn(y[0] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[4] * down))) << 16;
-      v.y = __half_as_ushort(__float2half_rn(y[1] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[5] * down))) << 16;
-      v.z = __half_as_ushort(__float2half_rn(y[2] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[6] * down))) << 16;
-      v.w = __half_as_ushort(__float2half_rn(y[3] * down)) | static_cast<uint32_t>(__half_as_ushort(__float2half_rn(y[7] * down))) << 16;
-      *reinterpret_cast<uint4*>(q_at + r * C::kQStride + tl * 8) = v;
-      if (tl == 0) s_f[r] = a.scale * kLog2e * up;
+      __half h[8];
+      float total = 0.0f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {  // nibbles 1, 3, 5, 7 are read 16 times too large
+        const float part = (c & 1) ? 0.0625f : 1.0f;
+        h[c] = __float2half_rn(y[c] * down * part);
+        total += __half2float(h[c]) * (c & 1 ? 16.0f : 1.0f);
+      }
+      sum = total;
+      __half2 v[4] = {__halves2half2(h[0], h[4]), __halves2half2(h[1], h[5]), __halves2half2(h[2], h[6]), __halves2half2(h[3], h[7])};
+      *reinterpret_cast<uint4*>(q_at + r * C::kQStride + tl * 8) = *reinterpret_cast<const uint4*>(v);
+    }
+#pragma unroll
+    for (int h = 1; h < kTeam; h *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, h);
+    if (r < kRows && tl == 0) {
+      s_f[r] = a.scale * kLog2e * up;
+      s_sum[r] = sum;
     }
   }
   __syncthreads();
@@ -220,14 +239,15 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
     __syncthreads();  // (s_o takes the queries' place)
   }
   // this lane's rows of S^T and O^T: 8 n + 2 t and the next
-  float f[kTiles][2], m[kTiles][2], mv[kTiles][2], l[kTiles][2], o[kDim / 16][kTiles][4];
+  float f[kTiles][2], zero[kTiles][2], m[kTiles][2], mv[kTiles][2], l[kTiles][2], o[kDim / 16][kTiles][4];
   int seen[kTiles][2], least = most;
 #pragma unroll
   for (int n = 0; n < kTiles; ++n)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int r = 8 * n + 2 * t + e;
-      f[n][e] = s_f[r];
+      f[n][e] = s_f[r] * 0x1p24f;
+      zero[n][e] = -8.0f * 0x1p-24f * s_sum[r];  // what the offset adds to a score, taken from its accumulator's start
       seen[n][e] = seen_by(seq, a.causal, min(row0 + r, row0 + rows - 1) / p.group);
       m[n][e] = mv[n][e] = -FLT_MAX;
       l[n][e] = 0.0f;
@@ -240,13 +260,17 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
 
   auto step = [&](int i, const Stage& s) {
     const int at = k0 + kStep * (warp + kWarps * i);
-    float x[kTiles][4] = {};
+    float x[kTiles][4];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[n][e] = zero[n][e & 1];
 #pragma unroll
     for (int w = 0; w < C::kKeyWords; ++w) {
       uint32_t k0w = s.k[0][w], k1w = s.k[1][w];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t a0 = codes_04(k0w), a1 = codes_04(k1w), a2 = codes_15(k0w), a3 = codes_15(k1w);
+        const uint32_t a0 = offsets_04(k0w), a1 = offsets_04(k1w), a2 = offsets_15(k0w), a3 = offsets_15(k1w);
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
           if constexpr (kQInRegs) {
@@ -263,7 +287,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
     const float own = lane < 16 ? s.scale : lg2(s.scale);
     const float dk0 = __shfl_sync(0xffffffffu, own, g), dk1 = __shfl_sync(0xffffffffu, own, g + 8);
     const float lv0 = __shfl_sync(0xffffffffu, own, g + 16), lv1 = __shfl_sync(0xffffffffu, own, g + 24);
-    float y[kTiles][4];
+    float y[kTiles][4], dx[kTiles][4], dy[kTiles][4];  // scores with the value's scale; both against their references
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -278,12 +302,19 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         for (int e = 0; e < 4; ++e)
           if (at + g + (e < 2 ? 0 : 8) >= min(seen[n][e & 1], s.end)) x[n][e] = y[n][e] = -INFINITY;
     }
-    bool grown = false;
+    float up = -INFINITY;
+    auto against = [&]() {
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n)
+      for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) grown |= x[n][e] > m[n][e & 1] + kGrowth || y[n][e] > mv[n][e & 1] + kGrowth;
-    if (__any_sync(0xffffffffu, grown)) {
+        for (int e = 0; e < 4; ++e) {
+          dx[n][e] = x[n][e] - m[n][e & 1];
+          dy[n][e] = y[n][e] - mv[n][e & 1];
+          up = fmaxf(up, fmaxf(dx[n][e], dy[n][e]));
+        }
+    };
+    against();
+    if (__any_sync(0xffffffffu, up > kGrowth)) {  // move the references to the rows' maxima
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -304,14 +335,15 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
             o[c][n][e + 2] *= keep;
           }
         }
+      against();
     }
     uint32_t b0[kTiles], b1[kTiles];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        l[n][e & 1] += ex2(x[n][e] - m[n][e & 1]);
-        y[n][e] = ex2(y[n][e] - mv[n][e & 1]);
+        l[n][e & 1] += ex2(dx[n][e]);
+        y[n][e] = ex2(dy[n][e]);
       }
       const __half2 lo = __floats2half2_rn(y[n][0], y[n][1]), hi = __floats2half2_rn(y[n][2], y[n][3]);
       b0[n] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
@@ -404,59 +436,70 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   }
 }
 
-// The chunks of every query row joined: a team of D / 8 lanes a row.
+// The chunks of a query row (one head of one token) joined by a CTA: teams of D / 8 lanes take every kTeams-th chunk.
 template <typename T, int kDim>
 __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const __grid_constant__ Kv4Params p) {
-  constexpr int kTeam = kDim / 8;
+  constexpr int kTeam = kDim / 8, kTeams = 32 * kWarps / kTeam;
+  __shared__ float s_m[kTeams], s_l[kTeams];
+  __shared__ __align__(16) float s_y[kTeams][kDim];
   const Kv4AttentionArgs& a = p.a;
+  const int token = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
+  const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam;
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t row_id = (static_cast<int64_t>(blockIdx.x) * (32 * kWarps) + threadIdx.x) / kTeam;
-  const int tl = threadIdx.x % kTeam;
-  // (a warp's rows may lie in two sequences: the search is made for each of them by the whole warp)
-  int token = static_cast<int>(min(row_id / a.heads, static_cast<int64_t>(a.total_q) - 1));
-  const int head = static_cast<int>(row_id % a.heads);
-  int b = -1, first = 0;
-  for (int s = 0; s < 32 / kTeam; ++s) {
-    int b1, f1;
-    const bool found = find_sequence(a.cu_q, a.batch, __shfl_sync(0xffffffffu, token, s * kTeam), b1, f1);
-    if (static_cast<int>(threadIdx.x & 31) / kTeam == s && found) {
-      b = b1;
-      first = f1;
-    }
-  }
-  Sequence seq = {0, 0, 0};
-  bool mine = b >= 0 && row_id < static_cast<int64_t>(a.total_q) * a.heads;
-  if (mine) mine = load_sequence(a, b, seq) && seq.q0 == first;
-  const int kvh = head / p.group, r = (token - seq.q0) * p.group + head % p.group;
-  const int tile = mine ? r / p.rows : 0;
-  const int most = mine ? seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group) : 0;
+  int b, first;
+  Sequence seq;
+  if (!find_sequence(a.cu_q, a.batch, token, b, first) || !load_sequence(a, b, seq) || seq.q0 != first) return;
+  const int kvh = head / p.group, r = (token - first) * p.group + head % p.group, tile = r / p.rows;
+  const int most = seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group);
   const int chunks = (most + p.chunk - 1) / p.chunk;
-  mine = mine && chunks > 1;  // (one chunk's result is written by its CTA)
-  const size_t unit = (static_cast<size_t>(max(b, 0)) * a.pool.kv_heads + kvh) * p.row_tiles + tile;
+  if (chunks < 2) return;  // its CTA has written the result
+  const size_t unit = (static_cast<size_t>(b) * a.pool.kv_heads + kvh) * p.row_tiles + tile;
   const float* const src = p.part + (unit * p.chunks * p.rows + r % p.rows) * (kDim + 2);
   const size_t next = static_cast<size_t>(p.rows) * (kDim + 2);
-  float top = -FLT_MAX, sum = 0.0f, y[8] = {};
-  if (mine) {
-    for (int c = 0; c < chunks; ++c) top = fmaxf(top, src[c * next + kDim]);
+  float m = -FLT_MAX, l = 0.0f, y[8] = {};
 #pragma unroll 4
-    for (int c = 0; c < chunks; ++c) {
-      const float* at = src + c * next;
-      const float k = ex2(at[kDim] - top);
-      sum += at[kDim + 1] * k;
+  for (int c = team; c < chunks; c += kTeams) {
+    const float* const at = src + c * next;
+    const float2 ml = *reinterpret_cast<const float2*>(at + kDim);
+    float2 v[4];
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float2 v = *reinterpret_cast<const float2*>(at + tl * 8 + e);
-        y[e] += v.x * k;
-        y[e + 1] += v.y * k;
-      }
+    for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float2*>(at + tl * 8 + 2 * e);
+    const float top = fmaxf(m, ml.x), keep = ex2(m - top), k = ex2(ml.x - top);
+    m = top;
+    l = l * keep + ml.y * k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[2 * e] = y[2 * e] * keep + v[e].x * k;
+      y[2 * e + 1] = y[2 * e + 1] * keep + v[e].y * k;
     }
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (tl == 0) {
+    s_m[team] = m;
+    s_l[team] = l;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(&s_y[team][tl * 8 + e]) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  m = s_m[0];
+  l = 0.0f;
+#pragma unroll
+  for (int w = 1; w < kTeams; ++w) m = fmaxf(m, s_m[w]);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kTeams; ++w) {
+    const float k = ex2(s_m[w] - m);
+    l += s_l[w] * k;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] += s_y[w][tl * 8 + e] * k;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
   for (int c = 0; c < 8; ++c) y[c] *= inv;
   if (a.pool.rotate) rotate_head<kTeam>(y);
-  if (mine) *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+  if (team == 0) *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
 }
 
 int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * (a.heads / a.pool.kv_heads) <= 8 ? 8 : 16; }
@@ -493,7 +536,7 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
   plan_split(a, a.ws ? a.ws_bytes : 0, &p);
   p.part = static_cast<float*>(a.ws);
   const int64_t ctas = static_cast<int64_t>(a.batch) * a.pool.kv_heads * p.row_tiles * p.chunks;
-  const int64_t joins = (static_cast<int64_t>(a.total_q) * a.heads * (kDim / 8) + 32 * kWarps - 1) / (32 * kWarps);
+  const int64_t joins = static_cast<int64_t>(a.total_q) * a.heads;
   if (ctas > 0x7fffffff || joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
   constexpr int kSmem = kWarps * 8 * kTiles * kDim * 4;
   auto kern = attention_kv4_kernel<T, kDim, kTiles>;
