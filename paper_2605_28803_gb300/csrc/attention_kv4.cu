@@ -3,18 +3,19 @@
 // with codes ck, cv, scales Dk, Dv and, for a rotated cache, q' = q H / sqrt(D) and the output o H / sqrt(D).
 //
 // For single tokens the codes' bytes (D + 8 for a token and head) are the bound, for chunks the launch and the matrix
-// instructions.  A warp takes 16 cached tokens at a time, straight from global memory into the registers of mma.m16n8k16
-// fragments: the contraction over channels and the rows of O may be permuted at will, so a lane's share of a key is D / 8
-// contiguous bytes and of a value D / 16, and no byte crosses shared memory.
+// instructions.  A warp takes 16 cached tokens at a time through a ring of its own in shared memory (16-byte cp.async, several
+// steps ahead; loads into registers came no further ahead than one step) into the registers of mma.m16n8k16 fragments:
+// the contraction over channels and the rows of O may be permuted at will, so a lane's share of a key is D / 8 contiguous
+// bytes and of a value D / 16.  16-byte pieces are placed so that no read meets a bank conflict.
 //   S^T = K Q^T      A = key codes (16 keys x 16 channels), B = queries (8 rows): grouped heads' single tokens fill 8 columns
 //   O^T += V^T P^T   A = value codes (16 channels x 16 keys), B = P^T, from S^T's accumulators by an 8 x 8 transpose
 // A value's code becomes float16 by one logic operation and one exact addition on two at a time.  A key's takes the logic
 // operation alone: code + 8 in the low bits of a float16 is the subnormal (code + 8) 2^-24 (2^-20 from the nibble above, whose
 // queries carry a factor 1/16), and 8 sum_c q'_c is taken from the row's scores.  (For values that offset would grow with
 // the number of tokens and cost the sum its last bits.)
-//   Dk_j multiplies the score.  Dv_j joins the exponent: the weight that is rounded to float16 for the second product is
-// w_j = exp2(s_j + log2 Dv_j - r) against a running reference r of its own, so it has float16's 11 bits whatever the scales'
-// size, while sum_j p_j is kept in float32 against max s.  References move when a weight would pass 2^8.
+//   Dk_j multiplies the score, Dv_j the probability: p_j = exp2(s_j - r) is summed in float32, and w_j = p_j Dv_j is rounded to
+// float16 for the second product.  The row's reference r follows the largest w, not the largest p, so a weight has float16's
+// 11 bits whatever the scales' size; it moves when a w would pass 2^8 (or a p 2^96, where all scales are tiny).
 //   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
 // float16.
 //
@@ -32,7 +33,8 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kGrowth = 8.0f;  // log2 of the largest weight
+constexpr float kMostWeight = 256.0f, kMostP = 0x1p96f;  // what a reference lets through
+constexpr float kLeastScale = -88.0f;                     // log2 of the scale below which p bounds the reference
 constexpr int kStep = 16;        // cached tokens a warp takes at once
 
 struct Kv4Params {
@@ -71,23 +73,22 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
 }
 
 template <int kWords>
-__device__ __forceinline__ void load_words(uint32_t (&r)[kWords], const uint8_t* p) {
+__device__ __forceinline__ void read_words(uint32_t (&r)[kWords], uint32_t at) {
   if constexpr (kWords == 1) {
-    r[0] = __ldg(reinterpret_cast<const unsigned int*>(p));
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r[0]) : "r"(at));
   } else if constexpr (kWords == 2) {
-    const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-    r[0] = v.x;
-    r[1] = v.y;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(at));
   } else {
-#pragma unroll
-    for (int i = 0; i < kWords; i += 4) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + i * 4));
-      r[i] = v.x;
-      r[i + 1] = v.y;
-      r[i + 2] = v.z;
-      r[i + 3] = v.w;
-    }
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
   }
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kBut>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kBut) : "memory");
 }
 
 // One sequence as the launch's bounds admit it; false where it is to be skipped.
@@ -103,25 +104,32 @@ __device__ __forceinline__ bool load_sequence(const Kv4AttentionArgs& a, int b, 
 // Cached tokens that query token i sees.
 __device__ __forceinline__ int seen_by(const Sequence& s, int causal, int i) { return causal ? max(0, s.len - s.n + i + 1) : s.len; }
 
-template <int kDim>
+template <int kDim, int kTiles>
 struct Cfg {
-  static constexpr int kKeyWords = kDim / 32, kValueWords = kDim / 64;  // a lane's words of a key, of a value
-  static constexpr int kStages = kDim == 64 ? 4 : 2;                    // 16-token steps in flight
-  static constexpr int kTeam = kDim / 8;                                // lanes that hold a head, 8 channels each
-  static constexpr int kQStride = kDim + 8;                             // float16 of a staged query row
+  static constexpr int kRows = 8 * kTiles;
+  static constexpr int kTeam = kDim / 8;                   // lanes that hold a head, 8 channels each
+  static constexpr int kQStride = kDim + 8;                // float16 of a staged query row
+  static constexpr int kStages = kDim == 256 ? 3 : 4;      // steps of a warp's ring
+  static constexpr int kStepBytes = kStep * (kDim + 8);    // key codes, value codes, key scales, value scales
+  static constexpr int kRing = kWarps * kStages * kStepBytes;
+  static constexpr int kJoin = kWarps * kRows * kDim * 4;  // the warps' sums, over the ring at the end
+  static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kRows * kQStride * 2;
 };
 
 template <typename T, int kDim, int kTiles>
 __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid_constant__ Kv4Params p) {
-  using C = Cfg<kDim>;
-  constexpr int kRows = 8 * kTiles, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam;
+  using C = Cfg<kDim, kTiles>;
+  constexpr int kRows = C::kRows, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam, kStages = C::kStages;
+  constexpr int kRow = kDim / 2;  // bytes of a token's codes
   constexpr bool kQInRegs = kTiles * kDim <= 256;
   const Kv4AttentionArgs& a = p.a;
-  extern __shared__ float s_o[];                                   // [kWarps][kRows][kDim] at the end
-  __half* const s_q = reinterpret_cast<__half*>(s_o);              // [kRows][kQStride] until then (where Q is in registers)
+  extern __shared__ __align__(128) uint8_t s_raw[];
+  __half* const q_at = reinterpret_cast<__half*>(s_raw);                      // [kRows][kQStride]
+  uint8_t* const s_ring = s_raw + kRows * C::kQStride * 2;                    // [kWarps][kStages][kStepBytes]
+  float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kDim] at the end
+  static_assert(kRows * C::kQStride * 2 % 128 == 0, "the ring's pieces are placed by 128-byte lines");
   __shared__ float s_f[kRows], s_sum[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
-  __shared__ __align__(16) __half s_q2[kQInRegs ? 8 : kRows * C::kQStride];
-  __half* const q_at = kQInRegs ? s_q : s_q2;
+  __shared__ int s_end[kWarps][kStages];  // first token of a step's that nobody may use
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int u = blockIdx.x;
@@ -146,44 +154,52 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   // ---- the first cached tokens are asked for before the queries are worked on
   const uint32_t block = (kDim + 8u) << a.pool.log_page, stride = block * a.pool.kv_heads;  // of a head's page, of a page
   const uint8_t* const base = a.pool.base + static_cast<uint64_t>(kvh) * block;
-  const int plane = (kDim / 2) << a.pool.log_page, slots = (1 << a.pool.log_page) - 1;
-  const uint32_t k_lane = g * (kDim / 2) + t * (kDim / 8), v_lane = plane + 2 * t * (kDim / 2) + g * (kDim / 16);
-  const uint32_t s_lane = 2 * plane + (((lane >> 4) << a.pool.log_page) + (lane & 15)) * 4;
-  struct Stage {
-    uint32_t k[2][C::kKeyWords];    // tokens g and g + 8, this lane's quarter of the channels
-    uint32_t v[4][C::kValueWords];  // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, this lane's eighth
-    float scale;                    // lane i < 16: the key scale of token i; else the value scale of token i - 16
-    int end;                        // first token that nobody may use
-  } st[C::kStages];
+  const int plane = kRow << a.pool.log_page, slots = (1 << a.pool.log_page) - 1;
   const int steps = k1 > k0 + kStep * warp ? (k1 - k0 - kStep * warp + kStep * kWarps - 1) / (kStep * kWarps) : 0;
-  int pages = 0;  // of 32 steps, one a lane
-  auto load = [&](int i, Stage& s) {
-    if (i >= steps) return;
-    if ((i & 31) == 0) {
-      const int at = k0 + kStep * (warp + kWarps * (i + lane));
-      pages = at < k1 ? __ldg(a.table + static_cast<size_t>(b) * a.max_pages + (at >> a.pool.log_page)) : 0;
+  // Places in the ring.  Keys: as they are, with 256 channels a row's 16-byte pieces exchanged in pairs in odd rows.  Values: a
+  // 128-byte line's pieces c at c ^ 2 x, x counting pairs of rows (with 64 channels groups of four).
+  const uint32_t ring = smem_u32(s_ring) + warp * kStages * C::kStepBytes;
+  auto key_piece = [](int row, int c) { return kDim == 256 ? c ^ (row & 1) : c; };
+  auto value_place = [](int row, int c) {  // of piece c of a row's kRow / 16
+    const int at = row * (kRow / 16) + c, x = kDim == 64 ? (row >> 2) & 1 : (row >> 1) & 3;
+    return 16 * ((at & ~7) | ((at & 7) ^ (2 * x)));
+  };
+  const int row_first = lane / (kRow / 16), piece = lane % (kRow / 16);
+  const uint32_t k_put = row_first * kRow + 16 * key_piece(row_first, piece), v_put = 8 * kDim + value_place(row_first, piece);
+  const uint32_t s_put = 16 * kDim + (lane & 7) * 16;
+  const uint32_t s_src = 2 * plane + (((lane >> 2) & 1) << a.pool.log_page) * 4 + (lane & 3) * 16;
+  int pages = 0;         // of 32 steps, one a lane
+  uint32_t missing = 0;  // those of them that are not there
+  auto load = [&](int i, int slot) {
+    if (i < steps) {
+      if ((i & 31) == 0) {
+        const int at = k0 + kStep * (warp + kWarps * (i + lane));
+        pages = at < k1 ? __ldg(a.table + static_cast<size_t>(b) * a.max_pages + (at >> a.pool.log_page)) : 0;
+        const bool none = static_cast<uint32_t>(pages) >= static_cast<uint32_t>(a.pool.num_pages);
+        missing = __ballot_sync(0xffffffffu, none);
+        if (none) {
+          report_index();
+          pages = 0;
+        }
+      }
+      const int page = __shfl_sync(0xffffffffu, pages, i & 31);
+      const int in = (k0 + kStep * (warp + kWarps * i)) & slots;
+      const uint8_t* const src = base + static_cast<uint64_t>(static_cast<uint32_t>(page)) * stride;
+      const uint8_t* const codes = src + in * kRow + lane * 16;
+      const uint32_t to = ring + slot * C::kStepBytes;
+#pragma unroll
+      for (int c = 0; c < kDim / 64; ++c) {
+        // (256 channels: the next four rows, whose pieces are placed two pairs of rows on)
+        copy16(to + (k_put + c * 512), codes + c * 512);
+        copy16(to + ((kDim == 256 && (c & 1) ? v_put ^ 64 : v_put) + c * 512), codes + plane + c * 512);
+      }
+      if (lane < 8) copy16(to + s_put, src + s_src + in * 4);
+      if (lane == 0) s_end[warp][slot] = missing >> (i & 31) & 1 ? 0 : k1;
     }
-    int page = __shfl_sync(0xffffffffu, pages, i & 31);
-    const int at = k0 + kStep * (warp + kWarps * i);
-    s.end = k1;
-    if (page < 0 || page >= a.pool.num_pages) {
-      if (lane == 0) report_index();
-      page = 0;
-      s.end = 0;
-    }
-    const uint8_t* const src = base + static_cast<uint64_t>(static_cast<uint32_t>(page)) * stride;
-    const uint8_t* const codes = src + (at & slots) * (kDim / 2);
-    const uint8_t *const ks = codes + k_lane, *const vs = codes + v_lane;
-    load_words(s.k[0], ks);
-    load_words(s.k[1], ks + 8 * (kDim / 2));
-    load_words(s.v[0], vs);
-    load_words(s.v[1], vs + kDim / 2);
-    load_words(s.v[2], vs + 8 * (kDim / 2));
-    load_words(s.v[3], vs + 9 * (kDim / 2));
-    s.scale = __ldg(reinterpret_cast<const float*>(src + (at & slots) * 4 + s_lane));
+    copy_commit();
   };
 #pragma unroll
-  for (int i = 0; i < C::kStages; ++i) load(i, st[i]);
+  for (int i = 0; i < kStages - 1; ++i) load(i, i);
 
   // ---- queries: rotated, scaled by a power of two, float16, in the order of the codes' pairs
 #pragma unroll
@@ -236,10 +252,9 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         q[n][4 * w + 2] = v.z;
         q[n][4 * w + 3] = v.w;
       }
-    __syncthreads();  // (s_o takes the queries' place)
   }
   // this lane's rows of S^T and O^T: 8 n + 2 t and the next
-  float f[kTiles][2], zero[kTiles][2], m[kTiles][2], mv[kTiles][2], l[kTiles][2], o[kDim / 16][kTiles][4];
+  float f[kTiles][2], zero[kTiles][2], m[kTiles][2], l[kTiles][2], o[kDim / 16][kTiles][4];
   int seen[kTiles][2], least = most;
 #pragma unroll
   for (int n = 0; n < kTiles; ++n)
@@ -249,7 +264,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
       f[n][e] = s_f[r] * 0x1p24f;
       zero[n][e] = -8.0f * 0x1p-24f * s_sum[r];  // what the offset adds to a score, taken from its accumulator's start
       seen[n][e] = seen_by(seq, a.causal, min(row0 + r, row0 + rows - 1) / p.group);
-      m[n][e] = mv[n][e] = -FLT_MAX;
+      m[n][e] = -FLT_MAX;
       l[n][e] = 0.0f;
     }
   if (a.causal) least = seen_by(seq, 1, row0 / p.group);  // of the first row
@@ -258,15 +273,49 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.0f;
 
-  auto step = [&](int i, const Stage& s) {
+  // this lane's reads of a step: tokens g and g + 8 of the keys, 2 t, 2 t + 1, 2 t + 8 and 2 t + 9 of the values
+  constexpr int kKeyWords = kDim / 32, kValueWords = kDim / 64;
+  const uint32_t k_get = g * kRow + (kDim == 256 ? 0 : t * (kDim / 8));
+  uint32_t v_get[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) v_get[e] = 8 * kDim + value_place(2 * t + e, g * (kDim / 16) / 16) + (g * (kDim / 16) & 15);
+  auto step = [&](int i, int slot) {
     const int at = k0 + kStep * (warp + kWarps * i);
-    float x[kTiles][4];
+    const uint32_t from = ring + slot * C::kStepBytes;
+    struct {
+      uint32_t k[2][kKeyWords], v[4][kValueWords];
+      int end;
+    } s;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if constexpr (kDim == 256) {
+        uint32_t lo[4], hi[4];
+        read_words(lo, from + k_get + e * 8 * kRow + 16 * ((2 * t) ^ (g & 1)));
+        read_words(hi, from + k_get + e * 8 * kRow + 16 * ((2 * t + 1) ^ (g & 1)));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          s.k[e][w] = lo[w];
+          s.k[e][w + kKeyWords - 4] = hi[w];
+        }
+      } else {
+        read_words(s.k[e], from + k_get + e * 8 * kRow);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) read_words(s.v[e], from + v_get[e & 1] + (e >> 1) * 8 * kRow);
+    uint32_t scale[4][1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) read_words(scale[e], from + 16 * kDim + g * 4 + e * 32);
+    const float dk0 = __uint_as_float(scale[0][0]), dk1 = __uint_as_float(scale[1][0]), dv0 = __uint_as_float(scale[2][0]), dv1 = __uint_as_float(scale[3][0]);
+    s.end = *const_cast<volatile int*>(&s_end[warp][slot]);
+    constexpr int kChains = kTiles == 1 ? 2 : 1;  // independent sums of a score
+    float x[kTiles][4], x2[4] = {};
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[n][e] = zero[n][e & 1];
 #pragma unroll
-    for (int w = 0; w < C::kKeyWords; ++w) {
+    for (int w = 0; w < kKeyWords; ++w) {
       uint32_t k0w = s.k[0][w], k1w = s.k[1][w];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -274,7 +323,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
           if constexpr (kQInRegs) {
-            mma16816(x[n], a0, a1, a2, a3, q[n][4 * w + 2 * h], q[n][4 * w + 2 * h + 1]);
+            mma16816(kChains == 2 && h ? x2 : x[n], a0, a1, a2, a3, q[n][4 * w + 2 * h], q[n][4 * w + 2 * h + 1]);
           } else {
             const uint2 v = *reinterpret_cast<const uint2*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w + 4 * h);
             mma16816(x[n], a0, a1, a2, a3, v.x, v.y);
@@ -284,51 +333,52 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         k1w >>= 8;
       }
     }
-    const float own = lane < 16 ? s.scale : lg2(s.scale);
-    const float dk0 = __shfl_sync(0xffffffffu, own, g), dk1 = __shfl_sync(0xffffffffu, own, g + 8);
-    const float lv0 = __shfl_sync(0xffffffffu, own, g + 16), lv1 = __shfl_sync(0xffffffffu, own, g + 24);
-    float y[kTiles][4], dx[kTiles][4], dy[kTiles][4];  // scores with the value's scale; both against their references
-#pragma unroll
-    for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[n][e] *= (e < 2 ? dk0 : dk1) * f[n][e & 1];
-        y[n][e] = x[n][e] + (e < 2 ? lv0 : lv1);
-      }
-    if (at + kStep > min(least, s.end)) {  // some row does not see all of these tokens
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (at + g + (e < 2 ? 0 : 8) >= min(seen[n][e & 1], s.end)) x[n][e] = y[n][e] = -INFINITY;
-    }
-    float up = -INFINITY;
+    float pr[kTiles][4], wt[kTiles][4];  // probabilities, weights
+    float most_p = 0.0f, most_w = 0.0f;
+    const bool hidden = at + kStep > min(least, s.end);  // some row does not see all of these tokens
     auto against = [&]() {
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          dx[n][e] = x[n][e] - m[n][e & 1];
-          dy[n][e] = y[n][e] - mv[n][e & 1];
-          up = fmaxf(up, fmaxf(dx[n][e], dy[n][e]));
+          pr[n][e] = ex2(fmaf(x[n][e], (e < 2 ? dk0 : dk1) * f[n][e & 1], -m[n][e & 1]));
+          wt[n][e] = pr[n][e] * (e < 2 ? dv0 : dv1);
         }
+      if (hidden) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at + g + (e < 2 ? 0 : 8) >= min(seen[n][e & 1], s.end)) pr[n][e] = wt[n][e] = 0.0f;
+      }
     };
+    if constexpr (kChains == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[0][e] += x2[e];
+    }
     against();
-    if (__any_sync(0xffffffffu, up > kGrowth)) {  // move the references to the rows' maxima
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        most_p = fmaxf(most_p, fmaxf(pr[n][e], pr[n][e + 1]));
+        most_w = fmaxf(most_w, fmaxf(wt[n][e], wt[n][e + 1]));
+      }
+    // (p = inf times a scale of 0 is the NaN that fmax passes over: p shows it)
+    if (__any_sync(0xffffffffu, most_w > kMostWeight || most_p > kMostP)) {  // move the references
+      const float lv0 = fmaxf(lg2(dv0), kLeastScale), lv1 = fmaxf(lg2(dv1), kLeastScale);
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float top = fmaxf(m[n][e], fmaxf(x[n][e], x[n][e + 2])), topv = fmaxf(mv[n][e], fmaxf(y[n][e], y[n][e + 2]));
+          float top = m[n][e];
+          if (!hidden || at + g < min(seen[n][e], s.end)) top = fmaxf(top, x[n][e] * (dk0 * f[n][e]) + lv0);
+          if (!hidden || at + g + 8 < min(seen[n][e], s.end)) top = fmaxf(top, x[n][e + 2] * (dk1 * f[n][e]) + lv1);
 #pragma unroll
-          for (int h = 4; h < 32; h *= 2) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
-            topv = fmaxf(topv, __shfl_xor_sync(0xffffffffu, topv, h));
-          }
-          l[n][e] *= ex2(m[n][e] - top);
-          const float keep = ex2(mv[n][e] - topv);
+          for (int h = 4; h < 32; h *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
+          const float keep = ex2(m[n][e] - top);
+          l[n][e] *= keep;
           m[n][e] = top;
-          mv[n][e] = topv;
 #pragma unroll
           for (int c = 0; c < kDim / 16; ++c) {
             o[c][n][e] *= keep;
@@ -341,16 +391,13 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        l[n][e & 1] += ex2(dx[n][e]);
-        y[n][e] = ex2(dy[n][e]);
-      }
-      const __half2 lo = __floats2half2_rn(y[n][0], y[n][1]), hi = __floats2half2_rn(y[n][2], y[n][3]);
+      for (int e = 0; e < 4; ++e) l[n][e & 1] += pr[n][e];
+      const __half2 lo = __floats2half2_rn(wt[n][0], wt[n][1]), hi = __floats2half2_rn(wt[n][2], wt[n][3]);
       b0[n] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
       b1[n] = transpose8(*reinterpret_cast<const uint32_t*>(&hi));
     }
 #pragma unroll
-    for (int w = 0; w < C::kValueWords; ++w)
+    for (int w = 0; w < kValueWords; ++w)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {  // channels 4 h .. 4 h + 3 of the word, two tokens in each register
         uint32_t v0 = __byte_perm(s.v[0][w], s.v[1][w], h ? 0x7632 : 0x5410), v1 = __byte_perm(s.v[2][w], s.v[3][w], h ? 0x7632 : 0x5410);
@@ -364,17 +411,19 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         }
       }
   };
-  for (int i = 0; i < steps; i += C::kStages) {
-#pragma unroll
-    for (int e = 0; e < C::kStages; ++e) {
-      if (i + e < steps) {
-        step(i + e, st[e]);
-        load(i + e + C::kStages, st[e]);
-      }
-    }
+  int slot = 0, fill = kStages - 1;
+  for (int i = 0; i < steps; ++i) {
+    copy_wait<kStages - 2>();
+    __syncwarp();  // step i has landed for every lane, and every lane has read step i - 1
+    load(i + kStages - 1, fill);
+    step(i, slot);
+    fill = slot;
+    if (++slot == kStages) slot = 0;
   }
+  copy_wait<0>();
+  __syncthreads();  // the warps' sums take the rings' place
 
-  // ---- join the warps; sums over the values are brought to the reference of the sum of p
+  // ---- join the warps
 #pragma unroll
   for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -386,12 +435,11 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         s_m[warp][r] = m[n][e];
         s_l[warp][r] = l[n][e];
       }
-      const float back = ex2(mv[n][e] - m[n][e]);
       float* const dst = s_o + (warp * kRows + r) * kDim + g * (kDim / 8);
 #pragma unroll
       for (int c = 0; c < kDim / 16; ++c) {
-        dst[2 * c] = o[c][n][e] * back;
-        dst[2 * c + 1] = o[c][n][e + 2] * back;
+        dst[2 * c] = o[c][n][e];
+        dst[2 * c + 1] = o[c][n][e + 2];
       }
     }
   __syncthreads();
@@ -538,16 +586,16 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
   const int64_t ctas = static_cast<int64_t>(a.batch) * a.pool.kv_heads * p.row_tiles * p.chunks;
   const int64_t joins = static_cast<int64_t>(a.total_q) * a.heads;
   if (ctas > 0x7fffffff || joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  constexpr int kSmem = kWarps * 8 * kTiles * kDim * 4;
+  using C = Cfg<kDim, kTiles>;
   auto kern = attention_kv4_kernel<T, kDim, kTiles>;
-  if (kSmem > 48 * 1024) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  if (C::kSmem > 48 * 1024) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ctas));
   cfg.blockDim = dim3(32 * kWarps);
-  cfg.dynamicSmemBytes = kSmem;
+  cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = a.stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
