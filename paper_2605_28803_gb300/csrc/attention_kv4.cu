@@ -3,7 +3,7 @@
 // with codes ck, cv, scales Dk, Dv and, for a rotated cache, q' = q H / sqrt(D) and the output o H / sqrt(D).
 //
 // For single tokens the codes' bytes (D + 8 for a token and head) are the bound, for chunks the launch and the matrix
-// instructions.  A warp takes 16 cached tokens at a time through a ring of its own in shared memory (16-byte cp.async, several
+// instructions.  A warp takes 16 or 32 cached tokens at a time through a ring of its own in shared memory (16-byte cp.async, several
 // steps ahead; loads into registers came no further ahead than one step) into the registers of mma.m16n8k16 fragments:
 // the contraction over channels and the rows of O may be permuted at will, so a lane's share of a key is D / 8 contiguous
 // bytes and of a value D / 16.  16-byte pieces are placed so that no read meets a bank conflict.
@@ -35,7 +35,7 @@ constexpr int kWarps = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostWeight = 256.0f, kMostP = 0x1p96f;  // what a reference lets through
 constexpr float kLeastScale = -88.0f;                     // log2 of the scale below which p bounds the reference
-constexpr int kStep = 16;        // cached tokens a warp takes at once
+constexpr int kTile = 16;        // cached tokens of a matrix instruction
 
 struct Kv4Params {
   Kv4AttentionArgs a;
@@ -109,8 +109,12 @@ struct Cfg {
   static constexpr int kRows = 8 * kTiles;
   static constexpr int kTeam = kDim / 8;                   // lanes that hold a head, 8 channels each
   static constexpr int kQStride = kDim + 8;                // float16 of a staged query row
-  static constexpr int kStages = kDim == 256 ? 3 : 4;      // steps of a warp's ring
-  static constexpr int kStepBytes = kStep * (kDim + 8);    // key codes, value codes, key scales, value scales
+  // A step of 32 tokens halves the work around the matrix instructions, for as many registers as single tokens leave free.
+  static constexpr int kParts = kTiles == 1 && kDim < 256 ? 2 : 1;
+  static constexpr int kStep = kTile * kParts;              // cached tokens a warp takes at once
+  static constexpr int kStages = kDim == 256 || kParts == 2 ? 3 : 4;  // steps of a warp's ring
+  static constexpr int kPartBytes = kTile * (kDim + 8);    // key codes, value codes, key scales, value scales
+  static constexpr int kStepBytes = kParts * kPartBytes;
   static constexpr int kRing = kWarps * kStages * kStepBytes;
   static constexpr int kJoin = kWarps * kRows * kDim * 4;  // the warps' sums, over the ring at the end
   static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kRows * kQStride * 2;
@@ -119,7 +123,8 @@ struct Cfg {
 template <typename T, int kDim, int kTiles>
 __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid_constant__ Kv4Params p) {
   using C = Cfg<kDim, kTiles>;
-  constexpr int kRows = C::kRows, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam, kStages = C::kStages;
+  constexpr int kRows = C::kRows, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam, kStages = C::kStages, kParts = C::kParts,
+                kStep = C::kStep;
   constexpr int kRow = kDim / 2;  // bytes of a token's codes
   constexpr bool kQInRegs = kTiles * kDim <= 256;
   const Kv4AttentionArgs& a = p.a;
@@ -129,7 +134,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kDim] at the end
   static_assert(kRows * C::kQStride * 2 % 128 == 0, "the ring's pieces are placed by 128-byte lines");
   __shared__ float s_f[kRows], s_sum[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
-  __shared__ int s_end[kWarps][kStages];  // first token of a step's that nobody may use
+  __shared__ int s_end[kWarps][kStages][kParts];  // first token that nobody may use
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   int u = blockIdx.x;
@@ -168,12 +173,13 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   const uint32_t k_put = row_first * kRow + 16 * key_piece(row_first, piece), v_put = 8 * kDim + value_place(row_first, piece);
   const uint32_t s_put = 16 * kDim + (lane & 7) * 16;
   const uint32_t s_src = 2 * plane + (((lane >> 2) & 1) << a.pool.log_page) * 4 + (lane & 3) * 16;
-  int pages = 0;         // of 32 steps, one a lane
+  constexpr int kFetch = 32 / kParts;  // steps whose pages are fetched at once, one a lane
+  int pages = 0;
   uint32_t missing = 0;  // those of them that are not there
   auto load = [&](int i, int slot) {
     if (i < steps) {
-      if ((i & 31) == 0) {
-        const int at = k0 + kStep * (warp + kWarps * (i + lane));
+      if (i % kFetch == 0) {
+        const int at = k0 + kStep * (warp + kWarps * (i + lane / kParts)) + kTile * (lane % kParts);
         pages = at < k1 ? __ldg(a.table + static_cast<size_t>(b) * a.max_pages + (at >> a.pool.log_page)) : 0;
         const bool none = static_cast<uint32_t>(pages) >= static_cast<uint32_t>(a.pool.num_pages);
         missing = __ballot_sync(0xffffffffu, none);
@@ -182,19 +188,24 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
           pages = 0;
         }
       }
-      const int page = __shfl_sync(0xffffffffu, pages, i & 31);
-      const int in = (k0 + kStep * (warp + kWarps * i)) & slots;
-      const uint8_t* const src = base + static_cast<uint64_t>(static_cast<uint32_t>(page)) * stride;
-      const uint8_t* const codes = src + in * kRow + lane * 16;
-      const uint32_t to = ring + slot * C::kStepBytes;
+      const int at = k0 + kStep * (warp + kWarps * i);
+      uint32_t to = ring + slot * C::kStepBytes;
 #pragma unroll
-      for (int c = 0; c < kDim / 64; ++c) {
-        // (256 channels: the next four rows, whose pieces are placed two pairs of rows on)
-        copy16(to + (k_put + c * 512), codes + c * 512);
-        copy16(to + ((kDim == 256 && (c & 1) ? v_put ^ 64 : v_put) + c * 512), codes + plane + c * 512);
+      for (int h = 0; h < kParts; ++h, to += C::kPartBytes) {
+        const int from = i % kFetch * kParts + h;
+        const int page = __shfl_sync(0xffffffffu, pages, from);
+        const int in = (at + kTile * h) & slots;
+        const uint8_t* const src = base + static_cast<uint64_t>(static_cast<uint32_t>(page)) * stride;
+        const uint8_t* const codes = src + in * kRow + lane * 16;
+#pragma unroll
+        for (int c = 0; c < kDim / 64; ++c) {
+          // (256 channels: the next four rows, whose pieces are placed two pairs of rows on)
+          copy16(to + (k_put + c * 512), codes + c * 512);
+          copy16(to + ((kDim == 256 && (c & 1) ? v_put ^ 64 : v_put) + c * 512), codes + plane + c * 512);
+        }
+        if (lane < 8) copy16(to + s_put, src + s_src + in * 4);
+        if (lane == 0) s_end[warp][slot][h] = missing >> from & 1 ? 0 : k1;
       }
-      if (lane < 8) copy16(to + s_put, src + s_src + in * 4);
-      if (lane == 0) s_end[warp][slot] = missing >> (i & 31) & 1 ? 0 : k1;
     }
     copy_commit();
   };
@@ -282,98 +293,109 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   auto step = [&](int i, int slot) {
     const int at = k0 + kStep * (warp + kWarps * i);
     const uint32_t from = ring + slot * C::kStepBytes;
-    struct {
-      uint32_t k[2][kKeyWords], v[4][kValueWords];
-      int end;
-    } s;
+    float x[kParts][kTiles][4], dk[kParts][2], dv[kParts][2];
+    int end[kParts], first_end = k1;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      if constexpr (kDim == 256) {
-        uint32_t lo[4], hi[4];
-        read_words(lo, from + k_get + e * 8 * kRow + 16 * ((2 * t) ^ (g & 1)));
-        read_words(hi, from + k_get + e * 8 * kRow + 16 * ((2 * t + 1) ^ (g & 1)));
+    for (int h = 0; h < kParts; ++h) {
+      uint32_t k[2][kKeyWords];
+      const uint32_t part = from + h * C::kPartBytes;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          s.k[e][w] = lo[w];
-          s.k[e][w + kKeyWords - 4] = hi[w];
-        }
-      } else {
-        read_words(s.k[e], from + k_get + e * 8 * kRow);
-      }
-    }
+      for (int e = 0; e < 2; ++e) {
+        if constexpr (kDim == 256) {
+          uint32_t lo[4], hi[4];
+          read_words(lo, part + k_get + e * 8 * kRow + 16 * ((2 * t) ^ (g & 1)));
+          read_words(hi, part + k_get + e * 8 * kRow + 16 * ((2 * t + 1) ^ (g & 1)));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) read_words(s.v[e], from + v_get[e & 1] + (e >> 1) * 8 * kRow);
-    uint32_t scale[4][1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) read_words(scale[e], from + 16 * kDim + g * 4 + e * 32);
-    const float dk0 = __uint_as_float(scale[0][0]), dk1 = __uint_as_float(scale[1][0]), dv0 = __uint_as_float(scale[2][0]), dv1 = __uint_as_float(scale[3][0]);
-    s.end = *const_cast<volatile int*>(&s_end[warp][slot]);
-    constexpr int kChains = kTiles == 1 ? 2 : 1;  // independent sums of a score
-    float x[kTiles][4], x2[4] = {};
-#pragma unroll
-    for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] = zero[n][e & 1];
-#pragma unroll
-    for (int w = 0; w < kKeyWords; ++w) {
-      uint32_t k0w = s.k[0][w], k1w = s.k[1][w];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t a0 = offsets_04(k0w), a1 = offsets_04(k1w), a2 = offsets_15(k0w), a3 = offsets_15(k1w);
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-          if constexpr (kQInRegs) {
-            mma16816(kChains == 2 && h ? x2 : x[n], a0, a1, a2, a3, q[n][4 * w + 2 * h], q[n][4 * w + 2 * h + 1]);
-          } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w + 4 * h);
-            mma16816(x[n], a0, a1, a2, a3, v.x, v.y);
+          for (int w = 0; w < 4; ++w) {
+            k[e][w] = lo[w];
+            k[e][w + kKeyWords - 4] = hi[w];
           }
+        } else {
+          read_words(k[e], part + k_get + e * 8 * kRow);
         }
-        k0w >>= 8;
-        k1w >>= 8;
+        uint32_t d[1];
+        read_words(d, part + 16 * kDim + g * 4 + e * 32);
+        dk[h][e] = __uint_as_float(d[0]);
+        read_words(d, part + 16 * kDim + 64 + g * 4 + e * 32);
+        dv[h][e] = __uint_as_float(d[0]);
       }
-    }
-    float pr[kTiles][4], wt[kTiles][4];  // probabilities, weights
-    float most_p = 0.0f, most_w = 0.0f;
-    const bool hidden = at + kStep > min(least, s.end);  // some row does not see all of these tokens
-    auto against = [&]() {
+      end[h] = *const_cast<volatile int*>(&s_end[warp][slot][h]);
+      first_end = min(first_end, end[h]);
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          pr[n][e] = ex2(fmaf(x[n][e], (e < 2 ? dk0 : dk1) * f[n][e & 1], -m[n][e & 1]));
-          wt[n][e] = pr[n][e] * (e < 2 ? dv0 : dv1);
+        for (int e = 0; e < 4; ++e) x[h][n][e] = zero[n][e & 1];
+      float x2[4] = {};  // one tile: two independent sums of a score
+#pragma unroll
+      for (int w = 0; w < kKeyWords; ++w) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t a0 = offsets_04(k[0][w]), a1 = offsets_04(k[1][w]), a2 = offsets_15(k[0][w]), a3 = offsets_15(k[1][w]);
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) {
+            if constexpr (kQInRegs) {
+              mma16816(kTiles == 1 && c ? x2 : x[h][n], a0, a1, a2, a3, q[n][4 * w + 2 * c], q[n][4 * w + 2 * c + 1]);
+            } else {
+              const uint2 v = *reinterpret_cast<const uint2*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w + 4 * c);
+              mma16816(x[h][n], a0, a1, a2, a3, v.x, v.y);
+            }
+          }
+          k[0][w] >>= 8;
+          k[1][w] >>= 8;
         }
-      if (hidden) {
+      }
+      if constexpr (kTiles == 1) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[h][0][e] += x2[e];
+      }
+    }
+    float pr[kParts][kTiles][4], wt[kParts][kTiles][4];  // probabilities, weights
+    const bool hidden = at + kStep > min(least, first_end);  // some row does not see all of these tokens
+    auto sees = [&](int h, int n, int e) { return at + kTile * h + g + (e < 2 ? 0 : 8) < min(seen[n][e & 1], end[h]); };
+    auto against = [&]() {
+#pragma unroll
+      for (int h = 0; h < kParts; ++h)
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (at + g + (e < 2 ? 0 : 8) >= min(seen[n][e & 1], s.end)) pr[n][e] = wt[n][e] = 0.0f;
+          for (int e = 0; e < 4; ++e) {
+            pr[h][n][e] = ex2(fmaf(x[h][n][e], dk[h][e >> 1] * f[n][e & 1], -m[n][e & 1]));
+            wt[h][n][e] = pr[h][n][e] * dv[h][e >> 1];
+          }
+      if (hidden) {
+#pragma unroll
+        for (int h = 0; h < kParts; ++h)
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!sees(h, n, e)) pr[h][n][e] = wt[h][n][e] = 0.0f;
       }
     };
-    if constexpr (kChains == 2) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[0][e] += x2[e];
-    }
     against();
+    float most_p = 0.0f, most_w = 0.0f;
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n)
+    for (int h = 0; h < kParts; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        most_p = fmaxf(most_p, fmaxf(pr[n][e], pr[n][e + 1]));
-        most_w = fmaxf(most_w, fmaxf(wt[n][e], wt[n][e + 1]));
-      }
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          most_p = fmaxf(most_p, fmaxf(pr[h][n][e], pr[h][n][e + 1]));
+          most_w = fmaxf(most_w, fmaxf(wt[h][n][e], wt[h][n][e + 1]));
+        }
     // (p = inf times a scale of 0 is the NaN that fmax passes over: p shows it)
     if (__any_sync(0xffffffffu, most_w > kMostWeight || most_p > kMostP)) {  // move the references
-      const float lv0 = fmaxf(lg2(dv0), kLeastScale), lv1 = fmaxf(lg2(dv1), kLeastScale);
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float top = m[n][e];
-          if (!hidden || at + g < min(seen[n][e], s.end)) top = fmaxf(top, x[n][e] * (dk0 * f[n][e]) + lv0);
-          if (!hidden || at + g + 8 < min(seen[n][e], s.end)) top = fmaxf(top, x[n][e + 2] * (dk1 * f[n][e]) + lv1);
+#pragma unroll
+          for (int h = 0; h < kParts; ++h)
+#pragma unroll
+            for (int c = e; c < 4; c += 2)
+              if (!hidden || sees(h, n, c))
+                top = fmaxf(top, x[h][n][c] * (dk[h][c >> 1] * f[n][e]) + fmaxf(lg2(dv[h][c >> 1]), kLeastScale));
 #pragma unroll
           for (int h = 4; h < 32; h *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
           const float keep = ex2(m[n][e] - top);
@@ -387,29 +409,35 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         }
       against();
     }
-    uint32_t b0[kTiles], b1[kTiles];
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n) {
+    for (int h = 0; h < kParts; ++h) {
+      uint32_t b0[kTiles], b1[kTiles];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) l[n][e & 1] += pr[n][e];
-      const __half2 lo = __floats2half2_rn(wt[n][0], wt[n][1]), hi = __floats2half2_rn(wt[n][2], wt[n][3]);
-      b0[n] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
-      b1[n] = transpose8(*reinterpret_cast<const uint32_t*>(&hi));
-    }
+      for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
-    for (int w = 0; w < kValueWords; ++w)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {  // channels 4 h .. 4 h + 3 of the word, two tokens in each register
-        uint32_t v0 = __byte_perm(s.v[0][w], s.v[1][w], h ? 0x7632 : 0x5410), v1 = __byte_perm(s.v[2][w], s.v[3][w], h ? 0x7632 : 0x5410);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const uint32_t a0 = codes_04(v0), a1 = codes_15(v0), a2 = codes_04(v1), a3 = codes_15(v1);
-#pragma unroll
-          for (int n = 0; n < kTiles; ++n) mma16816(o[4 * w + 2 * h + c][n], a0, a1, a2, a3, b0[n], b1[n]);
-          v0 >>= 8;
-          v1 >>= 8;
-        }
+        for (int e = 0; e < 4; ++e) l[n][e & 1] += pr[h][n][e];
+        const __half2 lo = __floats2half2_rn(wt[h][n][0], wt[h][n][1]), hi = __floats2half2_rn(wt[h][n][2], wt[h][n][3]);
+        b0[n] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
+        b1[n] = transpose8(*reinterpret_cast<const uint32_t*>(&hi));
       }
+      uint32_t v[4][kValueWords];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) read_words(v[e], from + h * C::kPartBytes + v_get[e & 1] + (e >> 1) * 8 * kRow);
+#pragma unroll
+      for (int w = 0; w < kValueWords; ++w)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {  // channels 4 u .. 4 u + 3 of the word, two tokens in each register
+          uint32_t v0 = __byte_perm(v[0][w], v[1][w], u ? 0x7632 : 0x5410), v1 = __byte_perm(v[2][w], v[3][w], u ? 0x7632 : 0x5410);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const uint32_t a0 = codes_04(v0), a1 = codes_15(v0), a2 = codes_04(v1), a3 = codes_15(v1);
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma16816(o[4 * w + 2 * u + c][n], a0, a1, a2, a3, b0[n], b1[n]);
+            v0 >>= 8;
+            v1 >>= 8;
+          }
+        }
+    }
   };
   int slot = 0, fill = kStages - 1;
   for (int i = 0; i < steps; ++i) {
@@ -554,7 +582,7 @@ int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * 
 
 // The split over the keys: CTAs enough to fill the device several times over (sequences may be much shorter than max_len), of
 // at least 64 tokens, as far as the workspace has room for their results.
-constexpr int kLeastChunk = kStep * kWarps;
+constexpr int kLeastChunk = kTile * kWarps;
 constexpr int kCtasPerSm = 16;
 void plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p) {
   p->group = a.heads / a.pool.kv_heads;
