@@ -19,8 +19,10 @@
 //   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
 // float16.
 //
-// The keys of a sequence are split into chunks of equal length over CTAs, of kWarps warps with every kWarps-th 16 tokens; the
-// chunks' results are joined by a second kernel where a sequence has more than one.
+// The cached tokens of a sequence are split into chunks over CTAs (of kWarps warps, each with every kWarps-th step), and the
+// chunks' results joined by a second kernel where a sequence has more than one.  The device decides the chunks from the lengths it
+// finds, so that short and long sequences of one call share the SMs evenly and a captured graph follows its lengths; the
+// host only bounds their number.
 #include <cuda_runtime.h>
 
 #include <cfloat>
@@ -41,10 +43,14 @@ struct Kv4Params {
   Kv4AttentionArgs a;
   int group;         // query heads on a key/value head
   int rows;          // query rows of a CTA (8 or 16): (token, head of the group), tokens outer
-  int row_tiles;     // for max_q queries
-  int chunk, chunks; // cached tokens of a CTA; CTAs for max_len
-  float* part;       // [unit][chunks][rows][head_dim + 2]: sums over the values, then max s, sum p
+  int per;           // CTAs of a chunk: kv_heads x row tiles for max_q queries
+  int row_tiles;
+  int target;        // CTAs to aim for; 0: one chunk a sequence
+  int ctas;          // at most this many: target and a CTA for the remainder of every sequence
+  float* part;       // [ctas][rows][head_dim + 2]: sums over the values, then the reference and sum p
 };
+constexpr int kLeastChunk = kTile * kWarps;
+constexpr int kCtasPerSm8 = 8, kCtasPerSm16 = 2;  // to aim for, with row tiles of 8 and of 16
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -91,18 +97,38 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kBut) : "memory");
 }
 
-// One sequence as the launch's bounds admit it; false where it is to be skipped.
+// One sequence's first query row, queries and cached tokens.
 struct Sequence {
   int q0, n, len;
 };
-__device__ __forceinline__ bool load_sequence(const Kv4AttentionArgs& a, int b, Sequence& s) {
+__device__ __forceinline__ Sequence load_sequence(const Kv4AttentionArgs& a, int b) {
+  Sequence s;
   s.q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q);
   s.n = min(max(__ldg(a.cu_q + b + 1), s.q0), a.total_q) - s.q0;
   s.len = __ldg(a.kv_len + b);
-  return s.n <= a.max_q && s.len >= 0 && s.len <= a.max_len;
+  return s;
 }
+// False where it exceeds the launch's bounds and is to be skipped.
+__device__ __forceinline__ bool usable(const Kv4AttentionArgs& a, const Sequence& s) { return s.n <= a.max_q && s.len >= 0 && s.len <= a.max_len; }
 // Cached tokens that query token i sees.
 __device__ __forceinline__ int seen_by(const Sequence& s, int causal, int i) { return causal ? max(0, s.len - s.n + i + 1) : s.len; }
+
+// The split: every sequence gets one chunk for each started `length` tokens, of equal size.
+__device__ __forceinline__ int usable_length(const Kv4AttentionArgs& a, int len) { return min(max(len, 0), a.max_len); }
+__device__ __forceinline__ int chunks_of(int len, int64_t length) { return len <= length ? 1 : static_cast<int>((len + length - 1) / length); }
+__device__ __forceinline__ int chunk_size(int len, int chunks) {
+  return ((len + chunks - 1) / chunks + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
+}
+// The same in every CTA of both kernels; `len`: of sequence `lane` (0 where there is none), loaded already.
+__device__ __forceinline__ int64_t chunk_length(const Kv4Params& p, int len) {
+  if (p.target == 0) return int64_t{1} << 31;
+  int64_t all = len;
+  for (int b = 32 + static_cast<int>(threadIdx.x & 31); b < p.a.batch; b += 32) all += usable_length(p.a, __ldg(p.a.kv_len + b));
+#pragma unroll
+  for (int h = 1; h < 32; h *= 2) all += __shfl_xor_sync(0xffffffffu, all, h);
+  const int64_t length = (all * p.per + p.target - 1) / p.target;
+  return max(static_cast<int64_t>(kLeastChunk), (length + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
+}
 
 template <int kDim, int kTiles>
 struct Cfg {
@@ -116,7 +142,10 @@ struct Cfg {
   static constexpr int kPartBytes = kTile * (kDim + 8);    // key codes, value codes, key scales, value scales
   static constexpr int kStepBytes = kParts * kPartBytes;
   static constexpr int kRing = kWarps * kStages * kStepBytes;
-  static constexpr int kJoin = kWarps * kRows * kDim * 4;  // the warps' sums, over the ring at the end
+  // The warps' sums, over the ring at the end: an eighth of a row's channels (a lane's) every kEighth floats, rows kJoinRow
+  // apart, which spreads the fragments' stores over the banks.
+  static constexpr int kEighth = kDim / 8 + 2, kJoinRow = 8 * kEighth + 4;
+  static constexpr int kJoin = kWarps * kRows * kJoinRow * 4;
   static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kRows * kQStride * 2;
 };
 
@@ -131,29 +160,48 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   extern __shared__ __align__(128) uint8_t s_raw[];
   __half* const q_at = reinterpret_cast<__half*>(s_raw);                      // [kRows][kQStride]
   uint8_t* const s_ring = s_raw + kRows * C::kQStride * 2;                    // [kWarps][kStages][kStepBytes]
-  float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kDim] at the end
+  float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kJoinRow] at the end
   static_assert(kRows * C::kQStride * 2 % 128 == 0, "the ring's pieces are placed by 128-byte lines");
   __shared__ float s_f[kRows], s_sum[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
   __shared__ int s_end[kWarps][kStages][kParts];  // first token that nobody may use
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  int u = blockIdx.x;
-  const int ch = u % p.chunks;
-  const int unit = u /= p.chunks;
-  const int tile = u % p.row_tiles;
-  u /= p.row_tiles;
-  const int kvh = u % a.pool.kv_heads, b = u / a.pool.kv_heads;
   griddep_wait();  // the queries, lengths and the cache may come from the previous kernel, which may still read o
   griddep_launch_dependents();
-  Sequence seq;
-  if (!load_sequence(a, b, seq)) {
+  // this CTA's sequence b, chunk ch of it, key/value head and row tile
+  const int rest = static_cast<int>(blockIdx.x) % p.per, tile = rest % p.row_tiles, kvh = rest / p.row_tiles;
+  int ch = static_cast<int>(blockIdx.x) / p.per, b = -1, chunk = 0;
+  Sequence seq = {0, 0, 0};  // of sequence b0 + lane, then of b
+  if (lane < a.batch) seq = load_sequence(a, lane);
+  {
+    const int64_t length = chunk_length(p, usable_length(a, seq.len));
+    for (int b0 = 0; b0 < a.batch && b < 0; b0 += 32) {
+      if (b0 > 0 && b0 + lane < a.batch) seq = load_sequence(a, b0 + lane);
+      const int len = usable_length(a, seq.len), n = b0 + lane < a.batch ? chunks_of(len, length) : 0;
+      int upto = n;
+#pragma unroll
+      for (int h = 1; h < 32; h *= 2) {
+        const int o = __shfl_up_sync(0xffffffffu, upto, h);
+        if (lane >= h) upto += o;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, ch < upto);
+      const int from = hit ? __ffs(hit) - 1 : 31;
+      ch -= __shfl_sync(0xffffffffu, hit ? upto - n : upto, from);
+      if (hit == 0) continue;
+      b = b0 + from;
+      chunk = __shfl_sync(0xffffffffu, chunk_size(len, max(n, 1)), from);
+      seq = {__shfl_sync(0xffffffffu, seq.q0, from), __shfl_sync(0xffffffffu, seq.n, from), __shfl_sync(0xffffffffu, seq.len, from)};
+    }
+  }
+  if (b < 0) return;
+  if (!usable(a, seq)) {
     if (threadIdx.x == 0) report_index();
     return;
   }
   const int row0 = tile * kRows, rows = min(kRows, seq.n * p.group - row0);
   if (rows <= 0) return;
   const int most = seen_by(seq, a.causal, (row0 + rows - 1) / p.group);  // tokens that the last row sees
-  const int k0 = ch * p.chunk, k1 = min(most, k0 + p.chunk);
+  const int k0 = ch * chunk, k1 = min(most, k0 + chunk);
   if (ch > 0 && k0 >= most) return;
 
   // ---- the first cached tokens are asked for before the queries are worked on
@@ -463,15 +511,12 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         s_m[warp][r] = m[n][e];
         s_l[warp][r] = l[n][e];
       }
-      float* const dst = s_o + (warp * kRows + r) * kDim + g * (kDim / 8);
+      float* const dst = s_o + (warp * kRows + r) * C::kJoinRow + g * C::kEighth;
 #pragma unroll
-      for (int c = 0; c < kDim / 16; ++c) {
-        dst[2 * c] = o[c][n][e];
-        dst[2 * c + 1] = o[c][n][e + 2];
-      }
+      for (int c = 0; c < kDim / 16; ++c) *reinterpret_cast<float2*>(dst + 2 * c) = make_float2(o[c][n][e], o[c][n][e + 2]);
     }
   __syncthreads();
-  const bool whole = most <= p.chunk;
+  const bool whole = most <= chunk;
 #pragma unroll
   for (int r0 = 0; r0 < kRows; r0 += kTeams) {
     const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
@@ -483,16 +528,13 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
     for (int w = 0; w < kWarps; ++w) {
       const float k = ex2(s_m[w][rr] - top);
       sum += s_l[w][rr] * k;
-      const float4* src = reinterpret_cast<const float4*>(s_o + (w * kRows + rr) * kDim + tl * 8);
-      const float4 lo = src[0], hi = src[1];
-      y[0] += lo.x * k;
-      y[1] += lo.y * k;
-      y[2] += lo.z * k;
-      y[3] += lo.w * k;
-      y[4] += hi.x * k;
-      y[5] += hi.y * k;
-      y[6] += hi.z * k;
-      y[7] += hi.w * k;
+      const float* const src = s_o + (w * kRows + rr) * C::kJoinRow + tl * 8 / (kDim / 8) * C::kEighth + tl * 8 % (kDim / 8);
+#pragma unroll
+      for (int c = 0; c < 8; c += 2) {
+        const float2 v = *reinterpret_cast<const float2*>(src + c);
+        y[c] += v.x * k;
+        y[c + 1] += v.y * k;
+      }
     }
     if (whole) {
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -504,7 +546,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
       }
     } else if (r < rows) {
-      float* const dst = p.part + ((static_cast<size_t>(unit) * p.chunks + ch) * kRows + r) * (kDim + 2);
+      float* const dst = p.part + (static_cast<size_t>(blockIdx.x) * kRows + r) * (kDim + 2);
 #pragma unroll
       for (int c = 0; c < 8; c += 2) *reinterpret_cast<float2*>(dst + tl * 8 + c) = make_float2(y[c], y[c + 1]);
       if (tl == 0) *reinterpret_cast<float2*>(dst + kDim) = make_float2(top, sum);
@@ -523,16 +565,25 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
   const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam;
   griddep_wait();
   griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, len = lane < a.batch ? usable_length(a, __ldg(a.kv_len + lane)) : 0;
   int b, first;
-  Sequence seq;
-  if (!find_sequence(a.cu_q, a.batch, token, b, first) || !load_sequence(a, b, seq) || seq.q0 != first) return;
+  if (!find_sequence(a.cu_q, a.batch, token, b, first)) return;
+  const Sequence seq = load_sequence(a, b);
+  if (!usable(a, seq) || seq.q0 != first) return;
+  const int64_t length = chunk_length(p, len);
+  const int chunk = chunk_size(seq.len, chunks_of(seq.len, length));
   const int kvh = head / p.group, r = (token - first) * p.group + head % p.group, tile = r / p.rows;
   const int most = seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group);
-  const int chunks = (most + p.chunk - 1) / p.chunk;
+  const int chunks = (most + chunk - 1) / max(chunk, 1);
   if (chunks < 2) return;  // its CTA has written the result
-  const size_t unit = (static_cast<size_t>(b) * a.pool.kv_heads + kvh) * p.row_tiles + tile;
-  const float* const src = p.part + (unit * p.chunks * p.rows + r % p.rows) * (kDim + 2);
-  const size_t next = static_cast<size_t>(p.rows) * (kDim + 2);
+  int before = 0;  // chunks of the sequences ahead
+  for (int b0 = 0; b0 < b; b0 += 32) {
+    const int at = b0 + lane;
+    before += __reduce_add_sync(0xffffffffu, at < b ? chunks_of(b0 == 0 ? len : usable_length(a, __ldg(a.kv_len + at)), length) : 0);
+  }
+  const size_t unit = static_cast<size_t>(before) * p.per + kvh * p.row_tiles + tile;
+  const float* const src = p.part + (unit * p.rows + r % p.rows) * (kDim + 2);
+  const size_t next = static_cast<size_t>(p.per) * p.rows * (kDim + 2);
   float m = -FLT_MAX, l = 0.0f, y[8] = {};
 #pragma unroll 4
   for (int c = team; c < chunks; c += kTeams) {
@@ -580,40 +631,35 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
 
 int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * (a.heads / a.pool.kv_heads) <= 8 ? 8 : 16; }
 
-// The split over the keys: CTAs enough to fill the device several times over (sequences may be much shorter than max_len), of
-// at least 64 tokens, as far as the workspace has room for their results.
-constexpr int kLeastChunk = kTile * kWarps;
-constexpr int kCtasPerSm = 16;
-void plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p) {
+// CTAs to aim for: the SMs filled once with row tiles of 16 (whose CTAs are long), several times with single tokens, as far as
+// the workspace has room for their results.
+cudaError_t plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p) {
   p->group = a.heads / a.pool.kv_heads;
   p->rows = rows_of(a);
-  p->row_tiles = static_cast<int>((static_cast<int64_t>(a.max_q) * p->group + p->rows - 1) / p->rows);
-  const int64_t units = static_cast<int64_t>(a.batch) * a.pool.kv_heads * p->row_tiles;
-  const int64_t target = static_cast<int64_t>(a.num_sms) * kCtasPerSm;
+  const int64_t tiles = (static_cast<int64_t>(a.max_q) * p->group + p->rows - 1) / p->rows;
+  const int64_t units = static_cast<int64_t>(a.batch) * a.pool.kv_heads * tiles;
+  if (units > 0x3fffffff) return cudaErrorInvalidConfiguration;
+  p->row_tiles = static_cast<int>(tiles);
+  p->per = static_cast<int>(a.pool.kv_heads * tiles);
+  int64_t target = static_cast<int64_t>(a.num_sms) * (p->rows == 8 ? kCtasPerSm8 : kCtasPerSm16);
   const int64_t part = static_cast<int64_t>(p->rows) * (a.pool.head_dim + 2) * 4;
-  const int64_t room = static_cast<int64_t>(ws_bytes) / (units * part);
-  const int64_t most = (static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk;
-  int64_t chunks = target / units;
-  if (chunks > room) chunks = room;
-  if (chunks > most) chunks = most;
-  if (chunks < 1) chunks = 1;
-  int64_t len = (a.max_len + chunks - 1) / chunks;
-  len = (len + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
-  if (len < kLeastChunk) len = kLeastChunk;
-  p->chunk = static_cast<int>(len > 0x7fffffff - kLeastChunk ? 0x7fffffff - kLeastChunk : len);
-  p->chunks = static_cast<int>((a.max_len + len - 1) / len);
-  if (p->chunks < 1) p->chunks = 1;
+  const int64_t most = units * ((static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk);  // with the least chunks
+  const int64_t room = static_cast<int64_t>(ws_bytes / part);
+  if (target > room - units) target = room - units;
+  if (target < units || most <= units) target = 0;  // (no more than a chunk a sequence)
+  p->target = static_cast<int>(target);
+  p->ctas = static_cast<int>(target == 0 ? units : target + units < most ? target + units : most);
+  return cudaSuccess;
 }
 
 template <typename T, int kDim, int kTiles>
 cudaError_t launch(const Kv4AttentionArgs& a) {
   Kv4Params p;
   p.a = a;
-  plan_split(a, a.ws ? a.ws_bytes : 0, &p);
+  if (cudaError_t e = plan_split(a, a.ws ? a.ws_bytes : 0, &p)) return e;
   p.part = static_cast<float*>(a.ws);
-  const int64_t ctas = static_cast<int64_t>(a.batch) * a.pool.kv_heads * p.row_tiles * p.chunks;
   const int64_t joins = static_cast<int64_t>(a.total_q) * a.heads;
-  if (ctas > 0x7fffffff || joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  if (joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
   using C = Cfg<kDim, kTiles>;
   auto kern = attention_kv4_kernel<T, kDim, kTiles>;
   if (C::kSmem > 48 * 1024) {
@@ -621,7 +667,7 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.gridDim = dim3(static_cast<unsigned>(p.ctas));
   cfg.blockDim = dim3(32 * kWarps);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = a.stream;
@@ -632,7 +678,7 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
   cfg.numAttrs = 1;
   cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
   if (e != cudaSuccess) return e;
-  if (p.chunks > 1) {
+  if (p.target > 0) {
     cfg.gridDim = dim3(static_cast<unsigned>(joins));
     cfg.dynamicSmemBytes = 0;
     e = cudaLaunchKernelEx(&cfg, attention_kv4_join_kernel<T, kDim>, p);
@@ -650,9 +696,8 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
 
 size_t attention_kv4_workspace(const Kv4AttentionArgs& a) {
   Kv4Params p;
-  plan_split(a, ~static_cast<size_t>(0) >> 1, &p);
-  if (p.chunks < 2) return 0;
-  const size_t n = static_cast<size_t>(a.batch) * a.pool.kv_heads * p.row_tiles * p.chunks * p.rows * (a.pool.head_dim + 2) * 4;
+  if (plan_split(a, ~static_cast<size_t>(0) >> 1, &p) != cudaSuccess || p.target == 0) return 0;
+  const size_t n = static_cast<size_t>(p.ctas) * p.rows * (a.pool.head_dim + 2) * 4;
   return (n + 255) & ~static_cast<size_t>(255);
 }
 
