@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
 
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bar_q[2], bar_kfull[kStages], bar_kempty[kStages], bar_vfull[kStages], bar_vok[kStages],
-      bar_vempty[kStages], bar_s[2], bar_p[2], bar_o[2], bar_done;
+      bar_vempty[kStages], bar_s[2], bar_p[2][2], bar_o[2], bar_done;
   __shared__ uint32_t s_tmem;
   __shared__ int s_found, s_bad;
   __shared__ Work s_work;
@@ -129,7 +129,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bar_q[i]), 1);
       mbar_init(smem_u32(&bar_s[i]), 1);
-      mbar_init(smem_u32(&bar_p[i]), 4);
+      mbar_init(smem_u32(&bar_p[i][0]), 4);
+      mbar_init(smem_u32(&bar_p[i][1]), 4);
       mbar_init(smem_u32(&bar_o[i]), 1);
     }
     for (int i = 0; i < kStages; ++i) {
@@ -279,18 +280,22 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         }
         __syncwarp();
       };
-      // O of tile t += P (buffer b) V (stage s)
-      auto values = [&](int t, int b, int s, bool first) {
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t d = tmem + static_cast<uint32_t>(C::kOCol + t * kDim), a = tmem + static_cast<uint32_t>(b * kBlock);
+      // O of tile t += P (buffer b, for the n-th time) V (stage s), in halves as P comes
+      auto values = [&](int t, int b, int n, int s, bool first) {
 #pragma unroll
-          for (int i = 0; i < kBlock / 16; ++i)
-            mma_f16_ts(d, a + static_cast<uint32_t>(i * 8), smem_desc_sw128_mn(smem_u32(smem_v + s * C::kKvBytes) + i * 2048, kKvBox), idesc_o,
-                       !(first && i == 0));
-          mma_commit(smem_u32(&bar_o[t]));
+        for (int half = 0; half < 2; ++half) {
+          if (!wait(&bar_p[b][half], n)) return;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t d = tmem + static_cast<uint32_t>(C::kOCol + t * kDim), a = tmem + static_cast<uint32_t>(b * kBlock);
+#pragma unroll
+            for (int i = half * kBlock / 32; i < (half + 1) * kBlock / 32; ++i)
+              mma_f16_ts(d, a + static_cast<uint32_t>(i * 8), smem_desc_sw128_mn(smem_u32(smem_v + s * C::kKvBytes) + i * 2048, kKvBox), idesc_o,
+                         !(first && i == 0));
+            if (half == 1) mma_commit(smem_u32(&bar_o[t]));
+          }
+          __syncwarp();
         }
-        __syncwarp();
       };
       auto release = [&](uint64_t* bar) {  // free once every product issued so far is done
         if (elect_one()) mma_commit(smem_u32(bar));
@@ -307,9 +312,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           if (!wait(&bar_vok[s], j / kStages)) break;
           if (j + 1 < most && !wait(&bar_kfull[s1], (j + 1) / kStages)) break;
           for (int t = 0; t < 2 && ok; ++t) {
-            if (j >= blocks[t] || !wait(&bar_p[t], j)) continue;
-            values(t, t, s, j == 0);
-            if (j + 1 < blocks[t]) scores(t, t, s1);  // over P, which the product before it has read
+            if (j >= blocks[t]) continue;
+            values(t, t, j, s, j == 0);
+            if (ok && j + 1 < blocks[t]) scores(t, t, s1);  // over P, which the product before it has read
           }
           if (!ok) break;
           release(&bar_vempty[s]);
@@ -327,9 +332,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
             scores(0, (j + 1) & 1, s1);
             release(&bar_kempty[s1]);
           }
-          if (!wait(&bar_vok[s], j / kStages) || !wait(&bar_p[j & 1], j >> 1)) break;
-          values(0, j & 1, s, j == 0);
-          release(&bar_vempty[s]);
+          if (!wait(&bar_vok[s], j / kStages)) break;
+          values(0, j & 1, j >> 1, s, j == 0);
+          if (ok) release(&bar_vempty[s]);
         }
       }
       if (elect_one()) {
@@ -423,24 +428,28 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           }
         }
         const float ref = m == -INFINITY ? 0.0f : m;  // (a row that has seen nothing yet)
-        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float2 scale2 = make_float2(p.c, p.c), ref2 = make_float2(-ref, -ref);
+        float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
         for (int i = 0; i < kBlock / 32; ++i) {
           uint32_t y[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float a = ex2(fmaf(__uint_as_float(x[i][e]), p.c, -ref)), d = ex2(fmaf(__uint_as_float(x[i][e + 1]), p.c, -ref));
-            part[e & 2] += a;
-            part[(e & 2) + 1] += d;
-            y[e / 2] = pack2<T>(a, d);
+            const float2 d = fma2(make_float2(__uint_as_float(x[i][e]), __uint_as_float(x[i][e + 1])), scale2, ref2);
+            const float2 v = make_float2(ex2(d.x), ex2(d.y));
+            part[e / 2 & 1] = add2(part[e / 2 & 1], v);
+            y[e / 2] = pack2<T>(v.x, v.y);
           }
           tmem_st16(s_at + i * 16, y);
+          if (i % (kBlock / 64) == kBlock / 64 - 1) {  // half of the block
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_p[b][i / (kBlock / 64)]));
+          }
         }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&bar_p[b]));
+        part[0] = add2(part[0], part[1]);
+        sum += part[0].x + part[0].y;
       }
       if (ok && n > 0) {
         // with one tile the last two products may both be outstanding (the last S was made ahead of the first of them), and a

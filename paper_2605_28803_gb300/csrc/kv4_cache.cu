@@ -26,25 +26,6 @@ constexpr int kWarpsPerSm = 32;   // below this many warps an SM, a warp takes f
 template <int kTeam>
 constexpr float kNorm = kTeam == 2 ? 0.125f : kTeam == 4 ? 0.08838834764831845f : 0.0625f;  // float32(1 / sqrt(32 kTeam))
 
-// Two float32 operations an instruction, each rounded like the single one.
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
-  return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(reinterpret_cast<uint64_t&>(r))
-      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)), "l"(reinterpret_cast<const uint64_t&>(c)));
-  return r;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
-  return r;
-}
-
 // q . H for codes (or sums of them) spread over kTeam lanes as above: v[k] holds channels 0 and 4, 1 and 5, 2 and 6, 3 and 7 of
 // group k's eight.  Every sum is exact.
 template <int kTeam>
