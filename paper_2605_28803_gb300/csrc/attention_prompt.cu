@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         for (int j = 0; j < most; ++j) {
           const int s = j % kStages;
           const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
-          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_kempty[s]), ph ^ 1u))) break;
+          if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_kempty[s]), ph ^ 1u))) break;
           if (elect_one()) {
             const uint32_t bar = smem_u32(&bar_kfull[s]);
             mbar_arrive_expect_tx(bar, C::kKvBytes);
@@ -232,8 +232,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
               tma_load_3d(smem_u32(smem_k + s * C::kKvBytes + c * kKvBox), &tmap_k, c * 64, w.kvh, w.k0 + j * kBlock, bar);
           }
           __syncwarp();
-          if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_vempty[s]), ph ^ 1u))) {
-            mbar_wait(smem_u32(&bar_kfull[s]), ph);
+          if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_vempty[s]), ph ^ 1u))) {
+            mbar_wait_short(smem_u32(&bar_kfull[s]), ph);
             break;
           }
           if (elect_one()) {
@@ -247,11 +247,11 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         }
         // before leaving, let every load land
         for (int t = 0; t < kTiles; ++t)
-          if (blocks[t] > 0) mbar_wait(smem_u32(&bar_q[t]), 0);
+          if (blocks[t] > 0) mbar_wait_short(smem_u32(&bar_q[t]), 0);
         for (int j = max(0, issued - kStages); j < issued; ++j) {
           const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
-          mbar_wait(smem_u32(&bar_kfull[j % kStages]), ph);
-          mbar_wait(smem_u32(&bar_vfull[j % kStages]), ph);
+          mbar_wait_short(smem_u32(&bar_kfull[j % kStages]), ph);
+          mbar_wait_short(smem_u32(&bar_vfull[j % kStages]), ph);
         }
       }
       __syncwarp();
@@ -260,9 +260,12 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       if constexpr (kTiles == 2) setmaxnreg_dec<64>();
       constexpr uint32_t idesc_s = idesc_f16_f32(kBf16, kRowsPerTile, kBlock, 0);
       constexpr uint32_t idesc_o = idesc_f16_f32(kBf16, kRowsPerTile, kDim, 1);
+      const uint32_t k_hi = static_cast<uint32_t>(smem_desc_sw128(0) >> 32), v_hi = static_cast<uint32_t>(smem_desc_sw128_mn(0, kKvBox) >> 32);
+      const uint32_t q_lo = static_cast<uint32_t>(smem_desc_sw128(smem_u32(smem))), k_lo = static_cast<uint32_t>(smem_desc_sw128(smem_u32(smem_k))),
+                     v_lo = static_cast<uint32_t>(smem_desc_sw128_mn(smem_u32(smem_v), kKvBox));  // addresses in units of 16 bytes
       bool ok = true;
       auto wait = [&](uint64_t* bar, int n) {  // completion n of a barrier
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), static_cast<uint32_t>(n) & 1u));
+        ok = ok && __all_sync(0xffffffffu, mbar_wait_short(smem_u32(bar), static_cast<uint32_t>(n) & 1u));
         return ok;
       };
       // S of tile t (buffer b) from K's stage s
@@ -270,12 +273,10 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         tc_fence_after();
         if (elect_one()) {
           const uint32_t d = tmem + static_cast<uint32_t>(b * kBlock);
+          const uint32_t k = k_lo + static_cast<uint32_t>(s * (C::kKvBytes / 16)), q = q_lo + static_cast<uint32_t>(t * (C::kQBytes / 16));
 #pragma unroll
-          for (int i = 0; i < kDim / 16; ++i) {
-            const uint32_t at = (i / 4) * kQBox + (i % 4) * 32, bt = (i / 4) * kKvBox + (i % 4) * 32;
-            mma_f16_ss(d, smem_desc_sw128(smem_u32(smem + t * C::kQBytes) + at), smem_desc_sw128(smem_u32(smem_k + s * C::kKvBytes) + bt),
-                       idesc_s, i != 0);
-          }
+          for (int i = 0; i < kDim / 16; ++i)
+            mma_f16_ss(d, q + (i / 4) * (kQBox / 16) + (i % 4) * 2, k_hi, k + (i / 4) * (kKvBox / 16) + (i % 4) * 2, k_hi, idesc_s, i != 0);
           mma_commit(smem_u32(&bar_s[b]));
         }
         __syncwarp();
@@ -288,10 +289,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           tc_fence_after();
           if (elect_one()) {
             const uint32_t d = tmem + static_cast<uint32_t>(C::kOCol + t * kDim), a = tmem + static_cast<uint32_t>(b * kBlock);
+            const uint32_t v = v_lo + static_cast<uint32_t>(s * (C::kKvBytes / 16));
 #pragma unroll
-            for (int i = half * kBlock / 32; i < (half + 1) * kBlock / 32; ++i)
-              mma_f16_ts(d, a + static_cast<uint32_t>(i * 8), smem_desc_sw128_mn(smem_u32(smem_v + s * C::kKvBytes) + i * 2048, kKvBox), idesc_o,
-                         !(first && i == 0));
+            for (int i = half * kBlock / 32; i < (half + 1) * kBlock / 32; ++i) mma_f16_ts(d, a + i * 8, v + i * 128, v_hi, idesc_o, !(first && i == 0));
             if (half == 1) mma_commit(smem_u32(&bar_o[t]));
           }
           __syncwarp();
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       }
       if (elect_one()) {
         mma_commit(smem_u32(&bar_done));  // every product issued above has completed once this flips
-        mbar_wait(smem_u32(&bar_done), 0);
+        mbar_wait_short(smem_u32(&bar_done), 0);
       }
       __syncwarp();
     } else if (warp < kWarpSoftmax) {
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       for (int j = 0; j < most; ++j) {
         const int s = j % kStages;
         const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_vfull[s]), ph))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_vfull[s]), ph))) break;
         const int inside = min(kBlock, w.keys - j * kBlock);  // rows of the sequence; the rest is its neighbour's
         const bool look = p.causal && j >= guard_from;
         if (look || inside < kBlock) {
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       bool ok = true;
       for (int j = 0; j < n; ++j) {
         const int b = kTiles == 2 ? t : j & 1, visit = kTiles == 2 ? j : j >> 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s[b]), static_cast<uint32_t>(visit) & 1u))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_s[b]), static_cast<uint32_t>(visit) & 1u))) { ok = false; break; }
         tc_fence_after();
         const uint32_t s_at = tmem + lanes + static_cast<uint32_t>(b * kBlock);
         uint32_t x[kBlock / 32][32];
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           sum *= keep;
           if (j > 0) {
             // the product of block j - 1 has to be in O (with two tiles S's completion shows that already)
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_o[t]), static_cast<uint32_t>(j - 1) & 1u))) { ok = false; break; }
+            if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_o[t]), static_cast<uint32_t>(j - 1) & 1u))) { ok = false; break; }
             tc_fence_after();
 #pragma unroll 1
             for (int i = 0; i < kDim / 32; ++i) {
@@ -454,8 +454,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       if (ok && n > 0) {
         // with one tile the last two products may both be outstanding (the last S was made ahead of the first of them), and a
         // barrier's phases are waited for one by one
-        if (kTiles == 1 && n > 1) mbar_wait(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 2) & 1u);
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 1) & 1u));
+        if (kTiles == 1 && n > 1) mbar_wait_short(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 2) & 1u);
+        ok = __all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 1) & 1u));
         tc_fence_after();
       }
       if (ok) {
