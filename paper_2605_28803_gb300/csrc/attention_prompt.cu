@@ -188,8 +188,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   griddep_launch_dependents();
-  const uint32_t tmem = s_tmem;
-  if (s_found) {
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);  // (values that the compiler knows to be the same in every lane)
+  if (__shfl_sync(0xffffffffu, s_found, 0)) {
     const Work w = s_work;
     // per tile: blocks to run, and the first of them that some row does not see whole
     int blocks[kTiles], partial[kTiles], most = 0, guard_from = 1 << 30;
@@ -198,6 +198,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       const int first = w.token + t * p.tokens, last = min(first + p.tokens, w.n) - 1;
       blocks[t] = first < w.n ? (seen_by(w, p.causal, last) + kBlock - 1) / kBlock : 0;
       partial[t] = seen_by(w, p.causal, first) / kBlock;
+      blocks[t] = __shfl_sync(0xffffffffu, blocks[t], 0);
       most = max(most, blocks[t]);
       if (blocks[t] > 0) guard_from = min(guard_from, partial[t]);
     }
