@@ -41,20 +41,23 @@ template <int kDim>
 struct Shape {
   static constexpr int kTiles = kDim == 256 ? 1 : 2;
   static constexpr int kBlock = kDim == 256 ? 64 : 128;
-  static constexpr int kStages = kDim == 64 ? 4 : 2;          // of K, and of V
+  // Stages: a load takes about 2000 cycles from the release of its stage, as long as a block's products, and V passes the guard too.
+  static constexpr int kStagesK = kDim == 64 ? 4 : kDim == 128 ? 2 : 3, kStagesV = kDim == 64 ? 4 : kDim == 128 ? 3 : 4;
+  static constexpr bool kQTmem = kDim == 256;                 // Q in TMEM beside S and O (there is room with one tile only)
   static constexpr int kThreads = 32 * (kWarpSoftmax + 4 * kTiles);
-  static constexpr int kQBytes = kRowsPerTile * kDim * 2;     // one tile
+  static constexpr int kQBytes = kQTmem ? 0 : kRowsPerTile * kDim * 2;  // one tile in shared memory
   static constexpr int kKvBytes = kBlock * kDim * 2;          // one block of K or V
-  static constexpr int kSmem = kTiles * kQBytes + 2 * kStages * kKvBytes + 1024;
-  static constexpr int kOCol = kDim == 256 ? 256 : 2 * kBlock;  // TMEM: two S buffers, then O of each tile
+  static constexpr int kSmem = kTiles * kQBytes + (kStagesK + kStagesV) * kKvBytes + 1024;
+  static constexpr int kOCol = 2 * kBlock, kQCol = kOCol + kTiles * kDim;  // TMEM: two S buffers, O of each tile, Q
 };
 
 struct PromptParams {
   const int32_t* cu_q;
   const int32_t* cu_k;
   void* o;
+  const void* q;
   const void* v;
-  int64_t v_stride;
+  int64_t q_stride, v_stride;
   int batch, total_q, total_k;
   int heads, kv_heads, group;  // group: query heads on a key/value head
   int chunk_heads, chunks;     // of them in one tile; tiles' head chunks
@@ -108,34 +111,36 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
     attention_prompt_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                             const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ PromptParams p) {
   using C = Shape<kDim>;
-  constexpr int kTiles = C::kTiles, kBlock = C::kBlock, kStages = C::kStages;
+  constexpr int kTiles = C::kTiles, kBlock = C::kBlock, kStagesK = C::kStagesK, kStagesV = C::kStagesV;
   constexpr int kBoxes = kDim / 64;            // 64-channel boxes of a row
   constexpr int kQBox = kRowsPerTile * 128, kKvBox = kBlock * 128;
   constexpr int kBf16 = std::is_same<T, __half>::value ? 0 : 1;
 
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q[2], bar_kfull[kStages], bar_kempty[kStages], bar_vfull[kStages], bar_vok[kStages],
-      bar_vempty[kStages], bar_s[2], bar_p[2][2], bar_o[2], bar_done;
+  __shared__ __align__(8) uint64_t bar_q[2], bar_kfull[kStagesK], bar_kempty[kStagesK], bar_vfull[kStagesV],
+      bar_vok[kStagesV], bar_vempty[kStagesV], bar_s[2], bar_p[2][2], bar_o[2], bar_done;
   __shared__ uint32_t s_tmem;
   __shared__ int s_found, s_bad;
   __shared__ Work s_work;
   uint8_t* const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* const smem_k = smem + kTiles * C::kQBytes;
-  uint8_t* const smem_v = smem_k + kStages * C::kKvBytes;
+  uint8_t* const smem_v = smem_k + kStagesK * C::kKvBytes;
 
   const int warp = warp_index(), lane = threadIdx.x & 31;
   if (warp == kWarpMma) tmem_alloc<512>(smem_u32(&s_tmem));
   if (threadIdx.x == 32 * kWarpGuard) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&bar_q[i]), 1);
+      mbar_init(smem_u32(&bar_q[i]), C::kQTmem ? 4 : 1);
       mbar_init(smem_u32(&bar_s[i]), 1);
       mbar_init(smem_u32(&bar_p[i][0]), 4);
       mbar_init(smem_u32(&bar_p[i][1]), 4);
       mbar_init(smem_u32(&bar_o[i]), 1);
     }
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < kStagesK; ++i) {
       mbar_init(smem_u32(&bar_kfull[i]), 1);
       mbar_init(smem_u32(&bar_kempty[i]), 1);
+    }
+    for (int i = 0; i < kStagesV; ++i) {
       mbar_init(smem_u32(&bar_vfull[i]), 1);
       mbar_init(smem_u32(&bar_vok[i]), kGuardWarps);
       mbar_init(smem_u32(&bar_vempty[i]), 1);
@@ -207,14 +212,13 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       // ------------------------------------------------------------------ TMA
       if constexpr (kTiles == 2) setmaxnreg_dec<64>();
       bool ok = *const_cast<volatile int*>(&g_debug_hold_loads) == 0;
-      int issued = 0;
       if (ok && most > 0) {
         if (elect_one()) {
           tma_prefetch_desc(&tmap_k);
           tma_prefetch_desc(&tmap_v);
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
-            if (blocks[t] == 0) continue;
+            if (C::kQTmem || blocks[t] == 0) continue;
             const uint32_t bar = smem_u32(&bar_q[t]);
             mbar_arrive_expect_tx(bar, static_cast<uint32_t>(p.chunk_heads * p.tokens * kDim * 2));
             for (int c = 0; c < kBoxes; ++c)
@@ -222,38 +226,28 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           }
         }
         __syncwarp();
+        auto fetch = [&](const CUtensorMap* map, uint8_t* stage, uint64_t* empty, uint64_t* full, int j, int stages) {
+          if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(empty), (static_cast<uint32_t>(j / stages) & 1u) ^ 1u))) return false;
+          if (elect_one()) {
+            mbar_arrive_expect_tx(smem_u32(full), C::kKvBytes);
+            for (int c = 0; c < kBoxes; ++c) tma_load_3d(smem_u32(stage + c * kKvBox), map, c * 64, w.kvh, w.k0 + j * kBlock, smem_u32(full));
+          }
+          __syncwarp();
+          return true;
+        };
+        int ks = 0, vs = 0;  // blocks of K and of V asked for
         for (int j = 0; j < most; ++j) {
-          const int s = j % kStages;
-          const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
-          if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_kempty[s]), ph ^ 1u))) break;
-          if (elect_one()) {
-            const uint32_t bar = smem_u32(&bar_kfull[s]);
-            mbar_arrive_expect_tx(bar, C::kKvBytes);
-            for (int c = 0; c < kBoxes; ++c)
-              tma_load_3d(smem_u32(smem_k + s * C::kKvBytes + c * kKvBox), &tmap_k, c * 64, w.kvh, w.k0 + j * kBlock, bar);
-          }
-          __syncwarp();
-          if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_vempty[s]), ph ^ 1u))) {
-            mbar_wait_short(smem_u32(&bar_kfull[s]), ph);
-            break;
-          }
-          if (elect_one()) {
-            const uint32_t bar = smem_u32(&bar_vfull[s]);
-            mbar_arrive_expect_tx(bar, C::kKvBytes);
-            for (int c = 0; c < kBoxes; ++c)
-              tma_load_3d(smem_u32(smem_v + s * C::kKvBytes + c * kKvBox), &tmap_v, c * 64, w.kvh, w.k0 + j * kBlock, bar);
-          }
-          __syncwarp();
-          issued = j + 1;
+          const int k = j % kStagesK, v = j % kStagesV;
+          if (!fetch(&tmap_k, smem_k + k * C::kKvBytes, &bar_kempty[k], &bar_kfull[k], j, kStagesK)) break;
+          ks = j + 1;
+          if (!fetch(&tmap_v, smem_v + v * C::kKvBytes, &bar_vempty[v], &bar_vfull[v], j, kStagesV)) break;
+          vs = j + 1;
         }
         // before leaving, let every load land
         for (int t = 0; t < kTiles; ++t)
-          if (blocks[t] > 0) mbar_wait_short(smem_u32(&bar_q[t]), 0);
-        for (int j = max(0, issued - kStages); j < issued; ++j) {
-          const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
-          mbar_wait_short(smem_u32(&bar_kfull[j % kStages]), ph);
-          mbar_wait_short(smem_u32(&bar_vfull[j % kStages]), ph);
-        }
+          if (!C::kQTmem && blocks[t] > 0) mbar_wait_short(smem_u32(&bar_q[t]), 0);
+        for (int j = max(0, ks - kStagesK); j < ks; ++j) mbar_wait_short(smem_u32(&bar_kfull[j % kStagesK]), static_cast<uint32_t>(j / kStagesK) & 1u);
+        for (int j = max(0, vs - kStagesV); j < vs; ++j) mbar_wait_short(smem_u32(&bar_vfull[j % kStagesV]), static_cast<uint32_t>(j / kStagesV) & 1u);
       }
       __syncwarp();
     } else if (warp == kWarpMma) {
@@ -275,9 +269,16 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         if (elect_one()) {
           const uint32_t d = tmem + static_cast<uint32_t>(b * kBlock);
           const uint32_t k = k_lo + static_cast<uint32_t>(s * (C::kKvBytes / 16)), q = q_lo + static_cast<uint32_t>(t * (C::kQBytes / 16));
+          const uint32_t qt = tmem + static_cast<uint32_t>(C::kQCol);
 #pragma unroll
-          for (int i = 0; i < kDim / 16; ++i)
-            mma_f16_ss(d, q + (i / 4) * (kQBox / 16) + (i % 4) * 2, k_hi, k + (i / 4) * (kKvBox / 16) + (i % 4) * 2, k_hi, idesc_s, i != 0);
+          for (int i = 0; i < kDim / 16; ++i) {
+            const uint32_t kk = k + (i / 4) * (kKvBox / 16) + (i % 4) * 2;
+            if constexpr (C::kQTmem) {
+              mma_f16_ts(d, qt + i * 8, kk, k_hi, idesc_s, i != 0);
+            } else {
+              mma_f16_ss(d, q + (i / 4) * (kQBox / 16) + (i % 4) * 2, k_hi, kk, k_hi, idesc_s, i != 0);
+            }
+          }
           mma_commit(smem_u32(&bar_s[b]));
         }
         __syncwarp();
@@ -309,17 +310,16 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           if (ok) release(&bar_kempty[0]);
         }
         for (int j = 0; j < most && ok; ++j) {
-          const int s = j % kStages, s1 = (j + 1) % kStages;
-          if (!wait(&bar_vok[s], j / kStages)) break;
-          if (j + 1 < most && !wait(&bar_kfull[s1], (j + 1) / kStages)) break;
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (j >= blocks[t]) continue;
-            values(t, t, j, s, j == 0);
+          const int s = j % kStagesV, s1 = (j + 1) % kStagesK;
+          if (!wait(&bar_vok[s], j / kStagesV)) break;
+          if (j + 1 < most && !wait(&bar_kfull[s1], (j + 1) / kStagesK)) break;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (ok && j < blocks[t]) values(t, t, j, s, j == 0);
+            if (t == 1 && ok) release(&bar_vempty[s]);
             if (ok && j + 1 < blocks[t]) scores(t, t, s1);  // over P, which the product before it has read
           }
-          if (!ok) break;
-          release(&bar_vempty[s]);
-          if (j + 1 < most) release(&bar_kempty[s1]);
+          if (ok && j + 1 < most) release(&bar_kempty[s1]);
         }
       } else {
         if (most > 0 && wait(&bar_kfull[0], 0) && wait(&bar_q[0], 0)) {
@@ -327,13 +327,13 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           release(&bar_kempty[0]);
         }
         for (int j = 0; j < most && ok; ++j) {
-          const int s = j % kStages, s1 = (j + 1) % kStages;
+          const int s = j % kStagesV, s1 = (j + 1) % kStagesK;
           if (j + 1 < most) {  // the next S, over the P that the product before last has read
-            if (!wait(&bar_kfull[s1], (j + 1) / kStages)) break;
+            if (!wait(&bar_kfull[s1], (j + 1) / kStagesK)) break;
             scores(0, (j + 1) & 1, s1);
             release(&bar_kempty[s1]);
           }
-          if (!wait(&bar_vok[s], j / kStages)) break;
+          if (!wait(&bar_vok[s], j / kStagesV)) break;
           values(0, j & 1, j >> 1, s, j == 0);
           if (ok) release(&bar_vempty[s]);
         }
@@ -347,9 +347,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       // ------------------------------------------------------------------ the guard of V
       if constexpr (kTiles == 2) setmaxnreg_dec<64>();
       for (int j = 0; j < most; ++j) {
-        const int s = j % kStages;
-        const uint32_t ph = static_cast<uint32_t>(j / kStages) & 1u;
-        if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_vfull[s]), ph))) break;
+        const int s = j % kStagesV;
+        if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_vfull[s]), static_cast<uint32_t>(j / kStagesV) & 1u))) break;
         const int inside = min(kBlock, w.keys - j * kBlock);  // rows of the sequence; the rest is its neighbour's
         const bool look = p.causal && j >= guard_from;
         if (look || inside < kBlock) {
@@ -386,6 +385,26 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       const int seen = live ? seen_by(w, p.causal, token) : w.keys;
       const int n = blocks[t], from = partial[t];
       const uint32_t o_at = tmem + lanes + static_cast<uint32_t>(C::kOCol + t * kDim);
+      if (C::kQTmem && n > 0) {  // this row of Q, two channels a column
+        const T* const src = static_cast<const T*>(p.q) + (w.q0 + token) * p.q_stride + (w.head + head) * kDim;
+#pragma unroll 2
+        for (int i = 0; i < kDim / 32; ++i) {
+          uint32_t y[16];
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(src + i * 32 + e * 2)) : make_uint4(0, 0, 0, 0);
+            y[e] = v.x;
+            y[e + 1] = v.y;
+            y[e + 2] = v.z;
+            y[e + 3] = v.w;
+          }
+          tmem_st16(tmem + lanes + static_cast<uint32_t>(C::kQCol + i * 16), y);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bar_q[0]));
+      }
       float m = -INFINITY, sum = 0.0f;
       bool ok = true;
       for (int j = 0; j < n; ++j) {
@@ -556,7 +575,9 @@ cudaError_t launch(const PromptArgs& a) {
   p.cu_q = a.cu_q;
   p.cu_k = a.cu_k;
   p.o = a.o;
+  p.q = a.q;
   p.v = a.v;
+  p.q_stride = a.q_stride;
   p.v_stride = a.v_stride;
   p.batch = a.batch;
   p.total_q = a.total_q;
