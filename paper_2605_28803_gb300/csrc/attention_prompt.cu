@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
 
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bar_q[2], bar_kfull[kStagesK], bar_kempty[kStagesK], bar_vfull[kStagesV],
-      bar_vok[kStagesV], bar_vempty[kStagesV], bar_s[2], bar_p[2][2], bar_o[2], bar_done;
+      bar_vok[kStagesV], bar_vempty[kStagesV], bar_s[2], bar_p[2][2], bar_o[2][2], bar_done;
   __shared__ uint32_t s_tmem;
   __shared__ int s_found, s_bad;
   __shared__ Work s_work;
@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       mbar_init(smem_u32(&bar_s[i]), 1);
       mbar_init(smem_u32(&bar_p[i][0]), 4);
       mbar_init(smem_u32(&bar_p[i][1]), 4);
-      mbar_init(smem_u32(&bar_o[i]), 1);
+      mbar_init(smem_u32(&bar_o[i][0]), 1);
+      mbar_init(smem_u32(&bar_o[i][1]), 1);
     }
     for (int i = 0; i < kStagesK; ++i) {
       mbar_init(smem_u32(&bar_kfull[i]), 1);
@@ -149,6 +150,11 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
     mbar_init_fence();
     s_bad = 0;
   }
+  if (threadIdx.x == 32 * kWarpSoftmax) {
+    tma_prefetch_desc(&tmap_q);
+    tma_prefetch_desc(&tmap_k);
+    tma_prefetch_desc(&tmap_v);
+  }
   griddep_wait();  // the offsets, q, k and v may come from the previous kernel, which may still read o
   if (warp == 0) {  // the sequence and tile of this CTA: 32 sequences a round, the last tiles of a sequence first
     const int per = p.kv_heads * p.chunks;
@@ -157,10 +163,12 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
     bool found = false;
     for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {
       const int b = b0 + lane;
-      int first = 0, n = 0;
+      int first = 0, n = 0, k_first = 0, k_next = 0;
       if (b < p.batch) {
-        first = min(max(p.cu_q[b], 0), p.total_q);
-        n = min(max(p.cu_q[b + 1], first), p.total_q) - first;
+        k_first = __ldg(p.cu_k + b);
+        k_next = __ldg(p.cu_k + b + 1);
+        first = min(max(__ldg(p.cu_q + b), 0), p.total_q);
+        n = min(max(__ldg(p.cu_q + b + 1), first), p.total_q) - first;
       }
       const int tiles = (n + kTiles * p.tokens - 1) / (kTiles * p.tokens);
       int upto = tiles;
@@ -178,8 +186,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         Work w;
         w.q0 = first;
         w.n = n;
-        w.k0 = min(max(p.cu_k[b], 0), p.total_k);
-        w.keys = min(max(p.cu_k[b + 1], w.k0), p.total_k) - w.k0;
+        w.k0 = min(max(k_first, 0), p.total_k);
+        w.keys = min(max(k_next, w.k0), p.total_k) - w.k0;
         w.token = (upto - 1 - tile) * kTiles * p.tokens;
         w.kvh = rest / p.chunks;
         w.head = w.kvh * p.group + (rest % p.chunks) * p.chunk_heads;
@@ -214,8 +222,6 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       bool ok = *const_cast<volatile int*>(&g_debug_hold_loads) == 0;
       if (ok && most > 0) {
         if (elect_one()) {
-          tma_prefetch_desc(&tmap_k);
-          tma_prefetch_desc(&tmap_v);
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
             if (C::kQTmem || blocks[t] == 0) continue;
@@ -284,7 +290,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         __syncwarp();
       };
       // O of tile t += P (buffer b, for the n-th time) V (stage s), in halves as P comes
-      auto values = [&](int t, int b, int n, int s, bool first) {
+      auto values = [&](int t, int b, int n, int s, int j) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           if (!wait(&bar_p[b][half], n)) return;
@@ -293,8 +299,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
             const uint32_t d = tmem + static_cast<uint32_t>(C::kOCol + t * kDim), a = tmem + static_cast<uint32_t>(b * kBlock);
             const uint32_t v = v_lo + static_cast<uint32_t>(s * (C::kKvBytes / 16));
 #pragma unroll
-            for (int i = half * kBlock / 32; i < (half + 1) * kBlock / 32; ++i) mma_f16_ts(d, a + i * 8, v + i * 128, v_hi, idesc_o, !(first && i == 0));
-            if (half == 1) mma_commit(smem_u32(&bar_o[t]));
+            for (int i = half * kBlock / 32; i < (half + 1) * kBlock / 32; ++i) mma_f16_ts(d, a + i * 8, v + i * 128, v_hi, idesc_o, !(j == 0 && i == 0));
+            if (half == 1) mma_commit(smem_u32(&bar_o[t][j & 1]));
           }
           __syncwarp();
         }
@@ -315,7 +321,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           if (j + 1 < most && !wait(&bar_kfull[s1], (j + 1) / kStagesK)) break;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            if (ok && j < blocks[t]) values(t, t, j, s, j == 0);
+            if (ok && j < blocks[t]) values(t, t, j, s, j);
             if (t == 1 && ok) release(&bar_vempty[s]);
             if (ok && j + 1 < blocks[t]) scores(t, t, s1);  // over P, which the product before it has read
           }
@@ -334,7 +340,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
             release(&bar_kempty[s1]);
           }
           if (!wait(&bar_vok[s], j / kStagesV)) break;
-          values(0, j & 1, j >> 1, s, j == 0);
+          values(0, j & 1, j >> 1, s, j);
           if (ok) release(&bar_vempty[s]);
         }
       }
@@ -387,18 +393,19 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       const uint32_t o_at = tmem + lanes + static_cast<uint32_t>(C::kOCol + t * kDim);
       if (C::kQTmem && n > 0) {  // this row of Q, two channels a column
         const T* const src = static_cast<const T*>(p.q) + (w.q0 + token) * p.q_stride + (w.head + head) * kDim;
-#pragma unroll 2
-        for (int i = 0; i < kDim / 32; ++i) {
-          uint32_t y[16];
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) {
-            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(src + i * 32 + e * 2)) : make_uint4(0, 0, 0, 0);
-            y[e] = v.x;
-            y[e + 1] = v.y;
-            y[e + 2] = v.z;
-            y[e + 3] = v.w;
+        for (int h = 0; h < kDim / 128; ++h) {  // 16 loads at once
+          uint32_t y[4][16];
+#pragma unroll
+          for (int e = 0; e < 64; e += 4) {
+            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(src + h * 128 + e * 2)) : make_uint4(0, 0, 0, 0);
+            y[e / 16][e % 16] = v.x;
+            y[e / 16][e % 16 + 1] = v.y;
+            y[e / 16][e % 16 + 2] = v.z;
+            y[e / 16][e % 16 + 3] = v.w;
           }
-          tmem_st16(tmem + lanes + static_cast<uint32_t>(C::kQCol + i * 16), y);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tmem_st16(tmem + lanes + static_cast<uint32_t>(C::kQCol + h * 64 + i * 16), y[i]);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -407,6 +414,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       }
       float m = -INFINITY, sum = 0.0f;
       bool ok = true;
+      // Product j of this tile is in O.  Up to two products may be outstanding where this is asked (S of a block shows that of two
+      // blocks before), so they complete on two barriers in turn: none can pass the phase that is waited for.
+      auto o_has = [&](int j) { return mbar_wait_short(smem_u32(&bar_o[t][j & 1]), static_cast<uint32_t>(j >> 1) & 1u); };
       for (int j = 0; j < n; ++j) {
         const int b = kTiles == 2 ? t : j & 1, visit = kTiles == 2 ? j : j >> 1;
         if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_s[b]), static_cast<uint32_t>(visit) & 1u))) { ok = false; break; }
@@ -432,8 +442,8 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           if (grown) m = top;
           sum *= keep;
           if (j > 0) {
-            // the product of block j - 1 has to be in O (with two tiles S's completion shows that already)
-            if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_o[t]), static_cast<uint32_t>(j - 1) & 1u))) { ok = false; break; }
+            // the product of block j - 1 has to be in O
+            if (!__all_sync(0xffffffffu, o_has(j - 1))) { ok = false; break; }
             tc_fence_after();
 #pragma unroll 1
             for (int i = 0; i < kDim / 32; ++i) {
@@ -472,17 +482,14 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         sum += part[0].x + part[0].y;
       }
       if (ok && n > 0) {
-        // with one tile the last two products may both be outstanding (the last S was made ahead of the first of them), and a
-        // barrier's phases are waited for one by one
-        if (kTiles == 1 && n > 1) mbar_wait_short(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 2) & 1u);
-        ok = __all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_o[t]), static_cast<uint32_t>(n - 1) & 1u));
+        ok = __all_sync(0xffffffffu, o_has(n - 1));
         tc_fence_after();
       }
       if (ok) {
         const bool bad = *const_cast<volatile int*>(&s_bad) != 0;
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         T* const dst = static_cast<T*>(p.o) + (static_cast<size_t>(w.q0 + token) * p.heads + w.head + head) * kDim;
-#pragma unroll 1
+#pragma unroll 2
         for (int i = 0; i < kDim / 32; ++i) {
           float y[32];
           uint32_t r[32];
