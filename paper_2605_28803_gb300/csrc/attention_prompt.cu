@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         }
         __syncwarp();
         auto fetch = [&](const CUtensorMap* map, uint8_t* stage, uint64_t* empty, uint64_t* full, int j, int stages) {
-          if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(empty), (static_cast<uint32_t>(j / stages) & 1u) ^ 1u))) return false;
+          if (!mbar_wait_warp(smem_u32(empty), (static_cast<uint32_t>(j / stages) & 1u) ^ 1u)) return false;
           if (elect_one()) {
             mbar_arrive_expect_tx(smem_u32(full), C::kKvBytes);
             for (int c = 0; c < kBoxes; ++c) tma_load_3d(smem_u32(stage + c * kKvBox), map, c * 64, w.kvh, w.k0 + j * kBlock, smem_u32(full));
@@ -251,9 +251,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         }
         // before leaving, let every load land
         for (int t = 0; t < kTiles; ++t)
-          if (!C::kQTmem && blocks[t] > 0) mbar_wait_short(smem_u32(&bar_q[t]), 0);
-        for (int j = max(0, ks - kStagesK); j < ks; ++j) mbar_wait_short(smem_u32(&bar_kfull[j % kStagesK]), static_cast<uint32_t>(j / kStagesK) & 1u);
-        for (int j = max(0, vs - kStagesV); j < vs; ++j) mbar_wait_short(smem_u32(&bar_vfull[j % kStagesV]), static_cast<uint32_t>(j / kStagesV) & 1u);
+          if (!C::kQTmem && blocks[t] > 0) mbar_wait_warp(smem_u32(&bar_q[t]), 0);
+        for (int j = max(0, ks - kStagesK); j < ks; ++j) mbar_wait_warp(smem_u32(&bar_kfull[j % kStagesK]), static_cast<uint32_t>(j / kStagesK) & 1u);
+        for (int j = max(0, vs - kStagesV); j < vs; ++j) mbar_wait_warp(smem_u32(&bar_vfull[j % kStagesV]), static_cast<uint32_t>(j / kStagesV) & 1u);
       }
       __syncwarp();
     } else if (warp == kWarpMma) {
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
                      v_lo = static_cast<uint32_t>(smem_desc_sw128_mn(smem_u32(smem_v), kKvBox));  // addresses in units of 16 bytes
       bool ok = true;
       auto wait = [&](uint64_t* bar, int n) {  // completion n of a barrier
-        ok = ok && __all_sync(0xffffffffu, mbar_wait_short(smem_u32(bar), static_cast<uint32_t>(n) & 1u));
+        ok = ok && mbar_wait_warp(smem_u32(bar), static_cast<uint32_t>(n) & 1u);
         return ok;
       };
       // S of tile t (buffer b) from K's stage s
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       }
       if (elect_one()) {
         mma_commit(smem_u32(&bar_done));  // every product issued above has completed once this flips
-        mbar_wait_short(smem_u32(&bar_done), 0);
+        mbar_wait(smem_u32(&bar_done), 0);
       }
       __syncwarp();
     } else if (warp < kWarpSoftmax) {
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       if constexpr (kTiles == 2) setmaxnreg_dec<64>();
       for (int j = 0; j < most; ++j) {
         const int s = j % kStagesV;
-        if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_vfull[s]), static_cast<uint32_t>(j / kStagesV) & 1u))) break;
+        if (!mbar_wait_warp(smem_u32(&bar_vfull[s]), static_cast<uint32_t>(j / kStagesV) & 1u)) break;
         const int inside = min(kBlock, w.keys - j * kBlock);  // rows of the sequence; the rest is its neighbour's
         const bool look = p.causal && j >= guard_from;
         if (look || inside < kBlock) {
@@ -416,10 +416,10 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       bool ok = true;
       // Product j of this tile is in O.  Up to two products may be outstanding where this is asked (S of a block shows that of two
       // blocks before), so they complete on two barriers in turn: none can pass the phase that is waited for.
-      auto o_has = [&](int j) { return mbar_wait_short(smem_u32(&bar_o[t][j & 1]), static_cast<uint32_t>(j >> 1) & 1u); };
+      auto o_has = [&](int j) { return mbar_wait_warp(smem_u32(&bar_o[t][j & 1]), static_cast<uint32_t>(j >> 1) & 1u); };
       for (int j = 0; j < n; ++j) {
         const int b = kTiles == 2 ? t : j & 1, visit = kTiles == 2 ? j : j >> 1;
-        if (!__all_sync(0xffffffffu, mbar_wait_short(smem_u32(&bar_s[b]), static_cast<uint32_t>(visit) & 1u))) { ok = false; break; }
+        if (!mbar_wait_warp(smem_u32(&bar_s[b]), static_cast<uint32_t>(visit) & 1u)) { ok = false; break; }
         tc_fence_after();
         const uint32_t s_at = tmem + lanes + static_cast<uint32_t>(b * kBlock);
         uint32_t x[kBlock / 32][32];
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           sum *= keep;
           if (j > 0) {
             // the product of block j - 1 has to be in O
-            if (!__all_sync(0xffffffffu, o_has(j - 1))) { ok = false; break; }
+            if (!o_has(j - 1)) { ok = false; break; }
             tc_fence_after();
 #pragma unroll 1
             for (int i = 0; i < kDim / 32; ++i) {
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         sum += part[0].x + part[0].y;
       }
       if (ok && n > 0) {
-        ok = __all_sync(0xffffffffu, o_has(n - 1));
+        ok = o_has(n - 1);
         tc_fence_after();
       }
       if (ok) {

@@ -103,13 +103,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   }
 }
 
-// The same for waits that are short as a rule: tries (each of which the hardware may hold for a while) come before the clock
-// and the limit are read, which takes longer than such a wait.
-__device__ __forceinline__ bool mbar_wait_short(uint32_t bar, uint32_t parity) {
+// The same for a whole warp, and for waits that are short as a rule: tries (each of which the hardware may hold for a while)
+// come before the clock and the limit are read, which takes longer than such a wait; the warp stays together, so a wait
+// that is over already costs one try and one vote.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
   for (int i = 0; i < 128; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
-  return mbar_wait(bar, parity);
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity));
 }
 
 __device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
