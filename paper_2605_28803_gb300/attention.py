@@ -1,0 +1,110 @@
+"""One attention block of the language backbone or the action head, as it is served: the fused Q/K/V linear (W4A4), attention, the
+output linear (W4A4), and a 4-bit key/value cache of its tokens.
+
+``prefill`` takes packed prompts: attention over the fresh keys and values (and over what the cache gives back where a
+sequence has tokens already), which then enter the cache.  ``step`` takes the next token or tokens of every sequence: they
+enter the cache and attend to it.  Every step of the computation is a libqvla call on the current stream; this file only
+places buffers and pages.
+"""
+
+from __future__ import annotations
+
+import torch
+
+from . import qvla as Q
+
+_TORCH = {Q.F16: torch.float16, Q.BF16: torch.bfloat16}
+
+
+class AttentionBlock:
+    """``qkv``: a Layer with N = (heads + 2 kv_heads) head_dim, columns [Q | K | V]; ``o``: a Layer with K = heads head_dim, of
+    one activation and output type.  Up to ``max_tokens`` tokens of each of ``batch`` sequences are cached."""
+
+    def __init__(self, qkv: Q.Layer, o: Q.Layer, heads: int, kv_heads: int, head_dim: int, batch: int, max_tokens: int,
+                 page_size: int = 64, rotate: bool = True, device=None):
+        if qkv.N != (heads + 2 * kv_heads) * head_dim or o.K != heads * head_dim:
+            raise ValueError("the layers' widths do not match the heads")
+        if not qkv.xdt == qkv.ydt == o.xdt == o.ydt or qkv.ydt not in _TORCH:
+            raise ValueError("the layers must share one 16-bit type")
+        self.qkv, self.o, self.heads, self.kv_heads, self.dim, self.batch = qkv, o, heads, kv_heads, head_dim, batch
+        self.dt, self.torch_dt = qkv.ydt, _TORCH[qkv.ydt]
+        self.device = torch.device("cuda") if device is None else device
+        self.scale = head_dim ** -0.5
+        self.max_tokens = max_tokens
+        self.width = -(-max_tokens // page_size)
+        pages = batch * self.width
+        self.pool = torch.zeros(Q.qvla_kv4_pool_bytes(pages, page_size, kv_heads, head_dim), dtype=torch.uint8, device=self.device)
+        self.cache = Q.Kv4Cache(self.pool, pages, page_size, kv_heads, head_dim, rotate)
+        self.table = torch.arange(pages, dtype=torch.int32, device=self.device).reshape(batch, self.width)
+        self.lens = [0] * batch  # cached tokens, and the same on the device
+        self.lens_device = torch.zeros(batch, dtype=torch.int32, device=self.device)
+        self._ws = torch.empty(256, dtype=torch.uint8, device=self.device)
+
+    def _workspace(self, nbytes: int) -> torch.Tensor:
+        if self._ws.numel() < nbytes:
+            self._ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return self._ws
+
+    def _linear(self, layer: Q.Layer, x, stream) -> torch.Tensor:
+        m = x.shape[0]
+        y = torch.empty(m, layer.N, dtype=self.torch_dt, device=self.device)
+        n = Q.qvla_linear_workspace_bytes(layer, m)
+        Q.qvla_w4a4_linear(layer, x, m, -1, y, self._workspace(n), n, stream)
+        return y
+
+    def _ints(self, values) -> torch.Tensor:
+        return torch.tensor(values, dtype=torch.int32, device=self.device)
+
+    def _split(self, y):
+        """Queries, keys and values in the fused output, where they lie."""
+        q, k = self.heads * self.dim, self.kv_heads * self.dim
+        return y[:, :q], y[:, q: q + k], y[:, q + k:]
+
+    def _store(self, y, lens, cu, stream) -> None:
+        if any(n + new > self.max_tokens for n, new in zip(self.lens, lens)):
+            raise ValueError(f"a sequence would exceed {self.max_tokens} cached tokens")
+        _, k, v = self._split(y)
+        Q.qvla_kv4_append(self.cache, k, v, self.dt, y.stride(0), y.stride(0), self.batch, cu, y.shape[0], self.table, self.width,
+                          self.lens_device, stream)
+        self.lens = [n + new for n, new in zip(self.lens, lens)]
+        self.lens_device = self._ints(self.lens)
+
+    def prefill(self, x: torch.Tensor, lens, causal: bool = True) -> torch.Tensor:
+        """x [sum(lens), qkv.K]: the next lens[b] tokens of every sequence (0 for none), packed.  Returns [sum(lens), o.N]."""
+        stream = torch.cuda.current_stream()
+        total, fresh = sum(lens), not any(self.lens)
+        cu = self._ints([sum(lens[:b]) for b in range(self.batch + 1)])
+        y = self._linear(self.qkv, x, stream)
+        q, k, v = self._split(y)
+        ks = vs = y.stride(0)
+        self._store(y, lens, cu, stream)
+        cu_k, total_k = cu, total
+        if not fresh:  # earlier tokens come from the cache, and the new ones with them
+            total_k = sum(self.lens)
+            cu_k = self._ints([sum(self.lens[:b]) for b in range(self.batch + 1)])
+            k, v = (torch.empty(total_k, self.kv_heads * self.dim, dtype=self.torch_dt, device=self.device) for _ in range(2))
+            ks = vs = self.kv_heads * self.dim
+            Q.qvla_kv4_gather(self.cache, self.batch, cu_k, total_k, self.table, self.width, None, k, v, self.dt, stream)
+        a = torch.empty(total, self.heads * self.dim, dtype=self.torch_dt, device=self.device)
+        Q.qvla_attention_prompt(q, k, v, self.dt, self.heads, self.kv_heads, self.dim, y.stride(0), ks, vs, self.batch, cu, total,
+                                cu_k, total_k, self.scale, causal, a, stream)
+        return self._linear(self.o, a, stream)
+
+    def step(self, x: torch.Tensor, causal: bool = True) -> torch.Tensor:
+        """x [batch * n, qkv.K]: the next n tokens of every sequence.  Returns [batch * n, o.N]."""
+        stream = torch.cuda.current_stream()
+        total = x.shape[0]
+        n = total // self.batch
+        if n * self.batch != total:
+            raise ValueError("x holds the same number of tokens of every sequence")
+        cu = self._ints([b * n for b in range(self.batch + 1)])
+        y = self._linear(self.qkv, x, stream)
+        self._store(y, [n] * self.batch, cu, stream)
+        longest = max(self.lens)
+        a = torch.empty(total, self.heads * self.dim, dtype=self.torch_dt, device=self.device)
+        need = Q.qvla_attention_kv4_workspace_bytes(self.heads, self.kv_heads, self.dim, self.batch, max(total, 1), max(n, 1),
+                                                    max(longest, 1))
+        Q.qvla_attention_kv4(self.cache, self._split(y)[0], self.dt, self.heads, y.stride(0), self.batch, cu, total, n, self.table,
+                             self.width, self.lens_device, longest, self.scale, causal, a, self._workspace(need) if need else None,
+                             need, stream)
+        return self._linear(self.o, a, stream)
