@@ -13,6 +13,7 @@ using qvla::fail;
 namespace {
 
 constexpr int kMaxTokens = 1 << 24;
+constexpr int kMaxLength = 1 << 30;  // of a cached sequence
 constexpr int kMaxHeads = 1024;
 
 qvla_status check_heads(qvla_dtype dt, int heads, int kv_heads, int head_dim) {
@@ -142,7 +143,7 @@ size_t qvla_attention_kv4_workspace_bytes(int heads, int kv_heads, int head_dim,
                                           int max_len) {
   if (heads < 1 || heads > kMaxHeads || kv_heads < 1 || heads % kv_heads != 0 ||
       (head_dim != 64 && head_dim != 128 && head_dim != 256) || batch < 1 || batch > 65535 || total_q < 1 ||
-      total_q > kMaxTokens || max_q < 1 || max_len < 1)
+      total_q > kMaxTokens || max_q < 1 || max_q > kMaxTokens || max_len < 1 || max_len > kMaxLength)
     return 0;
   qvla::Kv4AttentionArgs a = {};
   a.pool.kv_heads = kv_heads;
@@ -171,8 +172,8 @@ qvla_status qvla_attention_kv4(const qvla_kv4_cache* cache, const void* q, qvla_
   if (qvla_status s = check_tokens("o", o, total_q, width, width)) return s;
   if (qvla_status s = check_batch(batch, cu_q, page_table, max_pages)) return s;
   if (batch > 0 && !kv_len) return fail(QVLA_ERR_INVALID_ARG, "kv_len must not be NULL");
-  if (max_q < 0 || max_q > kMaxTokens || max_len < 0)
-    return fail(QVLA_ERR_INVALID_ARG, "max_q=%d and max_len=%d must not be negative (max_q at most 2^24)", max_q, max_len);
+  if (max_q < 0 || max_q > kMaxTokens || max_len < 0 || max_len > kMaxLength)
+    return fail(QVLA_ERR_INVALID_ARG, "max_q=%d outside [0, 2^24] or max_len=%d outside [0, 2^30]", max_q, max_len);
   if (static_cast<int64_t>(max_len) > (static_cast<int64_t>(max_pages) << pool.log_page))
     return fail(QVLA_ERR_INVALID_ARG, "max_len=%d exceeds the %d pages of a sequence's table", max_len, max_pages);
   if (qvla_status s = check_scale(scale)) return s;

@@ -19,12 +19,15 @@
 //   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
 // float16.
 //
-// The cached tokens of a sequence are split into chunks over CTAs (of kWarps warps, each with every kWarps-th step), and the
-// chunks' results joined by a second kernel where a sequence has more than one.  The device decides the chunks from the lengths it
-// finds, so that short and long sequences of one call share the SMs evenly and a captured graph follows its lengths; the
-// host only bounds their number.
+// The cached tokens of a sequence are split into chunks over CTAs (of kWarps warps, each with every kWarps-th step).  The device
+// decides the chunks from the lengths it finds, so that a captured graph follows its lengths.  Two ways:
+//   - a cluster of up to 8 CTAs a sequence, head and row tile, each with an equal part, whose results are joined through
+//     distributed shared memory: one launch, for contexts short enough that the longest part does not outlast the rest;
+//   - chunks of about equal length over all sequences, joined by a second kernel: long and short contexts of one call share
+//     the SMs evenly.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cfloat>
 
 #include "griddep.cuh"
@@ -47,10 +50,12 @@ struct Kv4Params {
   int row_tiles;
   int target;        // CTAs to aim for; 0: one chunk a sequence
   int ctas;          // at most this many: target and a CTA for the remainder of every sequence
+  int cluster;       // CTAs of a cluster that share a sequence's keys; 0: chunks by length
   float* part;       // [ctas][rows][head_dim + 2]: sums over the values, then the reference and sum p
 };
 constexpr int kLeastChunk = kTile * kWarps;
 constexpr int kCtasPerSm8 = 8, kCtasPerSm16 = 2;  // to aim for, with row tiles of 8 and of 16
+constexpr int kClusterLen = 4096;                 // longest context that clusters share
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -90,6 +95,12 @@ __device__ __forceinline__ void read_words(uint32_t (&r)[kWords], uint32_t at) {
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// Two floats of a CTA of the cluster (address from mapa_shared).
+__device__ __forceinline__ float2 cluster_load2(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kBut>
@@ -146,7 +157,8 @@ struct Cfg {
   // apart, which spreads the fragments' stores over the banks.
   static constexpr int kEighth = kDim / 8 + 2, kJoinRow = 8 * kEighth + 4;
   static constexpr int kJoin = kWarps * kRows * kJoinRow * 4;
-  static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kRows * kQStride * 2;
+  static constexpr int kPart = kRows * (kDim + 2) * 4;      // this CTA's result, for its cluster
+  static constexpr int kSmem = (kRing > kJoin + kPart ? kRing : kJoin + kPart) + kRows * kQStride * 2;
 };
 
 template <typename T, int kDim, int kTiles>
@@ -161,6 +173,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   __half* const q_at = reinterpret_cast<__half*>(s_raw);                      // [kRows][kQStride]
   uint8_t* const s_ring = s_raw + kRows * C::kQStride * 2;                    // [kWarps][kStages][kStepBytes]
   float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kJoinRow] at the end
+  float* const s_part = reinterpret_cast<float*>(s_ring + C::kJoin);          // [kRows][kDim + 2]
   static_assert(kRows * C::kQStride * 2 % 128 == 0, "the ring's pieces are placed by 128-byte lines");
   __shared__ float s_f[kRows], s_sum[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
   __shared__ int s_end[kWarps][kStages][kParts];  // first token that nobody may use
@@ -169,11 +182,17 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   griddep_wait();  // the queries, lengths and the cache may come from the previous kernel, which may still read o
   griddep_launch_dependents();
   // this CTA's sequence b, chunk ch of it, key/value head and row tile
-  const int rest = static_cast<int>(blockIdx.x) % p.per, tile = rest % p.row_tiles, kvh = rest / p.row_tiles;
-  int ch = static_cast<int>(blockIdx.x) / p.per, b = -1, chunk = 0;
+  const int unit = p.cluster ? static_cast<int>(blockIdx.x) / p.cluster : static_cast<int>(blockIdx.x);
+  const int rest = unit % p.per, tile = rest % p.row_tiles, kvh = rest / p.row_tiles;
+  int ch = unit / p.per, b = -1, chunk = 0;
   Sequence seq = {0, 0, 0};  // of sequence b0 + lane, then of b
-  if (lane < a.batch) seq = load_sequence(a, lane);
-  {
+  if (p.cluster) {
+    b = ch;
+    ch = static_cast<int>(blockIdx.x) % p.cluster;  // (the CTA's rank)
+    seq = load_sequence(a, b);
+    chunk = max(kLeastChunk, chunk_size(usable_length(a, seq.len), p.cluster));
+  } else {
+    if (lane < a.batch) seq = load_sequence(a, lane);
     const int64_t length = chunk_length(p, usable_length(a, seq.len));
     for (int b0 = 0; b0 < a.batch && b < 0; b0 += 32) {
       if (b0 > 0 && b0 + lane < a.batch) seq = load_sequence(a, b0 + lane);
@@ -202,7 +221,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   if (rows <= 0) return;
   const int most = seen_by(seq, a.causal, (row0 + rows - 1) / p.group);  // tokens that the last row sees
   const int k0 = ch * chunk, k1 = min(most, k0 + chunk);
-  if (ch > 0 && k0 >= most) return;
+  if (ch > 0 && k0 >= most && !p.cluster) return;  // (the CTAs of a cluster stay together)
 
   // ---- the first cached tokens are asked for before the queries are worked on
   const uint32_t block = (kDim + 8u) << a.pool.log_page, stride = block * a.pool.kv_heads;  // of a head's page, of a page
@@ -516,7 +535,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
       for (int c = 0; c < kDim / 16; ++c) *reinterpret_cast<float2*>(dst + 2 * c) = make_float2(o[c][n][e], o[c][n][e + 2]);
     }
   __syncthreads();
-  const bool whole = most <= chunk;
+  const bool whole = most <= chunk && !p.cluster;
 #pragma unroll
   for (int r0 = 0; r0 < kRows; r0 += kTeams) {
     const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
@@ -546,12 +565,47 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
         *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
       }
     } else if (r < rows) {
-      float* const dst = p.part + (static_cast<size_t>(blockIdx.x) * kRows + r) * (kDim + 2);
+      float* const dst = p.cluster ? s_part + r * (kDim + 2) : p.part + (static_cast<size_t>(blockIdx.x) * kRows + r) * (kDim + 2);
 #pragma unroll
       for (int c = 0; c < 8; c += 2) *reinterpret_cast<float2*>(dst + tl * 8 + c) = make_float2(y[c], y[c + 1]);
       if (tl == 0) *reinterpret_cast<float2*>(dst + kDim) = make_float2(top, sum);
     }
   }
+  if (!p.cluster) return;
+
+  // ---- join the cluster: its CTAs take the rows in turn
+  cluster_sync();
+  const uint32_t mine = smem_u32(s_part);
+  for (int r0 = 0; r0 < rows; r0 += kTeams * p.cluster) {
+    const int r = r0 + ch * kTeams + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
+    float m = -FLT_MAX, sum = 0.0f, y[8] = {};
+    if (r < rows) {
+      for (int c = 0; c < p.cluster; ++c) {
+        const uint32_t at = mapa_shared(mine + static_cast<uint32_t>(r) * (kDim + 2) * 4, static_cast<uint32_t>(c));
+        const float2 ml = cluster_load2(at + kDim * 4);
+        float2 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = cluster_load2(at + tl * 32 + e * 8);
+        const float top = fmaxf(m, ml.x), keep = ex2(m - top), k = ex2(ml.x - top);
+        m = top;
+        sum = sum * keep + ml.y * k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[2 * e] = y[2 * e] * keep + v[e].x * k;
+          y[2 * e + 1] = y[2 * e + 1] * keep + v[e].y * k;
+        }
+      }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) y[c] *= inv;
+    if (a.pool.rotate) rotate_head<kTeam>(y);
+    if (r < rows) {
+      const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
+      *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+    }
+  }
+  cluster_sync();  // nobody leaves while its result is being read
 }
 
 // The chunks of a query row (one head of one token) joined by a CTA: teams of D / 8 lanes take every kTeams-th chunk.
@@ -641,6 +695,17 @@ cudaError_t plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p)
   if (units > 0x3fffffff) return cudaErrorInvalidConfiguration;
   p->row_tiles = static_cast<int>(tiles);
   p->per = static_cast<int>(a.pool.kv_heads * tiles);
+  // A cluster a unit where clusters of eight leave SMs to spare and a part stays short: then the second launch is what a call
+  // can save (one token over 817: 9.4 against 10.4 us).  With more units the chunks by length are faster (23 ragged contexts
+  // of up to 6001 tokens: 20.5 us against 24 with clusters).
+  const int64_t parts = (static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk;
+  p->cluster = 0;
+  if (units * 8 <= a.num_sms && parts > 1 && a.max_len <= kClusterLen) {
+    p->cluster = static_cast<int>(parts < 8 ? parts : 8);
+    p->target = 0;
+    p->ctas = static_cast<int>(units * p->cluster);
+    return cudaSuccess;
+  }
   int64_t target = static_cast<int64_t>(a.num_sms) * (p->rows == 8 ? kCtasPerSm8 : kCtasPerSm16);
   const int64_t part = static_cast<int64_t>(p->rows) * (a.pool.head_dim + 2) * 4;
   const int64_t most = units * ((static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk);  // with the least chunks
@@ -662,20 +727,32 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
   if (joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
   using C = Cfg<kDim, kTiles>;
   auto kern = attention_kv4_kernel<T, kDim, kTiles>;
-  if (C::kSmem > 48 * 1024) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  if (C::kSmem > 48 * 1024) {  // once a device
+    static std::atomic<uint64_t> raised{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
+    if (bit == 0 || !(raised.load(std::memory_order_relaxed) & bit)) {
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+      if (e != cudaSuccess) return e;
+      raised.fetch_or(bit, std::memory_order_relaxed);
+    }
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.ctas));
   cfg.blockDim = dim3(32 * kWarps);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = a.stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(p.cluster);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.cluster ? 2 : 1;
   cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
   if (e != cudaSuccess) return e;
   if (p.target > 0) {
