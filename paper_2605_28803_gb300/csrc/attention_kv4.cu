@@ -69,8 +69,11 @@ __device__ __forceinline__ float lg2(float x) {
 }
 
 // Of a word of 8 codes: (code + 8) 2^-24 at nibbles 0 and 4, (code + 8) 2^-20 at 1 and 5.
-__device__ __forceinline__ uint32_t offsets_04(uint32_t w) { return (w & 0x000f000fu) ^ 0x00080008u; }
-__device__ __forceinline__ uint32_t offsets_15(uint32_t w) { return (w & 0x00f000f0u) ^ 0x00800080u; }
+struct OffsetBits {
+  uint32_t low = hidden_constant<0x00080008u>(), high = hidden_constant<0x00800080u>();
+  __device__ __forceinline__ uint32_t offsets_04(uint32_t w) const { return and_xor(w, 0x000f000fu, low); }
+  __device__ __forceinline__ uint32_t offsets_15(uint32_t w) const { return and_xor(w, 0x00f000f0u, high); }
+};
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -357,6 +360,8 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
   uint32_t v_get[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) v_get[e] = 8 * kDim + value_place(2 * t + e, g * (kDim / 16) / 16) + (g * (kDim / 16) & 15);
+  const OffsetBits kbits;
+  const CodeBits vbits;
   auto step = [&](int i, int slot) {
     const int at = k0 + kStep * (warp + kWarps * i);
     const uint32_t from = ring + slot * C::kStepBytes;
@@ -397,7 +402,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
       for (int w = 0; w < kKeyWords; ++w) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const uint32_t a0 = offsets_04(k[0][w]), a1 = offsets_04(k[1][w]), a2 = offsets_15(k[0][w]), a3 = offsets_15(k[1][w]);
+          const uint32_t a0 = kbits.offsets_04(k[0][w]), a1 = kbits.offsets_04(k[1][w]), a2 = kbits.offsets_15(k[0][w]), a3 = kbits.offsets_15(k[1][w]);
 #pragma unroll
           for (int n = 0; n < kTiles; ++n) {
             if constexpr (kQInRegs) {
@@ -497,7 +502,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid
           uint32_t v0 = __byte_perm(v[0][w], v[1][w], u ? 0x7632 : 0x5410), v1 = __byte_perm(v[2][w], v[3][w], u ? 0x7632 : 0x5410);
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const uint32_t a0 = codes_04(v0), a1 = codes_15(v0), a2 = codes_04(v1), a3 = codes_15(v1);
+            const uint32_t a0 = vbits.codes_04(v0), a1 = vbits.codes_15(v0), a2 = vbits.codes_04(v1), a3 = vbits.codes_15(v1);
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) mma16816(o[4 * w + 2 * u + c][n], a0, a1, a2, a3, b0[n], b1[n]);
             v0 >>= 8;

@@ -79,18 +79,35 @@ __device__ __forceinline__ void rotate_head(float (&y)[8]) {
   for (int i = 0; i < 8; ++i) y[i] *= f;
 }
 
+// (w & mask) ^ flip in one instruction.  Only one of its operands can be an immediate: `flip` comes from a register that the
+// compiler cannot see through (hidden_constant), or it would take two instructions with an immediate each.
+__device__ __forceinline__ uint32_t and_xor(uint32_t w, uint32_t mask, uint32_t flip) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(r) : "r"(w), "r"(mask), "r"(flip));
+  return r;
+}
+template <uint32_t kValue>
+__device__ __forceinline__ uint32_t hidden_constant() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %1;" : "=r"(r) : "n"(kValue));
+  return r;
+}
+
 // Of a word of 8 codes: the codes at nibbles 0 and 4, and at 1 and 5, as float16 pairs.  The bits 0x6408 ^ code read 1032 + code
 // and 0x5480 ^ (code << 4) read 72 + code, from which one exact addition takes the offset.
-__device__ __forceinline__ uint32_t codes_04(uint32_t w) {
-  w = (w & 0x000f000fu) ^ 0x64086408u;
-  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0xe408)));  // -1032
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t codes_15(uint32_t w) {
-  w = (w & 0x00f000f0u) ^ 0x54805480u;
-  const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0xd480)));  // -72
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
+struct CodeBits {
+  uint32_t low = hidden_constant<0x64086408u>(), high = hidden_constant<0x54805480u>();
+  __device__ __forceinline__ uint32_t codes_04(uint32_t w) const {
+    w = and_xor(w, 0x000f000fu, low);
+    const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0xe408)));  // -1032
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  __device__ __forceinline__ uint32_t codes_15(uint32_t w) const {
+    w = and_xor(w, 0x00f000f0u, high);
+    const __half2 v = __hadd2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half(0xd480)));  // -72
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+};
 
 // Two float32 operations an instruction, each rounded like the single one.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {

@@ -253,14 +253,15 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
       for (int k = 0; k < 4; ++k) *reinterpret_cast<uint32_t*>(h.at + k * 4 * kTeam) = w[k];
       if (tl == 0) *h.scale = d;
     } else {
+      const CodeBits bits;
       __half2 v[4][4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t w = k == 0 ? h.x[0].x : k == 1 ? h.x[0].y : k == 2 ? h.x[0].z : h.x[0].w;
-        *reinterpret_cast<uint32_t*>(&v[k][0]) = codes_04(w);
-        *reinterpret_cast<uint32_t*>(&v[k][1]) = codes_15(w);
-        *reinterpret_cast<uint32_t*>(&v[k][2]) = codes_04(w >> 8);
-        *reinterpret_cast<uint32_t*>(&v[k][3]) = codes_15(w >> 8);
+        *reinterpret_cast<uint32_t*>(&v[k][0]) = bits.codes_04(w);
+        *reinterpret_cast<uint32_t*>(&v[k][1]) = bits.codes_15(w);
+        *reinterpret_cast<uint32_t*>(&v[k][2]) = bits.codes_04(w >> 8);
+        *reinterpret_cast<uint32_t*>(&v[k][3]) = bits.codes_15(w >> 8);
       }
       if (a.pool.rotate) rotate_codes<kTeam>(v);
       if (h.out == nullptr) return;
