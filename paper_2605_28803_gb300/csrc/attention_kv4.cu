@@ -48,13 +48,17 @@ struct Kv4Params {
   int rows;          // query rows of a CTA (8 or 16): (token, head of the group), tokens outer
   int per;           // CTAs of a chunk: kv_heads x row tiles for max_q queries
   int row_tiles;
-  int target;        // CTAs to aim for; 0: one chunk a sequence
-  int ctas;          // at most this many: target and a CTA for the remainder of every sequence
+  int target;        // CTAs to aim for, those that the SMs hold at once; 0: one chunk a sequence
+  int most_target;   // the same where there is work enough to even out over several waves
+  int ctas;          // at most this many: most_target and a CTA for the remainder of every sequence
   int cluster;       // CTAs of a cluster that share a sequence's keys; 0: chunks by length
   float* part;       // [ctas][rows][head_dim + 2]: sums over the values, then the reference and sum p
 };
 constexpr int kLeastChunk = kTile * kWarps;
-constexpr int kCtasPerSm8 = 8, kCtasPerSm16 = 2;  // to aim for, with row tiles of 8 and of 16
+// CTAs that an SM holds (their registers allow it), and how often to fill the SMs: single tokens' contexts differ in length.
+constexpr int ctas_per_sm(int dim, int rows) { return rows == 8 ? (dim == 256 ? 3 : 4) : (dim == 64 ? 3 : 2); }
+constexpr int kWaves8 = 2, kWaves16 = 1;
+constexpr int kLongChunk = 1024;  // tokens of a CTA above which more waves pay (a CTA's own start and end take about 5 us)
 constexpr int kClusterLen = 4096;                 // longest context that clusters share
 
 __device__ __forceinline__ float ex2(float x) {
@@ -140,8 +144,18 @@ __device__ __forceinline__ int64_t chunk_length(const Kv4Params& p, int len) {
   for (int b = 32 + static_cast<int>(threadIdx.x & 31); b < p.a.batch; b += 32) all += usable_length(p.a, __ldg(p.a.kv_len + b));
 #pragma unroll
   for (int h = 1; h < 32; h *= 2) all += __shfl_xor_sync(0xffffffffu, all, h);
-  const int64_t length = (all * p.per + p.target - 1) / p.target;
-  return max(static_cast<int64_t>(kLeastChunk), (length + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
+  const int target = all * p.per > static_cast<int64_t>(p.target) * kLongChunk ? p.most_target : p.target;
+  auto rounded = [](int64_t v) { return max(static_cast<int64_t>(kLeastChunk), (v + kLeastChunk - 1) / kLeastChunk * kLeastChunk); };
+  int64_t length = rounded((all * p.per + target - 1) / target);
+  // the remainders of the sequences come on top: lengthen the chunks until all fit the target, so that no CTA is left for a wave
+  // of its own (a few tries, where the lengths are at hand)
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  for (int i = 0; i < 4 && p.a.batch <= 32; ++i) {
+    const int64_t ctas = static_cast<int64_t>(__reduce_add_sync(0xffffffffu, lane < p.a.batch ? chunks_of(len, length) : 0)) * p.per;
+    if (ctas <= target) break;
+    length = rounded(length * ctas / target + 1);
+  }
+  return length;
 }
 
 template <int kDim, int kTiles>
@@ -165,7 +179,7 @@ struct Cfg {
 };
 
 template <typename T, int kDim, int kTiles>
-__global__ void __launch_bounds__(32 * kWarps) attention_kv4_kernel(const __grid_constant__ Kv4Params p) {
+__global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) attention_kv4_kernel(const __grid_constant__ Kv4Params p) {
   using C = Cfg<kDim, kTiles>;
   constexpr int kRows = C::kRows, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam, kStages = C::kStages, kParts = C::kParts,
                 kStep = C::kStep;
@@ -690,8 +704,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
 
 int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * (a.heads / a.pool.kv_heads) <= 8 ? 8 : 16; }
 
-// CTAs to aim for: the SMs filled once with row tiles of 16 (whose CTAs are long), several times with single tokens, as far as
-// the workspace has room for their results.
+// The split, as far as the workspace has room for the CTAs' results.
 cudaError_t plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p) {
   p->group = a.heads / a.pool.kv_heads;
   p->rows = rows_of(a);
@@ -705,20 +718,23 @@ cudaError_t plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p)
   // of up to 6001 tokens: 20.5 us against 24 with clusters).
   const int64_t parts = (static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk;
   p->cluster = 0;
+  p->target = p->most_target = 0;
   if (units * 8 <= a.num_sms && parts > 1 && a.max_len <= kClusterLen) {
     p->cluster = static_cast<int>(parts < 8 ? parts : 8);
-    p->target = 0;
     p->ctas = static_cast<int>(units * p->cluster);
     return cudaSuccess;
   }
-  int64_t target = static_cast<int64_t>(a.num_sms) * (p->rows == 8 ? kCtasPerSm8 : kCtasPerSm16);
+  int64_t target = static_cast<int64_t>(a.num_sms) * ctas_per_sm(a.pool.head_dim, p->rows), most_target = target * (p->rows == 8 ? kWaves8 : kWaves16);
   const int64_t part = static_cast<int64_t>(p->rows) * (a.pool.head_dim + 2) * 4;
-  const int64_t most = units * ((static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk);  // with the least chunks
-  const int64_t room = static_cast<int64_t>(ws_bytes / part);
-  if (target > room - units) target = room - units;
-  if (target < units || most <= units) target = 0;  // (no more than a chunk a sequence)
+  const int64_t least = units * parts;  // CTAs with the least chunks
+  const int64_t room = static_cast<int64_t>(ws_bytes / part) - units;
+  if (units * a.max_len <= target * kLongChunk) most_target = target;
+  if (target > room) target = room;
+  if (most_target > room) most_target = room;
+  if (target < units || least <= units) target = most_target = 0;  // (no more than a chunk a sequence)
   p->target = static_cast<int>(target);
-  p->ctas = static_cast<int>(target == 0 ? units : target + units < most ? target + units : most);
+  p->most_target = static_cast<int>(most_target);
+  p->ctas = static_cast<int>(target == 0 ? units : most_target + units < least ? most_target + units : least);
   return cudaSuccess;
 }
 
