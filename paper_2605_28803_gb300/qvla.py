@@ -302,13 +302,18 @@ def qvla_gemm_w4a8(layer: Layer, xq, xscale, M: int, y, acc, workspace, workspac
                                workspace_bytes, _stream(stream)))
 
 
+# The attention calls are short (a decoded token's takes a few microseconds): their wrappers take tensors only and call the
+# library without the helpers above.
+
 def qvla_attention_prompt(q, k, v, dt: int, heads: int, kv_heads: int, head_dim: int, q_stride: int, k_stride: int,
                           v_stride: int, batch: int, cu_q, total_q: int, cu_k, total_k: int, scale: float, causal: bool,
                           o, stream=None) -> None:
     """Softmax attention over packed prompts; strides in elements between tokens."""
-    _check(_lib.qvla_attention_prompt(_ptr(q), _ptr(k), _ptr(v), dt, heads, kv_heads, head_dim, q_stride, k_stride,
-                                      v_stride, batch, _ptr(cu_q), total_q, _ptr(cu_k), total_k, scale,
-                                      1 if causal else 0, _ptr(o), _stream(stream)))
+    status = _lib.qvla_attention_prompt(q.data_ptr(), k.data_ptr(), v.data_ptr(), dt, heads, kv_heads, head_dim, q_stride,
+                                        k_stride, v_stride, batch, cu_q.data_ptr(), total_q, cu_k.data_ptr(), total_k, scale,
+                                        1 if causal else 0, o.data_ptr(), _stream(stream))
+    if status:
+        _check(status)
 
 
 class _Kv4Struct(ctypes.Structure):
@@ -319,12 +324,13 @@ class Kv4Cache:
     """A 4-bit key/value cache (qvla_kv4_cache) over `pool`, a device buffer of qvla_kv4_pool_bytes(...) bytes that the
     caller owns and this object keeps alive."""
 
+    __slots__ = ("pool", "struct", "ref")
+
     def __init__(self, pool, num_pages: int, page_size: int, kv_heads: int, head_dim: int, rotate: bool = True):
-        if pool is not None and pool.numel() * pool.element_size() < qvla_kv4_pool_bytes(num_pages, page_size, kv_heads,
-                                                                                         head_dim):
+        if pool.nbytes < num_pages * page_size * kv_heads * (head_dim + 8):
             raise ValueError("the pool is smaller than qvla_kv4_pool_bytes(...)")
         self.pool = pool
-        self.struct = _Kv4Struct(_ptr(pool), num_pages, page_size, kv_heads, head_dim, 1 if rotate else 0)
+        self.struct = _Kv4Struct(pool.data_ptr(), num_pages, page_size, kv_heads, head_dim, 1 if rotate else 0)
         self.ref = ctypes.addressof(self.struct)
 
 
@@ -334,14 +340,21 @@ def qvla_kv4_pool_bytes(num_pages: int, page_size: int, kv_heads: int, head_dim:
 
 def qvla_kv4_append(cache: Kv4Cache, k, v, dt: int, k_stride: int, v_stride: int, batch: int, cu_new, total_new: int,
                     page_table, max_pages: int, start, stream=None) -> None:
-    _check(_lib.qvla_kv4_append(cache.ref, _ptr(k), _ptr(v), dt, k_stride, v_stride, batch, _ptr(cu_new), total_new,
-                                _ptr(page_table), max_pages, _ptr(start), _stream(stream)))
+    """Quantise new tokens into the cache; start None: every sequence begins at position 0."""
+    status = _lib.qvla_kv4_append(cache.ref, k.data_ptr(), v.data_ptr(), dt, k_stride, v_stride, batch, cu_new.data_ptr(),
+                                  total_new, page_table.data_ptr(), max_pages, None if start is None else start.data_ptr(),
+                                  _stream(stream))
+    if status:
+        _check(status)
 
 
 def qvla_kv4_gather(cache: Kv4Cache, batch: int, cu, total: int, page_table, max_pages: int, start, k, v, dt: int,
                     stream=None) -> None:
-    _check(_lib.qvla_kv4_gather(cache.ref, batch, _ptr(cu), total, _ptr(page_table), max_pages, _ptr(start), _ptr(k),
-                                _ptr(v), dt, _stream(stream)))
+    """Read cached tokens back as values; start None: from position 0."""
+    status = _lib.qvla_kv4_gather(cache.ref, batch, cu.data_ptr(), total, page_table.data_ptr(), max_pages,
+                                  None if start is None else start.data_ptr(), k.data_ptr(), v.data_ptr(), dt, _stream(stream))
+    if status:
+        _check(status)
 
 
 def qvla_attention_kv4_workspace_bytes(heads: int, kv_heads: int, head_dim: int, batch: int, total_q: int, max_q: int,
@@ -352,9 +365,13 @@ def qvla_attention_kv4_workspace_bytes(heads: int, kv_heads: int, head_dim: int,
 def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, batch: int, cu_q, total_q: int, max_q: int,
                        page_table, max_pages: int, kv_len, max_len: int, scale: float, causal: bool, o, workspace=None,
                        workspace_bytes: int = 0, stream=None) -> None:
-    _check(_lib.qvla_attention_kv4(cache.ref, _ptr(q), dt, heads, q_stride, batch, _ptr(cu_q), total_q, max_q,
-                                   _ptr(page_table), max_pages, _ptr(kv_len), max_len, scale, 1 if causal else 0, _ptr(o),
-                                   _ptr(workspace), workspace_bytes, _stream(stream)))
+    """Attention of a few query tokens of every sequence over its cached tokens."""
+    status = _lib.qvla_attention_kv4(cache.ref, q.data_ptr(), dt, heads, q_stride, batch, cu_q.data_ptr(), total_q, max_q,
+                                     page_table.data_ptr(), max_pages, kv_len.data_ptr(), max_len, scale, 1 if causal else 0,
+                                     o.data_ptr(), None if workspace is None else workspace.data_ptr(), workspace_bytes,
+                                     _stream(stream))
+    if status:
+        _check(status)
 
 
 def qvla_check_device(stream=None) -> None:
