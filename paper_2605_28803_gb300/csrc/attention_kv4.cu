@@ -240,7 +240,16 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   const int k0 = ch * chunk, k1 = min(most, k0 + chunk);
   if (ch > 0 && k0 >= most && !p.cluster) return;  // (the CTAs of a cluster stay together)
 
-  // ---- the first cached tokens are asked for before the queries are worked on
+  // ---- the queries and the first cached tokens are asked for together
+  constexpr int kQRounds = (kRows + kTeams - 1) / kTeams;
+  uint4 q_raw[kQRounds];
+#pragma unroll
+  for (int i = 0; i < kQRounds; ++i) {
+    const int r = i * kTeams + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
+    const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
+    q_raw[i] = r < rows ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + token * a.q_stride + head * kDim + tl * 8))
+                        : make_uint4(0, 0, 0, 0);
+  }
   const uint32_t block = (kDim + 8u) << a.pool.log_page, stride = block * a.pool.kv_heads;  // of a head's page, of a page
   const uint8_t* const base = a.pool.base + static_cast<uint64_t>(kvh) * block;
   const int plane = kRow << a.pool.log_page, slots = (1 << a.pool.log_page) - 1;
@@ -300,11 +309,8 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
 #pragma unroll
   for (int r0 = 0; r0 < kRows; r0 += kTeams) {
     const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
-    float y[8] = {};
-    if (r < rows) {
-      const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
-      unpack8<T>(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + token * a.q_stride + head * kDim + tl * 8)), y);
-    }
+    float y[8];
+    unpack8<T>(q_raw[r0 / kTeams], y);
     if (a.pool.rotate) rotate_head<kTeam>(y);
     float top = 0.0f;
 #pragma unroll
@@ -627,18 +633,22 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   cluster_sync();  // nobody leaves while its result is being read
 }
 
-// The chunks of a query row (one head of one token) joined by a CTA: teams of D / 8 lanes take every kTeams-th chunk.
-template <typename T, int kDim>
+// The chunks of a query row (one head of one token) joined, teams of D / 8 lanes taking chunks in turn: by a CTA, where there are
+// many, or by a warp.
+template <typename T, int kDim, bool kMany>
 __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const __grid_constant__ Kv4Params p) {
-  constexpr int kTeam = kDim / 8, kTeams = 32 * kWarps / kTeam;
-  __shared__ float s_m[kTeams], s_l[kTeams];
-  __shared__ __align__(16) float s_y[kTeams][kDim];
+  constexpr int kTeam = kDim / 8, kWarpTeams = 32 / kTeam, kTeams = kMany ? kWarps * kWarpTeams : kWarpTeams;
+  __shared__ float s_m[kMany ? kWarps : 1], s_l[kMany ? kWarps : 1];
+  __shared__ __align__(16) float s_y[kMany ? kWarps : 1][kMany ? kDim : 1];
   const Kv4AttentionArgs& a = p.a;
-  const int token = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
-  const int team = threadIdx.x / kTeam, tl = threadIdx.x % kTeam;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tl = lane % kTeam;
+  const int row = kMany ? blockIdx.x : blockIdx.x * kWarps + warp;
+  if (row >= a.total_q * a.heads) return;
+  const int token = row / a.heads, head = row % a.heads;
+  const int team = (kMany ? warp * kWarpTeams : 0) + lane / kTeam;
   griddep_wait();
   griddep_launch_dependents();
-  const int lane = threadIdx.x & 31, len = lane < a.batch ? usable_length(a, __ldg(a.kv_len + lane)) : 0;
+  const int len = lane < a.batch ? usable_length(a, __ldg(a.kv_len + lane)) : 0;
   int b, first;
   if (!find_sequence(a.cu_q, a.batch, token, b, first)) return;
   const Sequence seq = load_sequence(a, b);
@@ -658,48 +668,62 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
   const float* const src = p.part + (unit * p.rows + r % p.rows) * (kDim + 2);
   const size_t next = static_cast<size_t>(p.per) * p.rows * (kDim + 2);
   float m = -FLT_MAX, l = 0.0f, y[8] = {};
+  auto add = [&](float m2, float l2, const float (&y2)[8]) {
+    const float top = fmaxf(m, m2), keep = ex2(m - top), k = ex2(m2 - top);
+    m = top;
+    l = l * keep + l2 * k;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = y[e] * keep + y2[e] * k;
+  };
 #pragma unroll 4
   for (int c = team; c < chunks; c += kTeams) {
     const float* const at = src + c * next;
     const float2 ml = *reinterpret_cast<const float2*>(at + kDim);
-    float2 v[4];
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float2*>(at + tl * 8 + 2 * e);
-    const float top = fmaxf(m, ml.x), keep = ex2(m - top), k = ex2(ml.x - top);
-    m = top;
-    l = l * keep + ml.y * k;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      y[2 * e] = y[2 * e] * keep + v[e].x * k;
-      y[2 * e + 1] = y[2 * e + 1] * keep + v[e].y * k;
+    for (int e = 0; e < 8; e += 2) {
+      const float2 w = *reinterpret_cast<const float2*>(at + tl * 8 + e);
+      v[e] = w.x;
+      v[e + 1] = w.y;
     }
-  }
-  if (tl == 0) {
-    s_m[team] = m;
-    s_l[team] = l;
+    add(ml.x, ml.y, v);
   }
 #pragma unroll
-  for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(&s_y[team][tl * 8 + e]) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-  __syncthreads();
-  if (threadIdx.x >= 32) return;
-  m = s_m[0];
-  l = 0.0f;
+  for (int h = kTeam; h < 32; h *= 2) {  // the warp's teams (a sum or maximum of two is the same on both sides)
+    float v[8];
+    const float m2 = __shfl_xor_sync(0xffffffffu, m, h), l2 = __shfl_xor_sync(0xffffffffu, l, h);
 #pragma unroll
-  for (int w = 1; w < kTeams; ++w) m = fmaxf(m, s_m[w]);
+    for (int e = 0; e < 8; ++e) v[e] = __shfl_xor_sync(0xffffffffu, y[e], h);
+    add(m2, l2, v);
+  }
+  if constexpr (kMany) {
+    if (lane < kTeam) {
+      if (tl == 0) {
+        s_m[warp] = m;
+        s_l[warp] = l;
+      }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = 0.0f;
+      for (int e = 0; e < 8; e += 4) *reinterpret_cast<float4*>(&s_y[warp][tl * 8 + e]) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+    }
+    __syncthreads();
+    if (warp > 0) return;
+    m = -FLT_MAX;
+    l = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kTeams; ++w) {
-    const float k = ex2(s_m[w] - m);
-    l += s_l[w] * k;
+    for (int e = 0; e < 8; ++e) y[e] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] += s_y[w][tl * 8 + e] * k;
+    for (int w = 0; w < kWarps; ++w) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = s_y[w][tl * 8 + e];
+      add(s_m[w], s_l[w], v);
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
   for (int c = 0; c < 8; ++c) y[c] *= inv;
   if (a.pool.rotate) rotate_head<kTeam>(y);
-  if (team == 0) *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+  if (lane < kTeam) *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
 }
 
 int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * (a.heads / a.pool.kv_heads) <= 8 ? 8 : 16; }
@@ -777,9 +801,13 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
   cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
   if (e != cudaSuccess) return e;
   if (p.target > 0) {
-    cfg.gridDim = dim3(static_cast<unsigned>(joins));
+    // about so many chunks a sequence: a CTA a row where a warp would take many rounds
+    const int64_t units = static_cast<int64_t>(a.batch) * p.per;
+    const bool many = p.target >= 8 * units;
+    cfg.gridDim = dim3(static_cast<unsigned>(many ? joins : (joins + kWarps - 1) / kWarps));
     cfg.dynamicSmemBytes = 0;
-    e = cudaLaunchKernelEx(&cfg, attention_kv4_join_kernel<T, kDim>, p);
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, many ? attention_kv4_join_kernel<T, kDim, true> : attention_kv4_join_kernel<T, kDim, false>, p);
     if (e != cudaSuccess) return e;
   }
   return cudaGetLastError();
