@@ -162,7 +162,7 @@ template <int kDim, int kTiles>
 struct Cfg {
   static constexpr int kRows = 8 * kTiles;
   static constexpr int kTeam = kDim / 8;                   // lanes that hold a head, 8 channels each
-  static constexpr int kQStride = kDim + 8;                // float16 of a staged query row
+  static constexpr int kQBytes = kRows * kDim * 2;         // the staged queries, in the order of the fragments
   // A step of 32 tokens halves the work around the matrix instructions, for as many registers as single tokens leave free.
   static constexpr int kParts = kTiles == 1 && kDim < 256 ? 2 : 1;
   static constexpr int kStep = kTile * kParts;              // cached tokens a warp takes at once
@@ -175,7 +175,7 @@ struct Cfg {
   static constexpr int kEighth = kDim / 8 + 2, kJoinRow = 8 * kEighth + 4;
   static constexpr int kJoin = kWarps * kRows * kJoinRow * 4;
   static constexpr int kPart = kRows * (kDim + 2) * 4;      // this CTA's result, for its cluster
-  static constexpr int kSmem = (kRing > kJoin + kPart ? kRing : kJoin + kPart) + kRows * kQStride * 2;
+  static constexpr int kSmem = (kRing > kJoin + kPart ? kRing : kJoin + kPart) + kQBytes;
 };
 
 template <typename T, int kDim, int kTiles>
@@ -187,11 +187,13 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   constexpr bool kQInRegs = kTiles * kDim <= 256;
   const Kv4AttentionArgs& a = p.a;
   extern __shared__ __align__(128) uint8_t s_raw[];
-  __half* const q_at = reinterpret_cast<__half*>(s_raw);                      // [kRows][kQStride]
-  uint8_t* const s_ring = s_raw + kRows * C::kQStride * 2;                    // [kWarps][kStages][kStepBytes]
+  // Queries as B fragments: of row tile n, word w (8 channels of each lane's quarter) and half c of it, a lane's two registers.
+  uint2* const q_at = reinterpret_cast<uint2*>(s_raw);
+  auto q_index = [](int n, int w, int c) { return ((n * (kDim / 32) + w) * 2 + c) * 32; };
+  uint8_t* const s_ring = s_raw + C::kQBytes;                                 // [kWarps][kStages][kStepBytes]
   float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kJoinRow] at the end
   float* const s_part = reinterpret_cast<float*>(s_ring + C::kJoin);          // [kRows][kDim + 2]
-  static_assert(kRows * C::kQStride * 2 % 128 == 0, "the ring's pieces are placed by 128-byte lines");
+  static_assert(C::kQBytes % 128 == 0, "the ring's pieces are placed by 128-byte lines");
   __shared__ float s_f[kRows], s_sum[kRows], s_m[kWarps][kRows], s_l[kWarps][kRows];
   __shared__ int s_end[kWarps][kStages][kParts];  // first token that nobody may use
 
@@ -331,7 +333,9 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
       }
       sum = total;
       __half2 v[4] = {__halves2half2(h[0], h[4]), __halves2half2(h[1], h[5]), __halves2half2(h[2], h[6]), __halves2half2(h[3], h[7])};
-      *reinterpret_cast<uint4*>(q_at + r * C::kQStride + tl * 8) = *reinterpret_cast<const uint4*>(v);
+      const int w = tl % (kDim / 32), at = (r & 7) * 4 + tl / (kDim / 32);
+      q_at[q_index(r >> 3, w, 0) + at] = *reinterpret_cast<const uint2*>(v);
+      q_at[q_index(r >> 3, w, 1) + at] = *reinterpret_cast<const uint2*>(v + 2);
     }
 #pragma unroll
     for (int h = 1; h < kTeam; h *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, h);
@@ -347,11 +351,11 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
       for (int w = 0; w < kDim / 32; ++w) {
-        const uint4 v = *reinterpret_cast<const uint4*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w);
-        q[n][4 * w] = v.x;
-        q[n][4 * w + 1] = v.y;
-        q[n][4 * w + 2] = v.z;
-        q[n][4 * w + 3] = v.w;
+        const uint2 lo = q_at[q_index(n, w, 0) + lane], hi = q_at[q_index(n, w, 1) + lane];
+        q[n][4 * w] = lo.x;
+        q[n][4 * w + 1] = lo.y;
+        q[n][4 * w + 2] = hi.x;
+        q[n][4 * w + 3] = hi.y;
       }
   }
   // this lane's rows of S^T and O^T: 8 n + 2 t and the next
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
             if constexpr (kQInRegs) {
               mma16816(kTiles == 1 && c ? x2 : x[h][n], a0, a1, a2, a3, q[n][4 * w + 2 * c], q[n][4 * w + 2 * c + 1]);
             } else {
-              const uint2 v = *reinterpret_cast<const uint2*>(q_at + (8 * n + g) * C::kQStride + t * (kDim / 4) + 8 * w + 4 * c);
+              const uint2 v = q_at[q_index(n, w, c) + lane];
               mma16816(x[h][n], a0, a1, a2, a3, v.x, v.y);
             }
           }
