@@ -17,7 +17,8 @@
 // float16 for the second product.  The row's reference r follows the largest w, not the largest p, so a weight has float16's
 // 11 bits whatever the scales' size; it moves when a w would pass 2^8 (or a p 2^96, where all scales are tiny).
 //   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
-// float16.
+// float16.  That is exact for a float16 query but for rotated ones; those are taken in two parts, or their rounding
+// would show beside a float16 output's (error 1.6 times that of float32 queries; beside a bfloat16 output's it does not).
 //
 // The cached tokens of a sequence are split into chunks over CTAs (of kWarps warps, each with every kWarps-th step).  The device
 // decides the chunks from the lengths it finds, so that a captured graph follows its lengths.  Two ways:
@@ -29,6 +30,7 @@
 
 #include <atomic>
 #include <cfloat>
+#include <type_traits>
 
 #include "griddep.cuh"
 #include "kv4.cuh"
@@ -158,11 +160,11 @@ __device__ __forceinline__ int64_t chunk_length(const Kv4Params& p, int len) {
   return length;
 }
 
-template <int kDim, int kTiles>
+template <int kDim, int kTiles, bool kSplitQ>
 struct Cfg {
   static constexpr int kRows = 8 * kTiles;
   static constexpr int kTeam = kDim / 8;                   // lanes that hold a head, 8 channels each
-  static constexpr int kQBytes = kRows * kDim * 2;         // the staged queries, in the order of the fragments
+  static constexpr int kQBytes = kRows * kDim * (kSplitQ ? 4 : 2);  // the staged queries, in the order of the fragments
   // A step of 32 tokens halves the work around the matrix instructions, for as many registers as single tokens leave free.
   static constexpr int kParts = kTiles == 1 && kDim < 256 ? 2 : 1;
   static constexpr int kStep = kTile * kParts;              // cached tokens a warp takes at once
@@ -178,9 +180,9 @@ struct Cfg {
   static constexpr int kSmem = (kRing > kJoin + kPart ? kRing : kJoin + kPart) + kQBytes;
 };
 
-template <typename T, int kDim, int kTiles>
+template <typename T, int kDim, int kTiles, bool kSplitQ>
 __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) attention_kv4_kernel(const __grid_constant__ Kv4Params p) {
-  using C = Cfg<kDim, kTiles>;
+  using C = Cfg<kDim, kTiles, kSplitQ>;
   constexpr int kRows = C::kRows, kTeam = C::kTeam, kTeams = 32 * kWarps / kTeam, kStages = C::kStages, kParts = C::kParts,
                 kStep = C::kStep;
   constexpr int kRow = kDim / 2;  // bytes of a token's codes
@@ -189,6 +191,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   extern __shared__ __align__(128) uint8_t s_raw[];
   // Queries as B fragments: of row tile n, word w (8 channels of each lane's quarter) and half c of it, a lane's two registers.
   uint2* const q_at = reinterpret_cast<uint2*>(s_raw);
+  constexpr int kRest = kRows * kDim / 4;  // where what float16 leaves of the queries lies
   auto q_index = [](int n, int w, int c) { return ((n * (kDim / 32) + w) * 2 + c) * 32; };
   uint8_t* const s_ring = s_raw + C::kQBytes;                                 // [kWarps][kStages][kStepBytes]
   float* const s_o = reinterpret_cast<float*>(s_ring);                        // [kWarps][kRows][kJoinRow] at the end
@@ -323,19 +326,25 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
     const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
     float sum = 0.0f;  // of the rounded queries
     if (r < kRows) {
-      __half h[8];
+      __half h[8], rest[8];
       float total = 0.0f;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {  // nibbles 1, 3, 5, 7 are read 16 times too large
         const float part = (c & 1) ? 0.0625f : 1.0f;
         h[c] = __float2half_rn(y[c] * down * part);
-        total += __half2float(h[c]) * (c & 1 ? 16.0f : 1.0f);
+        rest[c] = __float2half_rn(y[c] * down * part - __half2float(h[c]));
+        total += (__half2float(h[c]) + (kSplitQ ? __half2float(rest[c]) : 0.0f)) * (c & 1 ? 16.0f : 1.0f);
       }
       sum = total;
       __half2 v[4] = {__halves2half2(h[0], h[4]), __halves2half2(h[1], h[5]), __halves2half2(h[2], h[6]), __halves2half2(h[3], h[7])};
       const int w = tl % (kDim / 32), at = (r & 7) * 4 + tl / (kDim / 32);
       q_at[q_index(r >> 3, w, 0) + at] = *reinterpret_cast<const uint2*>(v);
       q_at[q_index(r >> 3, w, 1) + at] = *reinterpret_cast<const uint2*>(v + 2);
+      if constexpr (kSplitQ) {
+        __half2 u[4] = {__halves2half2(rest[0], rest[4]), __halves2half2(rest[1], rest[5]), __halves2half2(rest[2], rest[6]), __halves2half2(rest[3], rest[7])};
+        q_at[kRest + q_index(r >> 3, w, 0) + at] = *reinterpret_cast<const uint2*>(u);
+        q_at[kRest + q_index(r >> 3, w, 1) + at] = *reinterpret_cast<const uint2*>(u + 2);
+      }
     }
 #pragma unroll
     for (int h = 1; h < kTeam; h *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, h);
@@ -434,6 +443,10 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
             } else {
               const uint2 v = q_at[q_index(n, w, c) + lane];
               mma16816(x[h][n], a0, a1, a2, a3, v.x, v.y);
+            }
+            if constexpr (kSplitQ) {
+              const uint2 v = q_at[kRest + q_index(n, w, c) + lane];
+              mma16816(kTiles == 1 && !c ? x2 : x[h][n], a0, a1, a2, a3, v.x, v.y);
             }
           }
           k[0][w] >>= 8;
@@ -766,7 +779,7 @@ cudaError_t plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p)
   return cudaSuccess;
 }
 
-template <typename T, int kDim, int kTiles>
+template <typename T, int kDim, int kTiles, bool kSplitQ>
 cudaError_t launch(const Kv4AttentionArgs& a) {
   Kv4Params p;
   p.a = a;
@@ -774,8 +787,8 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
   p.part = static_cast<float*>(a.ws);
   const int64_t joins = static_cast<int64_t>(a.total_q) * a.heads;
   if (joins > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  using C = Cfg<kDim, kTiles>;
-  auto kern = attention_kv4_kernel<T, kDim, kTiles>;
+  using C = Cfg<kDim, kTiles, kSplitQ>;
+  auto kern = attention_kv4_kernel<T, kDim, kTiles, kSplitQ>;
   if (C::kSmem > 48 * 1024) {  // once a device
     static std::atomic<uint64_t> raised{0};
     int dev = 0;
@@ -819,7 +832,9 @@ cudaError_t launch(const Kv4AttentionArgs& a) {
 
 template <typename T, int kDim>
 cudaError_t launch(const Kv4AttentionArgs& a) {
-  return rows_of(a) == 8 ? launch<T, kDim, 1>(a) : launch<T, kDim, 2>(a);
+  if (std::is_same<T, __half>::value && a.pool.rotate)
+    return rows_of(a) == 8 ? launch<T, kDim, 1, std::is_same<T, __half>::value>(a) : launch<T, kDim, 2, std::is_same<T, __half>::value>(a);
+  return rows_of(a) == 8 ? launch<T, kDim, 1, false>(a) : launch<T, kDim, 2, false>(a);
 }
 
 }  // namespace
