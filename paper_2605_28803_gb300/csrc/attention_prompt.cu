@@ -12,6 +12,9 @@
 // The maximum that P is taken against moves only when a row's maximum has grown by more than 2^8 (p <= 256 is harmless in
 // both types, and numerator and denominator use the same one), so O is rarely read back to be rescaled.
 //
+// Where a launch would leave SMs idle, a cluster of CTAs shares a group of tiles: each takes a run of the key blocks, and their O,
+// maxima and sums are joined through distributed shared memory.
+//
 // Keys that some row of the CTA does not see (the diagonal's blocks, a sequence's last block) need care on the value side, where
 // 0 * NaN would spread: two warps zero the rows behind the sequence's end and take NaN and infinities out of such
 // blocks; a row that does see one of those gets it back, exactly, when it is written out.
@@ -19,6 +22,7 @@
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <mutex>
 #include <set>
 #include <utility>
@@ -35,6 +39,8 @@ static __device__ int g_debug_hold_loads;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowsPerTile = 128;
 constexpr float kGrowth = 8.0f;  // log2 of what a row's maximum may grow by before its O is rescaled
+constexpr int kLeastKeys = 256;  // of a CTA where a cluster shares a sequence's, which then has at least kSplitKeys
+constexpr int kSplitKeys = 1024;
 constexpr int kWarpLoad = 0, kWarpMma = 1, kWarpGuard = 2, kGuardWarps = 2, kWarpSoftmax = 4;
 
 template <int kDim>
@@ -48,6 +54,9 @@ struct Shape {
   static constexpr int kQBytes = kQTmem ? 0 : kRowsPerTile * kDim * 2;  // one tile in shared memory
   static constexpr int kKvBytes = kBlock * kDim * 2;          // one block of K or V
   static constexpr int kSmem = kTiles * kQBytes + (kStagesK + kStagesV) * kKvBytes + 1024;
+  // a cluster's join: O in float32, rows kORow apart (which spreads a column over the banks), then maximum and sum of each row
+  static constexpr int kORow = kDim + 4, kOBytes = kTiles * kRowsPerTile * kORow * 4;
+  static_assert(kOBytes + kTiles * kRowsPerTile * 8 + 1024 <= kSmem, "the join fits over the operands");
   static constexpr int kOCol = 2 * kBlock, kQCol = kOCol + kTiles * kDim;  // TMEM: two S buffers, O of each tile, Q
 };
 
@@ -63,6 +72,7 @@ struct PromptParams {
   int chunk_heads, chunks;     // of them in one tile; tiles' head chunks
   int tokens;                  // tokens in one tile
   int causal;
+  int split;                   // CTAs of a cluster, which share the keys of a group of tiles
   float c;                     // scale * log2(e)
 };
 
@@ -101,12 +111,75 @@ __device__ __forceinline__ bool any_not_finite(uint32_t w) {
   return (((w & e) + one) & 0x80008000u) != 0;  // an exponent of all ones carries into the sign's place
 }
 
+__device__ __forceinline__ float2 cluster_load2(uint32_t at) {  // of a CTA of the cluster (address from mapa_shared)
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 cluster_load4(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+template <int kThreads>
+__device__ __forceinline__ void softmax_sync() {  // the softmax warps meet
+  asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+}
+
 // Keys that query token i of its sequence sees.
 __device__ __forceinline__ int seen_by(const Work& w, int causal, int i) {
   return causal ? max(0, min(w.keys, w.keys - w.n + i + 1)) : w.keys;
 }
 
-template <typename T, int kDim>
+// The rows of a cluster's tiles that fall to CTA `rank` of it, four channels a thread: O, maxima and sums of up to kCtas CTAs
+// are asked for at once, for kAhead places at a time (a row after the other took 8 us of a launch, this 3).
+template <typename T, int kDim, int kCtas, int kAhead>
+__device__ __forceinline__ void join(const PromptParams& p, const Work& w, const uint8_t* smem, int rank) {
+  using C = Shape<kDim>;
+  constexpr int kPer = kDim / 4, kRows = C::kTiles * kRowsPerTile;
+  const int step = p.split * C::kThreads;
+  uint32_t at[kCtas];
+#pragma unroll
+  for (int c = 0; c < kCtas; ++c) at[c] = mapa_shared(smem_u32(smem), static_cast<uint32_t>(min(c, p.split - 1)));
+  for (int u0 = rank * C::kThreads + threadIdx.x; u0 < kRows * kPer; u0 += kAhead * step) {
+    float2 ms[kAhead][kCtas];
+    float4 v[kAhead][kCtas];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int u = min(u0 + a * step, kRows * kPer - 1), r = u / kPer, e = u % kPer * 4;
+#pragma unroll
+      for (int c = 0; c < kCtas; ++c) {
+        ms[a][c] = cluster_load2(at[c] + C::kOBytes + r * 8);
+        v[a][c] = cluster_load4(at[c] + static_cast<uint32_t>((r * C::kORow + e) * 4));
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int u = u0 + a * step, r = u / kPer, e = u % kPer * 4, t = r / kRowsPerTile, row = r % kRowsPerTile;
+      const int token = w.token + t * p.tokens + row / p.chunk_heads, head = row % p.chunk_heads;
+      bool live = u < kRows * kPer && row < p.tokens * p.chunk_heads && token < w.n && head < w.heads;
+      float m = -INFINITY, sum = 0.0f, y[4] = {};
+#pragma unroll
+      for (int c = 0; c < kCtas; ++c) {
+        if (c >= p.split || ms[a][c].y == 0.0f) continue;  // this CTA's keys are none that the row sees
+        if (ms[a][c].y < 0.0f) live = false;               // a wait of that CTA ran out
+        const float top = fmaxf(m, ms[a][c].x), keep = m == -INFINITY ? 0.0f : ex2(m - top), k = ex2(ms[a][c].x - top);
+        m = top;
+        sum = sum * keep + ms[a][c].y * k;
+        y[0] = y[0] * keep + v[a][c].x * k;
+        y[1] = y[1] * keep + v[a][c].y * k;
+        y[2] = y[2] * keep + v[a][c].z * k;
+        y[3] = y[3] * keep + v[a][c].w * k;
+      }
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      if (live)
+        *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + (static_cast<size_t>(w.q0 + token) * p.heads + w.head + head) * kDim + e) =
+            make_uint2(pack2<T>(y[0] * inv, y[1] * inv), pack2<T>(y[2] * inv, y[3] * inv));
+    }
+  }
+}
+
+template <typename T, int kDim, bool kSplit>
 __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
     attention_prompt_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                             const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ PromptParams p) {
@@ -158,8 +231,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
   griddep_wait();  // the offsets, q, k and v may come from the previous kernel, which may still read o
   if (warp == 0) {  // the sequence and tile of this CTA: 32 sequences a round, the last tiles of a sequence first
     const int per = p.kv_heads * p.chunks;
-    int tile = static_cast<int>(blockIdx.x / per);
-    const int rest = static_cast<int>(blockIdx.x % per);
+    const int cta = static_cast<int>(blockIdx.x) / (kSplit ? p.split : 1);
+    int tile = cta / per;
+    const int rest = cta % per;
     bool found = false;
     for (int b0 = 0; b0 < p.batch && !found; b0 += 32) {
       const int b = b0 + lane;
@@ -203,16 +277,27 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
   griddep_launch_dependents();
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);  // (values that the compiler knows to be the same in every lane)
   if (__shfl_sync(0xffffffffu, s_found, 0)) {
-    const Work w = s_work;
+    Work w = s_work;
     // per tile: blocks to run, and the first of them that some row does not see whole
     int blocks[kTiles], partial[kTiles], most = 0, guard_from = 1 << 30;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const int first = w.token + t * p.tokens, last = min(first + p.tokens, w.n) - 1;
       blocks[t] = first < w.n ? (seen_by(w, p.causal, last) + kBlock - 1) / kBlock : 0;
-      partial[t] = seen_by(w, p.causal, first) / kBlock;
       blocks[t] = __shfl_sync(0xffffffffu, blocks[t], 0);
       most = max(most, blocks[t]);
+    }
+    if constexpr (kSplit) {  // this CTA's run of the blocks: from here on the keys begin with it
+      const int run = (most + p.split - 1) / p.split, from = static_cast<int>(blockIdx.x) % p.split * run;
+      w.k0 += from * kBlock;
+      w.keys -= from * kBlock;
+      most = max(0, min(run, most - from));
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) blocks[t] = max(0, min(blocks[t] - from, most));
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      partial[t] = seen_by(w, p.causal, w.token + t * p.tokens) / kBlock;
       if (blocks[t] > 0) guard_from = min(guard_from, partial[t]);
     }
 
@@ -485,8 +570,38 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         ok = o_has(n - 1);
         tc_fence_after();
       }
-      if (ok) {
-        const bool bad = *const_cast<volatile int*>(&s_bad) != 0;
+      const bool bad = *const_cast<volatile int*>(&s_bad) != 0;
+      const int seen_here = min(seen, most * kBlock);
+      auto add_bad = [&](float (&y)[32], int i) {  // the NaN and infinities that the guard took out and this row sees
+        for (int key = guard_from * kBlock; key < seen_here; ++key) {
+          const T* src = static_cast<const T*>(p.v) + (w.k0 + key) * p.v_stride + w.kvh * kDim + i * 32;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float x = static_cast<float>(src[e]);
+            if (!(fabsf(x) < INFINITY)) y[e] += x;
+          }
+        }
+      };
+      if constexpr (kSplit) {
+        // every product of the CTA is done once all its rows are here: O goes over the operands, for the cluster to read
+        softmax_sync<128 * kTiles>();
+        float* const dst = reinterpret_cast<float*>(smem) + (t * kRowsPerTile + row) * C::kORow;
+        reinterpret_cast<float2*>(smem + C::kOBytes)[t * kRowsPerTile + row] = make_float2(m, n <= 0 ? 0.0f : ok ? sum : -1.0f);
+        if (ok && n > 0) {
+#pragma unroll 1
+          for (int i = 0; i < kDim / 32; ++i) {
+            uint32_t r[32];
+            tmem_ld32(o_at + i * 32, r);
+            tmem_ld_wait();
+            float y[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(r[e]);
+            if (bad && live) add_bad(y, i);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + i * 32 + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+          }
+        }
+      } else if (ok) {
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         T* const dst = static_cast<T*>(p.o) + (static_cast<size_t>(w.q0 + token) * p.heads + w.head + head) * kDim;
 #pragma unroll 2
@@ -499,16 +614,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           }
 #pragma unroll
           for (int e = 0; e < 32; ++e) y[e] = n > 0 ? __uint_as_float(r[e]) * inv : 0.0f;
-          if (bad && live) {  // the NaN and infinities that the guard took out and this row sees
-            for (int key = guard_from * kBlock; key < seen; ++key) {
-              const T* src = static_cast<const T*>(p.v) + (w.k0 + key) * p.v_stride + w.kvh * kDim + i * 32;
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const float x = static_cast<float>(src[e]);
-                if (!(fabsf(x) < INFINITY)) y[e] += x;
-              }
-            }
-          }
+          if (bad && live) add_bad(y, i);
           if (live) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
@@ -523,6 +629,17 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         }
       }
       tc_fence_before();
+    }
+    if constexpr (kSplit) {
+      // ------------------------------------------------------------------ the cluster's join
+      __syncwarp();
+      cluster_sync();
+      const int rank = static_cast<int>(blockIdx.x) % p.split;
+      if (p.split == 2) join<T, kDim, 2, 4>(p, w, smem, rank);
+      else if (p.split <= 4) join<T, kDim, 4, 2>(p, w, smem, rank);
+      else join<T, kDim, 8, 1>(p, w, smem, rank);
+      __syncwarp();
+      cluster_sync();  // nobody leaves while its rows are being read
     }
   }
   __syncthreads();
@@ -572,12 +689,41 @@ cudaError_t prepare_kernel(const void* kern, int smem) {
   return e;
 }
 
+// Clusters of `size` CTAs that the current device holds at once (asked once a size and device); 0 if it cannot tell.
+template <typename T, int kDim>
+int resident_clusters(int size) {
+  using C = Shape<kDim>;
+  constexpr int kDevices = 32;
+  static std::atomic<int> known[kDevices][9];  // count + 1
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return 0;
+  const int seen = known[dev][size].load(std::memory_order_relaxed);
+  if (seen > 0) return seen - 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(size));
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(size);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  auto kern = attention_prompt_kernel<T, kDim, true>;
+  if (prepare_kernel(reinterpret_cast<const void*>(kern), C::kSmem) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+    cudaGetLastError();  // (plain launches do without)
+    n = 0;
+  }
+  known[dev][size].store(n + 1, std::memory_order_relaxed);
+  return n;
+}
+
 template <typename T, int kDim>
 cudaError_t launch(const PromptArgs& a) {
   using C = Shape<kDim>;
-  auto kern = attention_prompt_kernel<T, kDim>;
-  cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kern), C::kSmem);
-  if (e != cudaSuccess) return e;
   PromptParams p;
   p.cu_q = a.cu_q;
   p.cu_k = a.cu_k;
@@ -601,7 +747,7 @@ cudaError_t launch(const PromptArgs& a) {
   // without keys nothing is loaded; the maps still need a valid base
   const int bf16 = std::is_same<T, __half>::value ? 0 : 1, keys = a.total_k > 0 ? a.total_k : 1;
   CUtensorMap tq = {}, tk = {}, tv = {};
-  e = make_tmap_heads(&tq, a.q, bf16, kDim, a.heads, a.total_q, a.q_stride, p.chunk_heads, p.tokens);
+  cudaError_t e = make_tmap_heads(&tq, a.q, bf16, kDim, a.heads, a.total_q, a.q_stride, p.chunk_heads, p.tokens);
   if (e == cudaSuccess) e = make_tmap_heads(&tk, a.total_k > 0 ? a.k : a.q, bf16, kDim, a.kv_heads, keys, a.k_stride, 1, C::kBlock);
   if (e == cudaSuccess) e = make_tmap_heads(&tv, a.total_k > 0 ? a.v : a.q, bf16, kDim, a.kv_heads, keys, a.v_stride, 1, C::kBlock);
   if (e != cudaSuccess) return e;
@@ -610,16 +756,32 @@ cudaError_t launch(const PromptArgs& a) {
   const int64_t groups = (a.total_q + static_cast<int64_t>(a.batch) * (per - 1)) / per;
   const int64_t ctas = groups * a.kv_heads * p.chunks;
   if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  // Where CTAs would leave SMs idle and sequences of middling length have kSplitKeys keys, a cluster a group of tiles: as large as
+  // the SMs hold at once, with at least kLeastKeys keys a CTA. Clusters against CTAs, us, 8 heads of 128 channels on one: 64 tokens
+  // on 2000 keys 17.1 against 27.6, 1500 on 1500 20.1 against 23.0, but 816 on 816 16.8 against 15.8: the join takes 3 to 4.
+  const int64_t middling = a.total_k / a.batch;
+  int64_t split = middling < kSplitKeys ? 1 : a.num_sms / ctas;
+  if (split > middling / kLeastKeys) split = middling / kLeastKeys;
+  if (split > 8) split = 8;
+  while (split > 1 && resident_clusters<T, kDim>(static_cast<int>(split)) < ctas) --split;
+  p.split = split < 2 ? 1 : static_cast<int>(split);
+  auto kern = p.split > 1 ? attention_prompt_kernel<T, kDim, true> : attention_prompt_kernel<T, kDim, false>;
+  e = prepare_kernel(reinterpret_cast<const void*>(kern), C::kSmem);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas * p.split));
   cfg.blockDim = dim3(C::kThreads);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = a.stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(p.split);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.split > 1 ? 2 : 1;
   e = cudaLaunchKernelEx(&cfg, kern, tq, tk, tv, p);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();

@@ -68,6 +68,45 @@ def test_long_prompt_with_growing_scores(dim):
     check(q, k, v, [n], [n], False)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", [
+    (8, 1, 256, "bf16", [40], [1100]),  # a key range of several CTAs' worth for a tile or two
+    (8, 2, 128, "f16", [300], [1500]),
+    (6, 6, 64, "bf16", [1], [2048]),
+    (4, 2, 64, "f16", [17, 0, 200], [1900, 1500, 90]),  # long, without queries, and shorter than one CTA's share
+    (4, 1, 128, "bf16", [1300], [1030]),  # the first 270 queries see nothing where it is causal
+    (140, 1, 64, "bf16", [3], [1025]),
+], ids=lambda c: "-".join(map(str, c[:4])))
+def test_few_queries_on_long_sequences(case, causal):
+    heads, kv, dim, dt, lens_q, lens_k = case
+    rng = np.random.default_rng(heads * 77 + dim)
+    q = H.draw_heads(rng, sum(lens_q), heads, dim, dt)
+    k = H.draw_heads(rng, sum(lens_k), kv, dim, dt, outliers=True)
+    v = H.draw_heads(rng, sum(lens_k), kv, dim, dt)
+    check(q, k, v, lens_q, lens_k, causal)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_what_a_query_does_not_see_on_a_long_sequence(dim):
+    """NaN in keys and values behind the last query of interest, an infinite value that only the last rows see."""
+    rng = np.random.default_rng(dim + 1)
+    n, m = 30, 1400
+    q = H.draw_heads(rng, n, 2, dim, "bf16").to(H.DEV)
+    k = H.draw_heads(rng, m + 100, 1, dim, "bf16").to(H.DEV)
+    v = H.draw_heads(rng, m + 100, 1, dim, "bf16").to(H.DEV)
+    cu_k = H.ints([0, m])
+    clean = H.prompt(q, k, v, [n], [m], True, cu_k=cu_k)
+    k2, v2 = k.clone(), v.clone()
+    k2[m - 5:], v2[m - 5:] = float("nan"), float("nan")
+    v2[m - 10, 0, 3] = float("inf")
+    got = H.prompt(q, k2, v2, [n], [m], True, cu_k=cu_k)
+    Q.qvla_check_device(H.stream())
+    assert torch.equal(got[: n - 10], clean[: n - 10])
+    assert (got[n - 10: n - 5, :, 3] == float("inf")).all()
+    assert torch.equal(got[n - 10: n - 5, :, 4:], clean[n - 10: n - 5, :, 4:])
+    assert torch.isnan(got[n - 5:].float()).all()
+
+
 def test_scores_of_one_size_and_a_large_scale():
     rng = np.random.default_rng(5)
     q = torch.zeros(40, 2, 64, dtype=torch.float16)
