@@ -121,11 +121,12 @@ __device__ __forceinline__ void copy_wait() {
 struct Sequence {
   int q0, n, len;
 };
+template <bool kL2 = false>
 __device__ __forceinline__ Sequence load_sequence(const Kv4AttentionArgs& a, int b) {
   Sequence s;
-  s.q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q);
-  s.n = min(max(__ldg(a.cu_q + b + 1), s.q0), a.total_q) - s.q0;
-  s.len = __ldg(a.kv_len + b);
+  s.q0 = min(max(read_index<kL2>(a.cu_q + b), 0), a.total_q);
+  s.n = min(max(read_index<kL2>(a.cu_q + b + 1), s.q0), a.total_q) - s.q0;
+  s.len = read_index<kL2>(a.kv_len + b);
   return s;
 }
 // False where it exceeds the launch's bounds and is to be skipped.
@@ -135,27 +136,37 @@ __device__ __forceinline__ int seen_by(const Sequence& s, int causal, int i) { r
 
 // The split: every sequence gets one chunk for each started `length` tokens, of equal size.
 __device__ __forceinline__ int usable_length(const Kv4AttentionArgs& a, int len) { return min(max(len, 0), a.max_len); }
-__device__ __forceinline__ int chunks_of(int len, int64_t length) { return len <= length ? 1 : static_cast<int>((len + length - 1) / length); }
+__device__ __forceinline__ int chunks_of(int len, int length) {
+  return len <= length ? 1 : static_cast<int>((static_cast<unsigned>(len) + length - 1u) / static_cast<unsigned>(length));
+}
 __device__ __forceinline__ int chunk_size(int len, int chunks) {
-  return ((len + chunks - 1) / chunks + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
+  const unsigned even = (static_cast<unsigned>(len) + chunks - 1u) / static_cast<unsigned>(chunks);
+  return static_cast<int>((even + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
 }
 // The same in every CTA of both kernels; `len`: of sequence `lane` (0 where there is none), loaded already.
-__device__ __forceinline__ int64_t chunk_length(const Kv4Params& p, int len) {
-  if (p.target == 0) return int64_t{1} << 31;
+template <bool kL2 = false>
+__device__ __forceinline__ int chunk_length(const Kv4Params& p, int len) {
+  constexpr int kMost = 1 << 30;  // no context is longer
+  if (p.target == 0) return kMost;
   int64_t all = len;
-  for (int b = 32 + static_cast<int>(threadIdx.x & 31); b < p.a.batch; b += 32) all += usable_length(p.a, __ldg(p.a.kv_len + b));
+  for (int b = 32 + static_cast<int>(threadIdx.x & 31); b < p.a.batch; b += 32) all += usable_length(p.a, read_index<kL2>(p.a.kv_len + b));
 #pragma unroll
   for (int h = 1; h < 32; h *= 2) all += __shfl_xor_sync(0xffffffffu, all, h);
   const int target = all * p.per > static_cast<int64_t>(p.target) * kLongChunk ? p.most_target : p.target;
-  auto rounded = [](int64_t v) { return max(static_cast<int64_t>(kLeastChunk), (v + kLeastChunk - 1) / kLeastChunk * kLeastChunk); };
-  int64_t length = rounded((all * p.per + target - 1) / target);
+  // n * m / target, never less (a float's quotient with what four roundings can take off), in whole kLeastChunk
+  auto share = [&](float n, int m) {
+    const float v = n * static_cast<float>(m) / static_cast<float>(target) * (1.0f + 0x1p-20f);
+    const int up = v < static_cast<float>(kMost - kLeastChunk) ? static_cast<int>(v) + 1 : kMost;
+    return (up + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
+  };
+  int length = max(kLeastChunk, share(static_cast<float>(all), p.per));
   // the remainders of the sequences come on top: lengthen the chunks until all fit the target, so that no CTA is left for a wave
   // of its own (a few tries, where the lengths are at hand)
   const int lane = static_cast<int>(threadIdx.x & 31);
   for (int i = 0; i < 4 && p.a.batch <= 32; ++i) {
-    const int64_t ctas = static_cast<int64_t>(__reduce_add_sync(0xffffffffu, lane < p.a.batch ? chunks_of(len, length) : 0)) * p.per;
+    const int ctas = __reduce_add_sync(0xffffffffu, lane < p.a.batch ? chunks_of(len, length) : 0) * p.per;
     if (ctas <= target) break;
-    length = rounded(length * ctas / target + 1);
+    length = share(static_cast<float>(length), ctas);
   }
   return length;
 }
@@ -215,7 +226,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
     chunk = max(kLeastChunk, chunk_size(usable_length(a, seq.len), p.cluster));
   } else {
     if (lane < a.batch) seq = load_sequence(a, lane);
-    const int64_t length = chunk_length(p, usable_length(a, seq.len));
+    const int length = chunk_length(p, usable_length(a, seq.len));
     for (int b0 = 0; b0 < a.batch && b < 0; b0 += 32) {
       if (b0 > 0 && b0 + lane < a.batch) seq = load_sequence(a, b0 + lane);
       const int len = usable_length(a, seq.len), n = b0 + lane < a.batch ? chunks_of(len, length) : 0;
@@ -660,27 +671,33 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
   const Kv4AttentionArgs& a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tl = lane % kTeam;
   const int row = kMany ? blockIdx.x : blockIdx.x * kWarps + warp;
-  if (row >= a.total_q * a.heads) return;
   const int token = row / a.heads, head = row % a.heads;
   const int team = (kMany ? warp * kWarpTeams : 0) + lane / kTeam;
+  // Where the row's parts lie follows from offsets and lengths.  They can be read ahead of the wait: this kernel starts once all CTAs
+  // of the other one are past their own wait, so what wrote them has ended.
+  int b = 0, first = 0, chunks = 0, before = 0, kvh = 0, r = 0, tile = 0;
+  if (row < a.total_q * a.heads) {
+    const int len = lane < a.batch ? usable_length(a, read_index<true>(a.kv_len + lane)) : 0;
+    const bool found = find_sequence<true>(a.cu_q, a.batch, token, b, first);
+    const Sequence seq = load_sequence<true>(a, b);
+    if (found && usable(a, seq) && seq.q0 == first) {
+      const int length = chunk_length<true>(p, len);
+      const int chunk = chunk_size(seq.len, chunks_of(seq.len, length));
+      kvh = head / p.group;
+      r = (token - first) * p.group + head % p.group;
+      tile = r / p.rows;
+      const int most = seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group);
+      chunks = (most + chunk - 1) / max(chunk, 1);
+      for (int b0 = 0; b0 < b; b0 += 32) {  // chunks of the sequences ahead
+        const int at = b0 + lane;
+        before += __reduce_add_sync(
+            0xffffffffu, at < b ? chunks_of(b0 == 0 ? len : usable_length(a, read_index<true>(a.kv_len + at)), length) : 0);
+      }
+    }
+  }
   griddep_wait();
   griddep_launch_dependents();
-  const int len = lane < a.batch ? usable_length(a, __ldg(a.kv_len + lane)) : 0;
-  int b, first;
-  if (!find_sequence(a.cu_q, a.batch, token, b, first)) return;
-  const Sequence seq = load_sequence(a, b);
-  if (!usable(a, seq) || seq.q0 != first) return;
-  const int64_t length = chunk_length(p, len);
-  const int chunk = chunk_size(seq.len, chunks_of(seq.len, length));
-  const int kvh = head / p.group, r = (token - first) * p.group + head % p.group, tile = r / p.rows;
-  const int most = seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group);
-  const int chunks = (most + chunk - 1) / max(chunk, 1);
-  if (chunks < 2) return;  // its CTA has written the result
-  int before = 0;  // chunks of the sequences ahead
-  for (int b0 = 0; b0 < b; b0 += 32) {
-    const int at = b0 + lane;
-    before += __reduce_add_sync(0xffffffffu, at < b ? chunks_of(b0 == 0 ? len : usable_length(a, __ldg(a.kv_len + at)), length) : 0);
-  }
+  if (chunks < 2) return;  // its CTA has written the result, or nobody has to
   const size_t unit = static_cast<size_t>(before) * p.per + kvh * p.row_tiles + tile;
   const float* const src = p.part + (unit * p.rows + r % p.rows) * (kDim + 2);
   const size_t next = static_cast<size_t>(p.per) * p.rows * (kDim + 2);

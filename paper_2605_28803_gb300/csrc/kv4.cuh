@@ -11,21 +11,29 @@
 
 namespace qvla {
 
+// An offset or length; kL2: past the first-level cache, where the kernel has not waited for the previous one yet.
+template <bool kL2>
+__device__ __forceinline__ int read_index(const int32_t* p) {
+  if constexpr (kL2) return __ldcg(p);
+  return __ldg(p);
+}
+
 // The sequence of packed row t: the last b with cu[b] <= t, found by the whole warp, 32 offsets a round.  False when t lies in
 // no sequence.  Any contents of cu are safe: b stays in [0, batch).
+template <bool kL2 = false>
 __device__ __forceinline__ bool find_sequence(const int32_t* __restrict__ cu, int batch, int t, int& b, int& first) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = batch;
   while (n > 1) {
     const int step = (n + 31) >> 5;
-    const bool at_or_before = lane * step < n && __ldg(cu + lo + lane * step) <= t;
+    const bool at_or_before = lane * step < n && read_index<kL2>(cu + lo + lane * step) <= t;
     const int c = max(1, __popc(__ballot_sync(0xffffffffu, at_or_before)));
     lo += (c - 1) * step;
     n = min(step, n - (c - 1) * step);
   }
   b = lo;
-  first = __ldg(cu + lo);
-  return first <= t && t < __ldg(cu + lo + 1);
+  first = read_index<kL2>(cu + lo);
+  return first <= t && t < read_index<kL2>(cu + lo + 1);
 }
 
 __device__ __forceinline__ void report_index() { atomicOr(&g_error_word, kErrIndex); }
