@@ -136,39 +136,41 @@ __device__ __forceinline__ int seen_by(const Sequence& s, int causal, int i) { r
 
 // The split: every sequence gets one chunk for each started `length` tokens, of equal size.
 __device__ __forceinline__ int usable_length(const Kv4AttentionArgs& a, int len) { return min(max(len, 0), a.max_len); }
-__device__ __forceinline__ int chunks_of(int len, int length) {
-  return len <= length ? 1 : static_cast<int>((static_cast<unsigned>(len) + length - 1u) / static_cast<unsigned>(length));
-}
+// (a quotient in float, never above the exact one)
+__device__ __forceinline__ int chunks_of(int len, float per_length) { return 1 + static_cast<int>(static_cast<float>(len - 1) * per_length); }
 __device__ __forceinline__ int chunk_size(int len, int chunks) {
   const unsigned even = (static_cast<unsigned>(len) + chunks - 1u) / static_cast<unsigned>(chunks);
   return static_cast<int>((even + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
 }
-// The same in every CTA of both kernels; `len`: of sequence `lane` (0 where there is none), loaded already.
+// 1 / length, the same in every CTA of both kernels; `len`: of sequence `lane` (0 where there is none), loaded already.
 template <bool kL2 = false>
-__device__ __forceinline__ int chunk_length(const Kv4Params& p, int len) {
-  constexpr int kMost = 1 << 30;  // no context is longer
-  if (p.target == 0) return kMost;
-  int64_t all = len;
-  for (int b = 32 + static_cast<int>(threadIdx.x & 31); b < p.a.batch; b += 32) all += usable_length(p.a, read_index<kL2>(p.a.kv_len + b));
-#pragma unroll
-  for (int h = 1; h < 32; h *= 2) all += __shfl_xor_sync(0xffffffffu, all, h);
-  const int target = all * p.per > static_cast<int64_t>(p.target) * kLongChunk ? p.most_target : p.target;
-  // n * m / target, never less (a float's quotient with what four roundings can take off), in whole kLeastChunk
-  auto share = [&](float n, int m) {
-    const float v = n * static_cast<float>(m) / static_cast<float>(target) * (1.0f + 0x1p-20f);
-    const int up = v < static_cast<float>(kMost - kLeastChunk) ? static_cast<int>(v) + 1 : kMost;
-    return (up + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
+__device__ __forceinline__ float split_of(const Kv4Params& p, int len) {
+  if (p.target == 0) return 0.0f;
+  constexpr float kLess = 1.0f - 0x1p-20f;  // more than the roundings of a quotient can add
+  const int lane = static_cast<int>(threadIdx.x & 31);
+  uint32_t low = len & 0xffff, high = len >> 16;  // (65535 sequences of up to 2^30 tokens)
+  for (int b = 32 + lane; b < p.a.batch; b += 32) {
+    const int n = usable_length(p.a, read_index<kL2>(p.a.kv_len + b));
+    low += n & 0xffff;
+    high += n >> 16;
+  }
+  low = __reduce_add_sync(0xffffffffu, low);
+  high = __reduce_add_sync(0xffffffffu, high);
+  const float all = (static_cast<float>(high) * 65536.0f + static_cast<float>(low)) * static_cast<float>(p.per);
+  const float target = static_cast<float>(all > static_cast<float>(p.target) * kLongChunk ? p.most_target : p.target);
+  auto inverse = [](float length) {  // of the length in whole kLeastChunk
+    return __fdividef(kLess, fmaxf(1.0f, ceilf(length * (1.0f / kLeastChunk))) * kLeastChunk);
   };
-  int length = max(kLeastChunk, share(static_cast<float>(all), p.per));
+  float length = __fdividef(all, target * kLess), per_length = inverse(length);
   // the remainders of the sequences come on top: lengthen the chunks until all fit the target, so that no CTA is left for a wave
   // of its own (a few tries, where the lengths are at hand)
-  const int lane = static_cast<int>(threadIdx.x & 31);
   for (int i = 0; i < 4 && p.a.batch <= 32; ++i) {
-    const int ctas = __reduce_add_sync(0xffffffffu, lane < p.a.batch ? chunks_of(len, length) : 0) * p.per;
+    const float ctas = static_cast<float>(__reduce_add_sync(0xffffffffu, lane < p.a.batch ? chunks_of(len, per_length) : 0) * p.per);
     if (ctas <= target) break;
-    length = share(static_cast<float>(length), ctas);
+    length = __fdividef(ctas, target * per_length) + 1.0f;
+    per_length = inverse(length);
   }
-  return length;
+  return per_length;
 }
 
 template <int kDim, int kTiles, bool kSplitQ>
@@ -226,10 +228,10 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
     chunk = max(kLeastChunk, chunk_size(usable_length(a, seq.len), p.cluster));
   } else {
     if (lane < a.batch) seq = load_sequence(a, lane);
-    const int length = chunk_length(p, usable_length(a, seq.len));
+    const float per_length = split_of(p, usable_length(a, seq.len));
     for (int b0 = 0; b0 < a.batch && b < 0; b0 += 32) {
       if (b0 > 0 && b0 + lane < a.batch) seq = load_sequence(a, b0 + lane);
-      const int len = usable_length(a, seq.len), n = b0 + lane < a.batch ? chunks_of(len, length) : 0;
+      const int len = usable_length(a, seq.len), n = b0 + lane < a.batch ? chunks_of(len, per_length) : 0;
       int upto = n;
 #pragma unroll
       for (int h = 1; h < 32; h *= 2) {
@@ -259,12 +261,15 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   // ---- the queries and the first cached tokens are asked for together
   constexpr int kQRounds = (kRows + kTeams - 1) / kTeams;
   uint4 q_raw[kQRounds];
+  const int tl = threadIdx.x % kTeam, q_low = tl * (a.pool.rotate ? 4 : 8), q_high = a.pool.rotate ? kDim / 2 + q_low : q_low + 4;
 #pragma unroll
   for (int i = 0; i < kQRounds; ++i) {
-    const int r = i * kTeams + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
+    const int r = i * kTeams + static_cast<int>(threadIdx.x) / kTeam;
     const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
-    q_raw[i] = r < rows ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + token * a.q_stride + head * kDim + tl * 8))
-                        : make_uint4(0, 0, 0, 0);
+    const T* const src = static_cast<const T*>(a.q) + token * a.q_stride + head * kDim;
+    const uint2 low = r < rows ? __ldg(reinterpret_cast<const uint2*>(src + q_low)) : make_uint2(0, 0);
+    const uint2 high = r < rows ? __ldg(reinterpret_cast<const uint2*>(src + q_high)) : make_uint2(0, 0);
+    q_raw[i] = make_uint4(low.x, low.y, high.x, high.y);
   }
   const uint32_t block = (kDim + 8u) << a.pool.log_page, stride = block * a.pool.kv_heads;  // of a head's page, of a page
   const uint8_t* const base = a.pool.base + static_cast<uint64_t>(kvh) * block;
@@ -321,32 +326,40 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) load(i, i);
 
-  // ---- queries: rotated, scaled by a power of two, float16, in the order of the codes' pairs
+  // ---- queries: rotated, scaled by a power of two, float16, in the order of the codes' pairs (all rounds at once: one after the
+  // other their shuffles' latencies took 2 us with 16 rows of 256 channels)
+  float y[kQRounds][8], top[kQRounds], sums[kQRounds];  // sums: of the rounded queries
 #pragma unroll
-  for (int r0 = 0; r0 < kRows; r0 += kTeams) {
-    const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
-    float y[8];
-    unpack8<T>(q_raw[r0 / kTeams], y);
-    if (a.pool.rotate) rotate_head<kTeam>(y);
-    float top = 0.0f;
+  for (int i = 0; i < kQRounds; ++i) unpack8<T>(q_raw[i], y[i]);
+  if (a.pool.rotate) rotate_from_halves<kTeam>(y);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) top = fmaxf(top, fabsf(y[c]));
+  for (int i = 0; i < kQRounds; ++i) {
+    top[i] = 0.0f;
 #pragma unroll
-    for (int h = 1; h < kTeam; h *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
-    const int e = min(126, max(-126, static_cast<int>(__float_as_uint(top) >> 23) - 126));
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-    float sum = 0.0f;  // of the rounded queries
+    for (int c = 0; c < 8; ++c) top[i] = fmaxf(top[i], fabsf(y[i][c]));
+  }
+#pragma unroll
+  for (int h = 1; h < kTeam; h *= 2)
+#pragma unroll
+    for (int i = 0; i < kQRounds; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], h));
+#pragma unroll
+  for (int i = 0; i < kQRounds; ++i) {
+    const int r = i * kTeams + static_cast<int>(threadIdx.x) / kTeam;
+    const int e = min(126, max(-126, static_cast<int>(__float_as_uint(top[i]) >> 23) - 126));
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    top[i] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+    sums[i] = 0.0f;
     if (r < kRows) {
       __half h[8], rest[8];
       float total = 0.0f;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {  // nibbles 1, 3, 5, 7 are read 16 times too large
         const float part = (c & 1) ? 0.0625f : 1.0f;
-        h[c] = __float2half_rn(y[c] * down * part);
-        rest[c] = __float2half_rn(y[c] * down * part - __half2float(h[c]));
+        h[c] = __float2half_rn(y[i][c] * down * part);
+        rest[c] = __float2half_rn(y[i][c] * down * part - __half2float(h[c]));
         total += (__half2float(h[c]) + (kSplitQ ? __half2float(rest[c]) : 0.0f)) * (c & 1 ? 16.0f : 1.0f);
       }
-      sum = total;
+      sums[i] = total;
       __half2 v[4] = {__halves2half2(h[0], h[4]), __halves2half2(h[1], h[5]), __halves2half2(h[2], h[6]), __halves2half2(h[3], h[7])};
       const int w = tl % (kDim / 32), at = (r & 7) * 4 + tl / (kDim / 32);
       q_at[q_index(r >> 3, w, 0) + at] = *reinterpret_cast<const uint2*>(v);
@@ -357,11 +370,17 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
         q_at[kRest + q_index(r >> 3, w, 1) + at] = *reinterpret_cast<const uint2*>(u + 2);
       }
     }
+  }
 #pragma unroll
-    for (int h = 1; h < kTeam; h *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, h);
+  for (int h = 1; h < kTeam; h *= 2)
+#pragma unroll
+    for (int i = 0; i < kQRounds; ++i) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], h);
+#pragma unroll
+  for (int i = 0; i < kQRounds; ++i) {
+    const int r = i * kTeams + static_cast<int>(threadIdx.x) / kTeam;
     if (r < kRows && tl == 0) {
-      s_f[r] = a.scale * kLog2e * up;
-      s_sum[r] = sum;
+      s_f[r] = a.scale * kLog2e * top[i];
+      s_sum[r] = sums[i];
     }
   }
   __syncthreads();
@@ -591,9 +610,9 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   const bool whole = most <= chunk && !p.cluster;
 #pragma unroll
   for (int r0 = 0; r0 < kRows; r0 += kTeams) {
-    const int r = r0 + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
+    const int r = r0 + static_cast<int>(threadIdx.x) / kTeam;
     const int rr = min(r, kRows - 1);
-    float top = s_m[0][rr], sum = 0.0f, y[8] = {};
+    float top = s_m[0][rr], sum = 0.0f, z[1][8] = {}, (&y)[8] = z[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_m[w][rr]);
 #pragma unroll
@@ -612,10 +631,10 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
       for (int c = 0; c < 8; ++c) y[c] *= inv;
-      if (a.pool.rotate) rotate_head<kTeam>(y);
+      if (a.pool.rotate) rotate_to_halves<kTeam>(z);
       if (r < rows) {
         const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
-        *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+        store_head<kTeam>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim, y, a.pool.rotate);
       }
     } else if (r < rows) {
       float* const dst = p.cluster ? s_part + r * (kDim + 2) : p.part + (static_cast<size_t>(blockIdx.x) * kRows + r) * (kDim + 2);
@@ -630,8 +649,8 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   cluster_sync();
   const uint32_t mine = smem_u32(s_part);
   for (int r0 = 0; r0 < rows; r0 += kTeams * p.cluster) {
-    const int r = r0 + ch * kTeams + static_cast<int>(threadIdx.x) / kTeam, tl = threadIdx.x % kTeam;
-    float m = -FLT_MAX, sum = 0.0f, y[8] = {};
+    const int r = r0 + ch * kTeams + static_cast<int>(threadIdx.x) / kTeam;
+    float m = -FLT_MAX, sum = 0.0f, z[1][8] = {}, (&y)[8] = z[0];
     if (r < rows) {
       for (int c = 0; c < p.cluster; ++c) {
         const uint32_t at = mapa_shared(mine + static_cast<uint32_t>(r) * (kDim + 2) * 4, static_cast<uint32_t>(c));
@@ -652,10 +671,10 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int c = 0; c < 8; ++c) y[c] *= inv;
-    if (a.pool.rotate) rotate_head<kTeam>(y);
+    if (a.pool.rotate) rotate_to_halves<kTeam>(z);
     if (r < rows) {
       const int token = seq.q0 + (row0 + r) / p.group, head = kvh * p.group + (row0 + r) % p.group;
-      *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+      store_head<kTeam>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim, y, a.pool.rotate);
     }
   }
   cluster_sync();  // nobody leaves while its result is being read
@@ -681,8 +700,8 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
     const bool found = find_sequence<true>(a.cu_q, a.batch, token, b, first);
     const Sequence seq = load_sequence<true>(a, b);
     if (found && usable(a, seq) && seq.q0 == first) {
-      const int length = chunk_length<true>(p, len);
-      const int chunk = chunk_size(seq.len, chunks_of(seq.len, length));
+      const float per_length = split_of<true>(p, len);
+      const int chunk = chunk_size(seq.len, chunks_of(seq.len, per_length));
       kvh = head / p.group;
       r = (token - first) * p.group + head % p.group;
       tile = r / p.rows;
@@ -691,7 +710,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
       for (int b0 = 0; b0 < b; b0 += 32) {  // chunks of the sequences ahead
         const int at = b0 + lane;
         before += __reduce_add_sync(
-            0xffffffffu, at < b ? chunks_of(b0 == 0 ? len : usable_length(a, read_index<true>(a.kv_len + at)), length) : 0);
+            0xffffffffu, at < b ? chunks_of(b0 == 0 ? len : usable_length(a, read_index<true>(a.kv_len + at)), per_length) : 0);
       }
     }
   }
@@ -701,7 +720,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
   const size_t unit = static_cast<size_t>(before) * p.per + kvh * p.row_tiles + tile;
   const float* const src = p.part + (unit * p.rows + r % p.rows) * (kDim + 2);
   const size_t next = static_cast<size_t>(p.per) * p.rows * (kDim + 2);
-  float m = -FLT_MAX, l = 0.0f, y[8] = {};
+  float m = -FLT_MAX, l = 0.0f, z[1][8] = {}, (&y)[8] = z[0];
   auto add = [&](float m2, float l2, const float (&y2)[8]) {
     const float top = fmaxf(m, m2), keep = ex2(m - top), k = ex2(m2 - top);
     m = top;
@@ -756,8 +775,8 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
   for (int c = 0; c < 8; ++c) y[c] *= inv;
-  if (a.pool.rotate) rotate_head<kTeam>(y);
-  if (lane < kTeam) *reinterpret_cast<uint4*>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim + tl * 8) = pack8<T>(y);
+  if (a.pool.rotate) rotate_to_halves<kTeam>(z);
+  if (lane < kTeam) store_head<kTeam>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim, y, a.pool.rotate);
 }
 
 int rows_of(const Kv4AttentionArgs& a) { return static_cast<int64_t>(a.max_q) * (a.heads / a.pool.kv_heads) <= 8 ? 8 : 16; }

@@ -56,35 +56,67 @@ __device__ __forceinline__ uint8_t* kv4_block(const Kv4Pool& p, const int32_t* _
   return p.base + (static_cast<size_t>(page) * p.kv_heads + head) * kv4_block_bytes(p);
 }
 
-// x . H for a head spread over a team of kTeam adjacent lanes, 8 consecutive channels a lane: butterflies of distance 1, 2, 4
-// in registers, then 8, 16, ... between lanes, each output a + b or a - b (so any order of evaluation gives the same
-// bits), and the factor 1 / sqrt(8 kTeam) last.
-template <int kTeam>
-__device__ __forceinline__ void rotate_head(float (&y)[8]) {
+// x . H / sqrt(D) for heads spread over teams of kTeam = D / 8 adjacent lanes, n heads a team at once.  Distances within a lane's
+// 8 channels are butterflies in registers.  For the others two lanes first exchange a half of their registers, so that both ends of a
+// distance lie in one lane (4 shuffles a level and head where exchanging all would take 8).  That turns the order of the channels:
+// a lane has either channels 8 l to 8 l + 7 or channels 4 l to 4 l + 3 and those D / 2 further on (the halves' order).
+template <int n>
+__device__ __forceinline__ void butterflies(float (&y)[n][8], int h) {
 #pragma unroll
-  for (int h = 1; h < 8; h *= 2) {
+  for (int j = 0; j < n; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i)
       if ((i & h) == 0) {
-        const float a = y[i], b = y[i + h];
-        y[i] = a + b;
-        y[i + h] = a - b;
+        const float a = y[j][i], b = y[j][i + h];
+        y[j][i] = a + b;
+        y[j][i + h] = a - b;
       }
-    }
-  }
-  const int lane = threadIdx.x & 31;
+}
+template <int n>
+__device__ __forceinline__ void swap_halves(float (&y)[n][8], int h) {
+  const bool high = (threadIdx.x & h) != 0;
 #pragma unroll
-  for (int h = 1; h < kTeam; h *= 2) {
-    const bool high = (lane & h) != 0;
+  for (int j = 0; j < n; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float o = __shfl_xor_sync(0xffffffffu, y[i], h);
-      y[i] = high ? o - y[i] : y[i] + o;
+    for (int i = 0; i < 4; ++i) {
+      const float got = __shfl_xor_sync(0xffffffffu, high ? y[j][i] : y[j][i + 4], h);
+      y[j][i] = high ? got : y[j][i];
+      y[j][i + 4] = high ? y[j][i + 4] : got;
     }
-  }
+}
+template <int kTeam, int n>
+__device__ __forceinline__ void scale_rotated(float (&y)[n][8]) {
   constexpr float f = kTeam == 8 ? 0.125f : kTeam == 16 ? 0.08838834764831845f : 0.0625f;  // float32(1 / sqrt(8 kTeam))
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] *= f;
+  for (int j = 0; j < n; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[j][i] *= f;
+}
+// from the halves' order
+template <int kTeam, int n>
+__device__ __forceinline__ void rotate_from_halves(float (&y)[n][8]) {
+  butterflies(y, 1);
+  butterflies(y, 2);
+  butterflies(y, 4);
+#pragma unroll
+  for (int h = kTeam / 2; h > 0; h /= 2) {
+    swap_halves(y, h);
+    butterflies(y, 4);
+  }
+  scale_rotated<kTeam>(y);
+}
+// to the halves' order
+template <int kTeam, int n>
+__device__ __forceinline__ void rotate_to_halves(float (&y)[n][8]) {
+  butterflies(y, 1);
+  butterflies(y, 2);
+  butterflies(y, 4);
+#pragma unroll
+  for (int h = 1; h < kTeam; h *= 2) {
+    swap_halves(y, h);
+    butterflies(y, 4);
+  }
+  scale_rotated<kTeam>(y);
 }
 
 // (w & mask) ^ flip in one instruction.  Only one of its operands can be an immediate: `flip` comes from a register that the
@@ -169,6 +201,18 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = Pair<T>::from_float(y[2 * i], y[2 * i + 1]);
   return v;
+}
+// A lane's 8 channels of a head, in the halves' order where they have been rotated.
+template <int kTeam, typename T>
+__device__ __forceinline__ void store_head(T* head, const float (&y)[8], bool halves) {
+  const uint4 v = pack8<T>(y);
+  const int tl = threadIdx.x % kTeam;
+  if (halves) {
+    *reinterpret_cast<uint2*>(head + tl * 4) = make_uint2(v.x, v.y);
+    *reinterpret_cast<uint2*>(head + kTeam * 4 + tl * 4) = make_uint2(v.z, v.w);
+  } else {
+    *reinterpret_cast<uint4*>(head + tl * 8) = v;
+  }
 }
 
 }  // namespace qvla

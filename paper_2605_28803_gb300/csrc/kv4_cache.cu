@@ -67,7 +67,7 @@ __device__ __forceinline__ void rotate_codes(__half2 (&v)[4][4]) {
         }
 }
 
-// x . H / sqrt(32 kTeam) for a head spread over kTeam lanes as above; the sums of rotate_head in its order, so the same bits.
+// x . H / sqrt(32 kTeam) for a head spread over kTeam lanes as above; distances 1, 2, 4, ... in this order (another one rounds differently).
 template <int kTeam>
 __device__ __forceinline__ void rotate_groups(float2 (&y)[4][4]) {
   const float2 minus = make_float2(-1.0f, -1.0f);
