@@ -61,7 +61,7 @@ constexpr int kLeastChunk = kTile * kWarps;
 constexpr int ctas_per_sm(int dim, int rows) { return rows == 8 ? (dim == 256 ? 3 : 4) : (dim == 64 ? 3 : 2); }
 constexpr int kWaves8 = 2, kWaves16 = 1;
 constexpr int kLongChunk = 1024;  // tokens of a CTA above which more waves pay (a CTA's own start and end take about 5 us)
-constexpr int kClusterLen = 4096;                 // longest context that clusters share
+constexpr int cluster_len(int dim) { return dim == 256 ? 2048 : 4096; }  // longest context that clusters share
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -791,12 +791,13 @@ cudaError_t plan_split(const Kv4AttentionArgs& a, size_t ws_bytes, Kv4Params* p)
   p->row_tiles = static_cast<int>(tiles);
   p->per = static_cast<int>(a.pool.kv_heads * tiles);
   // A cluster a unit where clusters of eight leave SMs to spare and a part stays short: then the second launch is what a call
-  // can save (one token over 817: 9.4 against 10.4 us).  With more units the chunks by length are faster (23 ragged contexts
-  // of up to 6001 tokens: 20.5 us against 24 with clusters).
+  // can save.  One token over 817, 8 heads of 256 channels on one: 8.6 us either way on the device, 11.5 against 14 as the host's calls
+  // follow one another; over 4000, 8 heads of 128: 8.2 against 11.4 on the device; of 256 channels, 16 contexts: 16.4 against
+  // 14.0.  (23 ragged contexts of up to 6001 tokens and 8 heads, in clusters all the same: 24 against 20.5 when that was tried.)
   const int64_t parts = (static_cast<int64_t>(a.max_len) + kLeastChunk - 1) / kLeastChunk;
   p->cluster = 0;
   p->target = p->most_target = 0;
-  if (units * 8 <= a.num_sms && parts > 1 && a.max_len <= kClusterLen) {
+  if (units * 8 <= a.num_sms && parts > 1 && a.max_len <= cluster_len(a.pool.head_dim)) {
     p->cluster = static_cast<int>(parts < 8 ? parts : 8);
     p->ctas = static_cast<int>(units * p->cluster);
     return cudaSuccess;
