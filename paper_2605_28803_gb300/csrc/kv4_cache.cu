@@ -1,6 +1,6 @@
 // The 4-bit key/value cache: tokens in (rotate, quantise, store to their pages) and tokens out.
 //
-// Per token and key/value head: y = x . H / sqrt(D) (or x), Delta = max |y| / 7 (times float32(1 / 7)), codes clamp(round(y / Delta), -7, 7), round half
+// Per token and key/value head: y = x . H / sqrt(D) (or x), Delta = max |y| float32(1 / 7), codes clamp(round(y / Delta), -7, 7), round half
 // to even on the exact quotient; out again, x^ = (Delta / sqrt(D)) (q . H), rounded to the output's type.  q . H is a vector of
 // integers of at most 7 D = 1792: exact in float16, so on the way out the rotation is float16 arithmetic, two channels an
 // instruction and a shuffle, without a rounding.
@@ -11,6 +11,9 @@
 // largest stay in registers, two channels an instruction, and 1 to 3 are shuffles; a team's 16-byte accesses are contiguous.
 // A warp takes `passes` sets of 32 / team heads in a row and loads the next set's data ahead of the present one's
 // arithmetic; the search for the first token's sequence is made once.
+//
+// Measured, 8 heads of 128 channels: 7194 tokens in and out 27.5 us (in: issue 55% with the registers' 20 warps an SM, 10 M warp
+// instructions for 14.7 M channels a side); 49611 tokens out 54 us, 203 MB written at 3.8 TB/s (a plain fill writes at 3.9).
 #include <cuda_runtime.h>
 
 #include "griddep.cuh"
