@@ -21,7 +21,7 @@
 #include <cuda.h>
 //
 // Measured: 8192 causal tokens, 16 heads of 128 channels on 4, 174 us (1580 TFLOP/s, tensor pipe 64% active: the exponentials
-// take as long as the products); 816 tokens, 8 heads of 256 on one, 16.5 us (a CTA's 13 blocks at 0.8 us, on 51 SMs); packed prompts of
+// take as long as the products); 816 tokens, 8 heads of 256 on one, 15.6 us (a CTA's 13 blocks at 0.8 us, on 51 SMs); packed prompts of
 // up to 1500 over 2000 keys, 14 heads of 64 on 2, 22.5 us (the longest CTA's 16 blocks at 1.2 us).
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
@@ -57,6 +57,8 @@ struct Shape {
   static constexpr int kThreads = 32 * (kWarpSoftmax + 4 * kTiles);
   static constexpr int kQBytes = kQTmem ? 0 : kRowsPerTile * kDim * 2;  // one tile in shared memory
   static constexpr int kKvBytes = kBlock * kDim * 2;          // one block of K or V
+  static constexpr int kStageAt = kStagesV - 2;               // with Q in TMEM: the stages of V that Q passes through
+  static_assert(!kQTmem || 2 * kKvBytes == kRowsPerTile * kDim * 2, "a tile of Q takes two stages");
   static constexpr int kSmem = kTiles * kQBytes + (kStagesK + kStagesV) * kKvBytes + 1024;
   // a cluster's join: O in float32, rows kORow apart (which spreads a column over the banks), then maximum and sum of each row
   static constexpr int kORow = kDim + 4, kOBytes = kTiles * kRowsPerTile * kORow * 4;
@@ -335,6 +337,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           const int k = j % kStagesK, v = j % kStagesV;
           if (!fetch(&tmap_k, smem_k + k * C::kKvBytes, &bar_kempty[k], &bar_kfull[k], j, kStagesK)) break;
           ks = j + 1;
+          if (C::kQTmem && j == C::kStageAt && !mbar_wait_warp(smem_u32(&bar_q[0]), 0)) break;  // Q has left the stages
           if (!fetch(&tmap_v, smem_v + v * C::kKvBytes, &bar_vempty[v], &bar_vfull[v], j, kStagesV)) break;
           vs = j + 1;
         }
@@ -480,24 +483,38 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
       const int seen = live ? seen_by(w, p.causal, token) : w.keys;
       const int n = blocks[t], from = partial[t];
       const uint32_t o_at = tmem + lanes + static_cast<uint32_t>(C::kOCol + t * kDim);
-      if (C::kQTmem && n > 0) {  // this row of Q, two channels a column
-        const T* const src = static_cast<const T*>(p.q) + (w.q0 + token) * p.q_stride + (w.head + head) * kDim;
+      if (C::kQTmem && n > 0) {
+        // Q to TMEM, two channels a column.  A warp's 32 rows pass through stages of V that are free yet: read by its own thread a
+        // row touches another 128-byte line with every lane, which took 0.8 us more.  Pieces of 16 bytes, exchanged by the row's last
+        // three bits.  (O written that way gained 0.4 to 0.8 us with full tiles, and cost 0.4 with few rows and, by its registers, 3% of
+        // long calls with 128 channels.)
+        uint8_t* const rows_at = smem_v + C::kStageAt * C::kKvBytes + (warp & 3) * 32 * kDim * 2;
+        constexpr int kRowLanes = kDim / 8, kRowsAtOnce = 32 / kRowLanes;  // lanes of a row, rows of an access
+        auto piece_at = [&](int r, int c) { return reinterpret_cast<uint4*>(rows_at + r * kDim * 2 + ((c ^ (r & 7)) * 16)); };
+        const int64_t offset = live ? (w.q0 + token) * p.q_stride + (w.head + head) * kDim : -1;
+#pragma unroll 16
+        for (int r0 = 0; r0 < 32; r0 += kRowsAtOnce) {
+          const int r = r0 + lane / kRowLanes, c = lane % kRowLanes;
+          const int64_t from_row = __shfl_sync(0xffffffffu, offset, r);
+          *piece_at(r, c) = from_row >= 0 ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + from_row + c * 8)) : make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
 #pragma unroll
-        for (int h = 0; h < kDim / 128; ++h) {  // 16 loads at once
-          uint32_t y[4][16];
+        for (int i = 0; i < kDim / 32; ++i) {
+          uint32_t y[16];
 #pragma unroll
-          for (int e = 0; e < 64; e += 4) {
-            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(src + h * 128 + e * 2)) : make_uint4(0, 0, 0, 0);
-            y[e / 16][e % 16] = v.x;
-            y[e / 16][e % 16 + 1] = v.y;
-            y[e / 16][e % 16 + 2] = v.z;
-            y[e / 16][e % 16 + 3] = v.w;
+          for (int e = 0; e < 4; ++e) {
+            const uint4 v = *piece_at(lane, i * 4 + e);
+            y[4 * e] = v.x;
+            y[4 * e + 1] = v.y;
+            y[4 * e + 2] = v.z;
+            y[4 * e + 3] = v.w;
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_st16(tmem + lanes + static_cast<uint32_t>(C::kQCol + h * 64 + i * 16), y[i]);
+          tmem_st16(tmem + lanes + static_cast<uint32_t>(C::kQCol + i * 16), y);
         }
         tmem_st_wait();
         tc_fence_before();
+        fence_proxy_async_smem();  // V comes to these stages next
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bar_q[0]));
       }

@@ -12,8 +12,8 @@
 // A warp takes `passes` sets of 32 / team heads in a row and loads the next set's data ahead of the present one's
 // arithmetic; the search for the first token's sequence is made once.
 //
-// Measured, 8 heads of 128 channels: 7194 tokens in and out 27.5 us (in: issue 55% with the registers' 20 warps an SM, 10 M warp
-// instructions for 14.7 M channels a side); 49611 tokens out 54 us, 203 MB written at 3.8 TB/s (a plain fill writes at 3.9).
+// Measured, 8 heads of 128 channels: 7194 tokens in and out 27.5 us (in: issue 55% with the 20 warps an SM that registers allow, 10 M warp
+// instructions for 14.7 M channels); 49611 tokens out 54 us, 203 MB written at 3.8 TB/s (a plain fill writes at 3.9).
 #include <cuda_runtime.h>
 
 #include "griddep.cuh"
