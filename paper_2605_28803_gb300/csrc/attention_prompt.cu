@@ -21,8 +21,8 @@
 #include <cuda.h>
 //
 // Measured: 8192 causal tokens, 16 heads of 128 channels on 4, 174 us (1580 TFLOP/s, tensor pipe 64% active: the exponentials
-// take as long as the products); 816 tokens, 8 heads of 256 on one, 15.6 us (a CTA's 13 blocks at 0.8 us, on 51 SMs); packed prompts of
-// up to 1500 over 2000 keys, 14 heads of 64 on 2, 22.5 us (the longest CTA's 16 blocks at 1.2 us).
+// take as long as the products); 816 tokens, 8 heads of 256 on one, 15.3 us (a CTA's 13 blocks at 0.65 us, on 51 SMs); packed prompts of
+// up to 1500 over 2000 keys, 14 heads of 64 on 2, 22.2 us (the longest CTA's 16 blocks at 1.2 us).
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
@@ -126,6 +126,17 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t at) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
   return v;
+}
+// 32 bytes of a row, in one access (a whole sector) where o's address allows: 0.3 to 0.5 us of a call against 16 bytes at a time.
+__device__ __forceinline__ void store_row(void* dst, const uint32_t (&q)[8], bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]), "r"(q[4]),
+                 "r"(q[5]), "r"(q[6]), "r"(q[7])
+                 : "memory");
+  } else {
+    static_cast<uint4*>(dst)[0] = make_uint4(q[0], q[1], q[2], q[3]);
+    static_cast<uint4*>(dst)[1] = make_uint4(q[4], q[5], q[6], q[7]);
+  }
 }
 template <int kThreads>
 __device__ __forceinline__ void softmax_sync() {  // the softmax warps meet
@@ -624,6 +635,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
         }
       } else if (ok) {
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const bool wide = (reinterpret_cast<uint64_t>(p.o) & 31) == 0;
         T* const dst = static_cast<T*>(p.o) + (static_cast<size_t>(w.q0 + token) * p.heads + w.head + head) * kDim;
 #pragma unroll 2
         for (int i = 0; i < kDim / 32; ++i) {
@@ -638,13 +650,11 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           if (bad && live) add_bad(y, i);
           if (live) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint4 q;
-              q.x = pack2<T>(y[e], y[e + 1]);
-              q.y = pack2<T>(y[e + 2], y[e + 3]);
-              q.z = pack2<T>(y[e + 4], y[e + 5]);
-              q.w = pack2<T>(y[e + 6], y[e + 7]);
-              *reinterpret_cast<uint4*>(dst + i * 32 + e) = q;
+            for (int e = 0; e < 32; e += 16) {
+              uint32_t q[8];
+#pragma unroll
+              for (int c = 0; c < 8; ++c) q[c] = pack2<T>(y[e + 2 * c], y[e + 2 * c + 1]);
+              store_row(dst + i * 32 + e, q, wide);
             }
           }
         }

@@ -128,6 +128,23 @@ def test_slices_of_a_fused_projection():
     assert torch.equal(got, dense)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_an_output_at_any_16_bytes(dim):
+    """Aligned to 16 bytes and not to 32, between bytes that stay as they are."""
+    rng = np.random.default_rng(dim + 2)
+    lens = [150, 3]
+    q, k, v = (H.draw_heads(rng, sum(lens), h, dim, "f16").to(H.DEV) for h in (4, 2, 2))
+    want = H.prompt(q, k, v, lens, lens, True)
+    room = torch.full((want.numel() + 24,), 7.0, dtype=q.dtype, device=H.DEV)
+    o = room[8: 8 + want.numel()].view(want.shape)
+    cu = H.ints(H.offsets(lens))
+    Q.qvla_attention_prompt(q, k, v, Q.F16, 4, 2, dim, q.stride(0), k.stride(0), v.stride(0), 2, cu, sum(lens), cu, sum(lens), dim ** -0.5,
+                            True, o, H.stream())
+    Q.qvla_check_device(H.stream())
+    assert o.data_ptr() % 32 == 16
+    assert torch.equal(o, want) and (room[:8] == 7).all() and (room[8 + want.numel():] == 7).all()
+
+
 def test_queries_that_see_nothing_are_zero():
     rng = np.random.default_rng(9)
     lens_q, lens_k = [5, 200, 7, 3], [2, 60, 0, 3]  # causal: the first 3, 140 and 7 queries see no key
