@@ -145,9 +145,12 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
   griddep_wait();  // tokens, cache, tables and offsets may come from the previous kernel, which may still read the outputs
   griddep_launch_dependents();
   if (id0 >= all) return;
-  int t0 = static_cast<int>(id0 / rows), row0 = static_cast<int>(id0 % rows);  // the pass's first head
+  const int t0 = static_cast<int>(id0 / rows), row0 = static_cast<int>(id0 % rows);  // the first pass's first head
   int b, first, next;
   find_sequence(a.cu, a.batch, t0, b, first);
+  // this team's head, and what it moves on by from pass to pass (no division by `rows` there)
+  int t = t0 + (row0 + team) / rows, row = (row0 + team) % rows;
+  const int t_on = kHeads / rows, row_on = kHeads % rows;
   next = __ldg(a.cu + b + 1);
   const size_t block = kv4_block_bytes(a.pool);
   const int plane = (kDim / 2) << a.pool.log_page;  // bytes of a block's key codes
@@ -159,16 +162,12 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
     uint4 x[4];     // append: the token's values; gather: the codes of group k in x[0].xyzw
     float d;
   };
-  auto load = [&](Head& h) {
+  auto load = [&](Head& h, int t, int row) {
     h.out = nullptr;
     h.at = nullptr;
     h.d = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) h.x[k] = make_uint4(0, 0, 0, 0);
-    const int over = (row0 + team) / rows, t = t0 + over, row = row0 + team - over * rows;
-    row0 += kHeads;
-    t0 += row0 / rows;
-    row0 %= rows;
     if (t >= a.total) return;
     while (t >= next && b + 1 < a.batch) {  // (tokens come in order)
       first = next;
@@ -283,10 +282,18 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
     }
   };
   Head now, ahead;
-  load(now);
+  load(now, t, row);
   for (int i = 0; i < passes; ++i) {
     if (id0 + static_cast<int64_t>(i) * kHeads >= all) break;  // (the whole warp)
-    if (i + 1 < passes) load(ahead);
+    if (i + 1 < passes) {
+      t += t_on;
+      row += row_on;
+      if (row >= rows) {
+        row -= rows;
+        ++t;
+      }
+      load(ahead, t, row);
+    }
     finish(now);
     now = ahead;
   }
