@@ -9,11 +9,13 @@
 // log2 D sums a channel and its exchanges between lanes come close to it.  So a head is a team of only D / 32 lanes with four
 // groups of 8 channels each, group k of lane l at channel 8 (k team + l): of the butterflies' distances 1, 2, 4 and the two
 // largest stay in registers, two channels an instruction, and 1 to 3 are shuffles; a team's 16-byte accesses are contiguous.
-// A warp takes `passes` sets of 32 / team heads in a row and loads the next set's data ahead of the present one's
-// arithmetic; the search for the first token's sequence is made once.
+// A warp takes `sets` sets of 32 / team heads in a row, keys and then values of each (which lie in the same block of the cache), and
+// loads the next pass's data ahead of the present one's arithmetic; the search for the first token's sequence is made once.
 //
-// Measured, 8 heads of 128 channels: 7194 tokens in and out 27.5 us (in: issue 55% with the 20 warps an SM that registers allow, 10 M warp
-// instructions for 14.7 M channels); 49611 tokens out 54 us, 203 MB written at 3.8 TB/s (a plain fill writes at 3.9).
+// Measured, 8 heads of 128 channels: 7194 tokens in and out 24.4 us (on the way in the arithmetic's instruction issue, with the 20 warps
+// an SM that registers allow); 49611 tokens out 48.6 us, 203 MB written at 4.2 TB/s (a plain fill writes at 3.9).  Keys and
+// values of a head by the same warp, which finds their block once, took 49611 tokens from 50.5 to 48.6 and 3000 tokens of 8 heads of
+// 256 from 9.9 to 7.8 us.
 #include <cuda_runtime.h>
 
 #include "griddep.cuh"
@@ -23,8 +25,8 @@ namespace qvla {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kPasses = 8;        // of a warp, at most
-constexpr int kWarpsPerSm = 32;   // below this many warps an SM, a warp takes fewer passes
+constexpr int kSets = 4;          // of a warp, at most
+constexpr int kWarpsPerSm = 48;   // below this many warps an SM, a warp takes fewer sets (of 7194 tokens in and out: 40 warps 27.3 us, 48 24.6, 64 24.6)
 
 template <int kTeam>
 constexpr float kNorm = kTeam == 2 ? 0.125f : kTeam == 4 ? 0.08838834764831845f : 0.0625f;  // float32(1 / sqrt(32 kTeam))
@@ -135,39 +137,35 @@ __device__ __forceinline__ int code_of(float y, float d, float r) {
   return static_cast<int>(fminf(fmaxf(n, -7.0f), 7.0f));
 }
 
-template <typename T, int kTeam, bool kAppend>
-__global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constant__ Kv4RowsArgs a, int passes) {
+// kApart: a warp takes the keys or the values of one set, for calls of few tokens; else `sets` sets, keys and values.
+template <typename T, int kTeam, bool kAppend, bool kApart>
+__global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constant__ Kv4RowsArgs a, int sets) {
   constexpr int kDim = 32 * kTeam, kHeads = 32 / kTeam;  // heads of a warp's pass
   const int lane = threadIdx.x & 31, team = lane / kTeam, tl = lane % kTeam;
-  const int rows = 2 * a.pool.kv_heads;  // a token's heads: keys, then values
-  const int64_t all = static_cast<int64_t>(a.total) * rows;
-  const int64_t id0 = ((static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5) * passes * kHeads;
+  const int heads = a.pool.kv_heads;
+  const int64_t all = static_cast<int64_t>(a.total) * heads;
+  const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5;
+  const int side = kApart ? static_cast<int>(warp & 1) : 0;
+  const int64_t id0 = (kApart ? warp >> 1 : warp * sets) * kHeads;
   griddep_wait();  // tokens, cache, tables and offsets may come from the previous kernel, which may still read the outputs
   griddep_launch_dependents();
   if (id0 >= all) return;
-  const int t0 = static_cast<int>(id0 / rows), row0 = static_cast<int>(id0 % rows);  // the first pass's first head
-  int b, first, next;
-  find_sequence(a.cu, a.batch, t0, b, first);
-  // this team's head, and what it moves on by from pass to pass (no division by `rows` there)
-  int t = t0 + (row0 + team) / rows, row = (row0 + team) % rows;
-  const int t_on = kHeads / rows, row_on = kHeads % rows;
+  // this team's token and head, and what they move on by from set to set (no division by `heads` there)
+  const int64_t id = id0 + team;
+  int t = static_cast<int>(all >> 31 ? id / heads : static_cast<uint32_t>(id) / static_cast<uint32_t>(heads));
+  int head = static_cast<int>(id - static_cast<int64_t>(t) * heads), b, first, next;
+  find_sequence(a.cu, a.batch, __shfl_sync(0xffffffffu, t, 0), b, first);
   next = __ldg(a.cu + b + 1);
-  const size_t block = kv4_block_bytes(a.pool);
+  const int t_on = kHeads / heads, head_on = kHeads % heads;
   const int plane = (kDim / 2) << a.pool.log_page;  // bytes of a block's key codes
 
-  struct Head {
-    uint8_t* at;    // its block in the cache, at the token's codes and scale; null: none
-    float* scale;
-    T* out;         // gather's output, append's input; null: nothing to do
-    uint4 x[4];     // append: the token's values; gather: the codes of group k in x[0].xyzw
-    float d;
-  };
-  auto load = [&](Head& h, int t, int row) {
-    h.out = nullptr;
-    h.at = nullptr;
-    h.d = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) h.x[k] = make_uint4(0, 0, 0, 0);
+  // a team's head in the cache: its key's codes and scale at the token (null: none), the value's a plane further on
+  bool here = false;
+  uint8_t* codes = nullptr;
+  float* scale = nullptr;
+  auto find = [&]() {
+    here = false;
+    codes = nullptr;
     if (t >= a.total) return;
     while (t >= next && b + 1 < a.batch) {  // (tokens come in order)
       first = next;
@@ -175,20 +173,36 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
       next = __ldg(a.cu + b + 1);
     }
     if (t < first || t >= next) return;
-    const int value = row >= a.pool.kv_heads, head = row - value * a.pool.kv_heads;
-    h.out = static_cast<T*>(value ? a.v : a.k) + t * (value ? a.v_stride : a.k_stride) + head * kDim + tl * 8;
+    here = true;
     const int64_t pos = static_cast<int64_t>(a.start ? __ldg(a.start + b) : 0) + (t - first);
     uint8_t* const at = kv4_block(a.pool, a.table, a.max_pages, b, pos, head);
-    if (at != nullptr) {
-      const int slot = static_cast<int>(pos) & ((1 << a.pool.log_page) - 1);
-      h.at = at + value * plane + slot * (kDim / 2) + tl * 4;
-      h.scale = reinterpret_cast<float*>(at + 2 * plane) + (value << a.pool.log_page) + slot;
-    }
+    if (at == nullptr) return;
+    const int slot = static_cast<int>(pos) & ((1 << a.pool.log_page) - 1);
+    codes = at + slot * (kDim / 2) + tl * 4;
+    scale = reinterpret_cast<float*>(at + 2 * plane) + slot;
+  };
+  struct Head {
+    uint8_t* at;    // its codes in the cache; null: none
+    float* scale;
+    T* out;         // gather's output, append's input; null: nothing to do
+    uint4 x[4];     // append: the token's values; gather: the codes of group k in x[0].xyzw
+    float d;
+  };
+  auto load = [&](Head& h, int value) {
+    h.out = nullptr;
+    h.at = nullptr;
+    h.d = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) h.x[k] = make_uint4(0, 0, 0, 0);
+    if (!here) return;
+    h.out = static_cast<T*>(value ? a.v : a.k) + t * (value ? a.v_stride : a.k_stride) + head * kDim + tl * 8;
+    if (codes == nullptr) return;
+    h.at = codes + (value ? plane : 0);
+    h.scale = scale + (value << a.pool.log_page);
     if constexpr (kAppend) {
-      if (at == nullptr) return;
 #pragma unroll
       for (int k = 0; k < 4; ++k) h.x[k] = __ldg(reinterpret_cast<const uint4*>(h.out + k * 8 * kTeam));
-    } else if (at != nullptr) {
+    } else {
       h.x[0].x = __ldg(reinterpret_cast<const unsigned int*>(h.at));
       h.x[0].y = __ldg(reinterpret_cast<const unsigned int*>(h.at + 4 * kTeam));
       h.x[0].z = __ldg(reinterpret_cast<const unsigned int*>(h.at + 8 * kTeam));
@@ -281,30 +295,38 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
       }
     }
   };
-  Head now, ahead;
-  load(now, t, row);
-  for (int i = 0; i < passes; ++i) {
-    if (id0 + static_cast<int64_t>(i) * kHeads >= all) break;  // (the whole warp)
-    if (i + 1 < passes) {
-      t += t_on;
-      row += row_on;
-      if (row >= rows) {
-        row -= rows;
-        ++t;
-      }
-      load(ahead, t, row);
-    }
+  Head now;
+  find();
+  load(now, side);
+  if constexpr (kApart) {
     finish(now);
-    now = ahead;
+  } else {
+    for (int i = 0; i < 2 * sets; ++i) {  // a set's keys, then its values
+      if (id0 + static_cast<int64_t>(i / 2) * kHeads >= all) break;  // (the whole warp)
+      Head ahead;
+      if ((i & 1) && i + 1 < 2 * sets) {
+        t += t_on;
+        head += head_on;
+        if (head >= heads) {
+          head -= heads;
+          ++t;
+        }
+        find();
+      }
+      if (i + 1 < 2 * sets) load(ahead, (i + 1) & 1);
+      finish(now);
+      now = ahead;
+    }
   }
 }
 
 template <typename T, int kTeam, bool kAppend>
 cudaError_t launch_rows(const Kv4RowsArgs& a) {
-  const int64_t sets = (static_cast<int64_t>(a.total) * 2 * a.pool.kv_heads + 32 / kTeam - 1) / (32 / kTeam);
+  const int64_t all = (static_cast<int64_t>(a.total) * a.pool.kv_heads + 32 / kTeam - 1) / (32 / kTeam);
   const int64_t fill = static_cast<int64_t>(a.num_sms) * kWarpsPerSm;
-  const int passes = static_cast<int>(sets >= fill * kPasses ? kPasses : sets <= fill ? 1 : (sets + fill - 1) / fill);
-  const int64_t warps = (sets + passes - 1) / passes;
+  const int sets = static_cast<int>(all >= fill * kSets ? kSets : all <= fill ? 1 : (all + fill - 1) / fill);
+  const bool apart = 2 * all <= fill;
+  const int64_t warps = apart ? 2 * all : (all + sets - 1) / sets;
   const int64_t blocks = (warps * 32 + kThreads - 1) / kThreads;
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg = {};
@@ -316,7 +338,7 @@ cudaError_t launch_rows(const Kv4RowsArgs& a) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, kv4_rows_kernel<T, kTeam, kAppend>, a, passes);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, apart ? kv4_rows_kernel<T, kTeam, kAppend, true> : kv4_rows_kernel<T, kTeam, kAppend, false>, a, sets);
   if (e != cudaSuccess) return e;
   return cudaGetLastError();
 }
