@@ -66,6 +66,18 @@ def test_long_caches_are_split_and_joined(dim, kv, lens):
         assert np.abs(got - full).max() < 0.05
 
 
+@pytest.mark.parametrize("dim,kv,queries", [(64, 2, 1), (128, 8, 1), (256, 1, 3)])
+def test_more_sequences_than_a_warp_has_lanes(dim, kv, queries):
+    rng = np.random.default_rng(dim + 5)
+    lens = [int(n) for n in rng.integers(0, 300, 67)] + [2600, 0, 1, 5000]
+    lens_q = [queries if n >= queries else 0 for n in lens]
+    p = H.Paged(rng, lens, kv, dim, 32, True)
+    p.fill(rng, lens)
+    q = H.draw_heads(rng, sum(lens_q), 4 * kv, dim, "bf16")
+    check(p, q, lens_q, lens, True)
+    check(p, q, lens_q, lens, False)
+
+
 def test_scores_that_grow_along_the_cache_and_sharp_rows():
     rng = np.random.default_rng(2)
     lens = [3000]

@@ -118,6 +118,18 @@ def test_scores_of_one_size_and_a_large_scale():
     check(q, k, v, [40], [40], True, scale=1e-6)
 
 
+@pytest.mark.parametrize("dim,heads,kv", [(64, 6, 2), (128, 4, 4), (256, 8, 1)])
+def test_more_sequences_than_a_warp_has_lanes(dim, heads, kv):
+    rng = np.random.default_rng(dim + 6)
+    lens_q = [int(n) for n in rng.integers(0, 40, 75)] + [130, 0, 1]
+    lens_k = [int(n + m) for n, m in zip(lens_q, rng.integers(0, 60, 78))]
+    q = H.draw_heads(rng, sum(lens_q), heads, dim, "bf16")
+    k = H.draw_heads(rng, sum(lens_k), kv, dim, "bf16")
+    v = H.draw_heads(rng, sum(lens_k), kv, dim, "bf16")
+    check(q, k, v, lens_q, lens_k, True)
+    check(q, k, v, lens_q, lens_k, False)
+
+
 def test_slices_of_a_fused_projection():
     rng = np.random.default_rng(8)
     heads, kv, dim, lens = 8, 2, 128, [70, 200]

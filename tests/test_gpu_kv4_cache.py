@@ -78,6 +78,34 @@ def test_append_and_gather_to_the_bit(case):
         assert (np.abs(err) <= 0.5 * step + slack).all()
 
 
+@pytest.mark.parametrize("kv,dim,tokens", [(7, 64, 9000), (7, 64, 17100), (9, 256, 3400), (3, 128, 30000), (8, 256, 14700), (40, 64, 6100)])
+def test_long_calls_equal_short_ones_to_the_bit(kv, dim, tokens):
+    """Warps that take several heads in a row, against calls of a few hundred tokens."""
+    rng = np.random.default_rng(tokens + dim)
+    lens = [tokens // 2, 0, 1, tokens // 3]
+    lens.append(tokens - sum(lens))
+    start = [3, 5, 0, 200, 63]
+    p = H.Paged(rng, [n + s for n, s in zip(lens, start)], kv, dim, 32, True)
+    before = p.device.clone()
+    x = H.draw_heads(rng, tokens, 2 * kv, dim, "bf16").to(H.DEV)
+    k, v = x[:, :kv], x[:, kv:]
+    append(p, k, v, lens, start)
+    gk, gv = gather(p, lens, start, "bf16")
+    after = p.device.clone()
+    p.device.copy_(before)
+    at, table = H.offsets(lens), p.table_device
+    for b, n in enumerate(lens):
+        p.table_device = table[b: b + 1]
+        for i in range(0, n, 600):
+            m = min(600, n - i)
+            part = slice(at[b] + i, at[b] + i + m)
+            append(p, k[part], v[part], [m], [start[b] + i])
+            pk, pv = gather(p, [m], [start[b] + i], "bf16")
+            assert torch.equal(pk, gk[part]) and torch.equal(pv, gv[part])
+    Q.qvla_check_device(H.stream())
+    assert torch.equal(p.device, after)
+
+
 def test_ties_zeros_and_small_numbers():
     """Exact half-integer quotients round to even; a head of zeros has scale 0; subnormal heads keep their codes."""
     rng = np.random.default_rng(3)
