@@ -418,9 +418,9 @@ qvla_status qvla_attention_prompt(const void* q, const void* k, const void* v, q
  *   rotate    nonzero: every head is multiplied by H / sqrt(head_dim) (H the Sylvester Hadamard matrix)
  *             ahead of the quantiser, which spreads a head's large channels (Sec. 4.1 Eq. 3, applied
  *             to the cached heads).  Queries are rotated alike, and outputs rotated back.
- * A token's head has one scale, Delta = max |y| / 7 (the float32 product with float32(1 / 7)), and codes
- * round(y / Delta) in [-7, 7], round half to even on the exact quotient of the float32 numbers (Sec. 4.2
- * Eq. 5-6 per token and head); Delta = 0 gives codes 0.
+ * A token's head has one scale, Delta = max |y| / 7 (rounded to float32), and codes clamp(round(y / Delta),
+ * -7, 7), round half to even on the exact quotient of the float32 numbers (Sec. 4.2 Eq. 5-6 per token and
+ * head); Delta = 0 gives codes 0.
  * A head with a NaN or an infinity reads back as NaN.
  * A sequence's tokens lie at positions 0, 1, 2, ...; position p of sequence b is slot p % page_size of
  * page page_table[b * max_pages + p / page_size] (device int32 [batch][max_pages]). */

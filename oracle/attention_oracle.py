@@ -25,12 +25,12 @@ def hadamard(dim):
 
 
 def quantize_heads(x, rotate):
-    """Codes int8 [..., D] and float32 scales [...] of heads x: scale max |y| times float32(1 / 7), round half to even on the exact
-    quotient (that of two float32 numbers is decided by a float64 one); a head with a NaN or an infinity has a NaN scale."""
+    """Codes int8 [..., D] and float32 scales [...] of heads x: scale max |y| / 7, round half to even on the exact quotient
+    (that of two float32 numbers is decided by a float64 one); a head with a NaN or an infinity has a NaN scale."""
     with np.errstate(all="ignore"):
         y = rotate_f32(x) if rotate else np.array(x, dtype=np.float32)
         top = np.abs(y).max(-1)
-        d = (top * (np.float32(1.0) / np.float32(7.0))).astype(np.float32)
+        d = (top / np.float32(7.0)).astype(np.float32)
         d = np.where(np.isfinite(top), d, np.float32(np.nan))
         t = y.astype(np.float64) / d[..., None].astype(np.float64)
         codes = np.where((d > 0)[..., None], np.clip(np.rint(t), -7, 7), 0.0)

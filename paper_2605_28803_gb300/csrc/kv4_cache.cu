@@ -1,6 +1,6 @@
 // The 4-bit key/value cache: tokens in (rotate, quantise, store to their pages) and tokens out.
 //
-// Per token and key/value head: y = x . H / sqrt(D) (or x), Delta = max |y| float32(1 / 7), codes clamp(round(y / Delta), -7, 7), round half
+// Per token and key/value head: y = x . H / sqrt(D) (or x), Delta = max |y| / 7, codes clamp(round(y / Delta), -7, 7), round half
 // to even on the exact quotient; out again, x^ = (Delta / sqrt(D)) (q . H), rounded to the output's type.  q . H is a vector of
 // integers of at most 7 D = 1792: exact in float16, so on the way out the rotation is float16 arithmetic, two channels an
 // instruction and a shuffle, without a rounding.
@@ -229,8 +229,8 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
 #pragma unroll
       for (int s = 1; s < kTeam; s *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
       if (h.at == nullptr) return;
-      const float d = m < 0x7f800000u ? __fmul_rn(__uint_as_float(m), 1.0f / 7.0f) : __uint_as_float(0x7fffffffu);
-      // y / d is at most 7 (1 + 2^-23) by the choice of d, so codes need no clamp.  1.5 2^23 + y r rounds to half even in the last place, whose
+      const float d = m < 0x7f800000u ? __fdiv_rn(__uint_as_float(m), 7.0f) : __uint_as_float(0x7fffffffu);
+      // y / d is at most 7 (1 + 2^-24) by the choice of d, so codes need no clamp.  1.5 2^23 + y r rounds to half even in the last place, whose
       // byte is the code; where that lies within 1e-5 of a tie (or r is no number to use) the exact decision is taken.
       const float r = __frcp_rn(d);
       const float2 r2 = make_float2(r, r), big = make_float2(12582912.0f, 12582912.0f), neg = make_float2(-12582912.0f, -12582912.0f);
