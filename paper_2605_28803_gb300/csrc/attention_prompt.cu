@@ -9,8 +9,8 @@
 //   O += P V         tcgen05 with A = P from TMEM and B = V as it lies (MN-major), O in TMEM
 // While a warpgroup works out one tile's P, the tensor cores run the other tile's products; with 256 channels O takes half of
 // TMEM, so there is one tile with two S buffers instead, and its next S is made while P is worked out.
-// The maximum that P is taken against moves only when a row's maximum has grown by more than 2^8 (p <= 256 is harmless in
-// both types, and numerator and denominator use the same one), so O is rarely read back to be rescaled.
+// The maximum that P is taken against moves only when a row's maximum has grown by more than 2^8 (numerator and denominator use
+// the same one, and both types hold the p that result), so O is rarely read back to be rescaled.
 //
 // Where a launch would leave SMs idle, a cluster of CTAs shares a group of tiles: each takes a run of the key blocks, and their O,
 // maxima and sums are joined through distributed shared memory.
@@ -43,6 +43,10 @@ static __device__ int g_debug_hold_loads;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRowsPerTile = 128;
 constexpr float kGrowth = 8.0f;  // log2 of what a row's maximum may grow by before its O is rescaled
+// P is taken against a reference below the maximum in float16, so that p reaches up to 2^15 there: of a key far below the leading one
+// 2^-32 of the leading one's weight is resolved, where 2^-25 would lose what hundreds of thousands of such keys add up to.
+template <typename T>
+constexpr float kLift = std::is_same<T, __half>::value ? 7.0f : 0.0f;  // log2
 constexpr int kLeastKeys = 256;  // of a CTA where a cluster shares a sequence's, which then has at least kSplitKeys
 constexpr int kSplitKeys = 1024;
 constexpr int kWarpLoad = 0, kWarpMma = 1, kWarpGuard = 2, kGuardWarps = 2, kWarpSoftmax = 4;
@@ -574,7 +578,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
             tmem_st_wait();
           }
         }
-        const float ref = m == -INFINITY ? 0.0f : m;  // (a row that has seen nothing yet)
+        const float ref = m == -INFINITY ? 0.0f : m - kLift<T>;  // (a row that has seen nothing yet)
         const float2 scale2 = make_float2(p.c, p.c), ref2 = make_float2(-ref, -ref);
         float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll

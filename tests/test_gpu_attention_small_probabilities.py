@@ -1,0 +1,36 @@
+"""Many keys that are each far below a leading one: together they count, so their probabilities must not be lost to float16's
+smallest numbers."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_28803_gb300 import qvla as Q
+from tests import attention_helpers as H
+
+pytestmark = pytest.mark.gpu
+
+KEYS = 1 << 18
+LEAD = 16.90625  # the leading key's score: 2^24.39 in the probabilities' ratio
+
+
+def expected(n):
+    """The others' share, and its bound: probabilities and output of 11 bits, 2^-32 of the leading one absolutely for each key, float32
+    sums of n / 64 steps."""
+    one = float(np.exp(-LEAD))
+    total = 1.0 + (n - 1) * one
+    want = (n - 1) * one / total
+    return want, want * (2.0 ** -11 + 2.0 ** -11 + n / 64 * 2.0 ** -23 + 2.0 ** -20) + n * 2.0 ** -32 / total + 2.0 ** -25
+
+
+@pytest.mark.parametrize("others", [0, 299], ids=["shared", "alone"])  # sequences without tokens: the keys are then one CTA's
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_a_prompt_of_many_keys(dim, others):
+    k, v = (torch.zeros(KEYS, 1, dim, dtype=torch.float16, device=H.DEV) for _ in range(2))
+    q = torch.zeros(1, 1, dim, dtype=torch.float16, device=H.DEV)
+    q[0, 0, 0], k[0, 0, 0] = 1.0, LEAD
+    v[1:] = 1.0
+    got = H.f64(H.prompt(q, k, v, [1] + [0] * others, [KEYS] + [0] * others, False, scale=1.0))
+    Q.qvla_check_device(H.stream())
+    want, tol = expected(KEYS)
+    assert np.abs(got - want).max() <= tol, (got.ravel()[0], want, tol)
