@@ -15,7 +15,7 @@
 // the number of tokens and cost the sum its last bits.)
 //   Dk_j multiplies the score, Dv_j the probability: p_j = exp2(s_j - r) is summed in float32, and w_j = p_j Dv_j is rounded to
 // float16 for the second product.  The row's reference r follows the largest w, not the largest p, so a weight has float16's
-// 11 bits whatever the scales' size; it moves when a w would pass 2^8 (or a p 2^96, where all scales are tiny).
+// 11 bits whatever the scales' size; it moves when a w would pass 2^15 (or a p 2^96, where all scales are tiny).
 //   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
 // float16.  That is exact for a float16 query but for rotated ones; those are taken in two parts, or their rounding
 // would show beside a float16 output's (error 1.6 times that of float32 queries; beside a bfloat16 output's it does not).
@@ -44,8 +44,10 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kMostWeight = 256.0f, kMostP = 0x1p96f;  // what a reference lets through
-constexpr float kLeastScale = -88.0f;                     // log2 of the scale below which p bounds the reference
+// What a reference lets through.  It is set 2^7 below the largest weight, so that weights use float16's range up to 2^15 and 2^-32 of the
+// largest one is resolved; with 2^-25, hundreds of thousands of tokens far below a leading one would not add up.
+constexpr float kMostWeight = 0x1p15f, kMostP = 0x1p96f, kLift = 7.0f;  // (kLift: log2)
+constexpr float kLeastScale = -81.0f;                     // log2 of the scale below which p bounds the reference
 constexpr int kTile = 16;        // cached tokens of a matrix instruction
 
 struct Kv4Params {
@@ -538,7 +540,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
 #pragma unroll
             for (int c = e; c < 4; c += 2)
               if (!hidden || sees(h, n, c))
-                top = fmaxf(top, x[h][n][c] * (dk[h][c >> 1] * f[n][e]) + fmaxf(lg2(dv[h][c >> 1]), kLeastScale));
+                top = fmaxf(top, x[h][n][c] * (dk[h][c >> 1] * f[n][e]) + (fmaxf(lg2(dv[h][c >> 1]), kLeastScale) - kLift));
 #pragma unroll
           for (int h = 4; h < 32; h *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, h));
           const float keep = ex2(m[n][e] - top);
