@@ -459,7 +459,7 @@ size_t qvla_attention_kv4_workspace_bytes(int heads, int kv_heads, int head_dim,
 /* Attention of a few query tokens of every sequence over its cached keys and values: one token while
  * decoding, a chunk of action tokens, a few speculated tokens.  The codes are multiplied as they are and
  * the scales applied to scores and probabilities; nothing is written back to memory as values.
- *   q          [total_q] tokens;  max_q >= the queries of any sequence, at most 2^24
+ *   q          [total_q] tokens, total_q * heads < 2^31 - 16;  max_q >= the queries of any sequence, at most 2^24
  *   kv_len     device int32 [batch]: cached tokens of each sequence (with causal != 0 the queries' own
  *              tokens, appended before, are the last of them);  max_len >= every kv_len, at most 2^30.  max_q and
  *              max_len shape the launch: a sequence that exceeds them is skipped, and reported by

@@ -15,6 +15,7 @@ namespace {
 constexpr int kMaxTokens = 1 << 24;
 constexpr int kMaxLength = 1 << 30;  // of a cached sequence
 constexpr int kMaxHeads = 1024;
+constexpr int64_t kMaxRows = 0x7fffffff - 16;  // query heads of a call (rows of its tiles are numbered in 32 bits, the last tile's past them)
 
 qvla_status check_heads(qvla_dtype dt, int heads, int kv_heads, int head_dim) {
   if (dt != QVLA_F16 && dt != QVLA_BF16) return fail(QVLA_ERR_INVALID_ARG, "dtype %d must be F16 or BF16", static_cast<int>(dt));
@@ -63,6 +64,9 @@ qvla_status check_batch(int batch, const void* cu, const void* table, int max_pa
   if (max_pages < 1) return fail(QVLA_ERR_INVALID_ARG, "max_pages=%d must be positive", max_pages);
   return QVLA_OK;
 }
+
+// No sequence has more queries than the call.
+int queries_at_most(int max_q, int total_q) { return max_q < total_q ? max_q : total_q; }
 
 qvla_status current_sms(int* sms) {
   int device = 0;
@@ -143,7 +147,8 @@ size_t qvla_attention_kv4_workspace_bytes(int heads, int kv_heads, int head_dim,
                                           int max_len) {
   if (heads < 1 || heads > kMaxHeads || kv_heads < 1 || heads % kv_heads != 0 ||
       (head_dim != 64 && head_dim != 128 && head_dim != 256) || batch < 1 || batch > 65535 || total_q < 1 ||
-      total_q > kMaxTokens || max_q < 1 || max_q > kMaxTokens || max_len < 1 || max_len > kMaxLength)
+      total_q > kMaxTokens || max_q < 1 || max_q > kMaxTokens || max_len < 1 || max_len > kMaxLength ||
+      static_cast<int64_t>(total_q) * heads > kMaxRows)
     return 0;
   qvla::Kv4AttentionArgs a = {};
   a.pool.kv_heads = kv_heads;
@@ -151,7 +156,7 @@ size_t qvla_attention_kv4_workspace_bytes(int heads, int kv_heads, int head_dim,
   a.heads = heads;
   a.batch = batch;
   a.total_q = total_q;
-  a.max_q = max_q;
+  a.max_q = queries_at_most(max_q, total_q);
   a.max_len = max_len;
   if (current_sms(&a.num_sms) != QVLA_OK) {
     qvla::clear_error();
@@ -176,11 +181,13 @@ qvla_status qvla_attention_kv4(const qvla_kv4_cache* cache, const void* q, qvla_
     return fail(QVLA_ERR_INVALID_ARG, "max_q=%d outside [0, 2^24] or max_len=%d outside [0, 2^30]", max_q, max_len);
   if (static_cast<int64_t>(max_len) > (static_cast<int64_t>(max_pages) << pool.log_page))
     return fail(QVLA_ERR_INVALID_ARG, "max_len=%d exceeds the %d pages of a sequence's table", max_len, max_pages);
+  if (static_cast<int64_t>(total_q) * heads > kMaxRows)
+    return fail(QVLA_ERR_UNSUPPORTED, "%d tokens of %d heads are more rows than 2^31 - 17", total_q, heads);
   if (qvla_status s = check_scale(scale)) return s;
   if (workspace_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
     return fail(QVLA_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
   if (batch == 0 || total_q == 0 || max_q == 0) return QVLA_OK;
-  qvla::Kv4AttentionArgs a = {pool, q, static_cast<int>(dt), heads, q_stride, batch, cu_q, total_q, max_q, page_table,
+  qvla::Kv4AttentionArgs a = {pool, q, static_cast<int>(dt), heads, q_stride, batch, cu_q, total_q, queries_at_most(max_q, total_q), page_table,
                               max_pages, kv_len, max_len, scale, causal ? 1 : 0, o, workspace, workspace_bytes, 0,
                               static_cast<cudaStream_t>(stream)};
   if (qvla_status s = current_sms(&a.num_sms)) return s;

@@ -196,7 +196,7 @@ struct Kv4AttentionArgs {
   int64_t q_stride;
   int batch;
   const int32_t* cu_q;
-  int total_q, max_q;
+  int total_q, max_q;      // max_q <= total_q, and total_q * heads < 2^31 - 16
   const int32_t* table;
   int max_pages;
   const int32_t* kv_len;   // device [batch]
