@@ -45,6 +45,17 @@ class AttentionBlock:
             self._ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return self._ws
 
+    def _check(self, x, lens) -> None:
+        """The library takes sizes on trust where they lie on the device: an input of other sizes would be read past its end."""
+        if len(lens) != self.batch or any(n < 0 for n in lens):
+            raise ValueError(f"lens must hold the tokens of {self.batch} sequences")
+        if any(n + new > self.max_tokens for n, new in zip(self.lens, lens)):
+            raise ValueError(f"a sequence would exceed {self.max_tokens} cached tokens")
+        if tuple(x.shape) != (sum(lens), self.qkv.K) or x.dtype != self.torch_dt or not x.is_contiguous():
+            raise ValueError(f"x must be contiguous {self.torch_dt} [{sum(lens)}, {self.qkv.K}]")
+        if x.device.type != torch.device(self.device).type:
+            raise ValueError(f"x must lie on {self.device}")
+
     def _linear(self, layer: Q.Layer, x, stream) -> torch.Tensor:
         m = x.shape[0]
         y = torch.empty(m, layer.N, dtype=self.torch_dt, device=self.device)
@@ -61,8 +72,6 @@ class AttentionBlock:
         return y[:, :q], y[:, q: q + k], y[:, q + k:]
 
     def _store(self, y, lens, cu, stream) -> None:
-        if any(n + new > self.max_tokens for n, new in zip(self.lens, lens)):
-            raise ValueError(f"a sequence would exceed {self.max_tokens} cached tokens")
         _, k, v = self._split(y)
         Q.qvla_kv4_append(self.cache, k, v, self.dt, y.stride(0), y.stride(0), self.batch, cu, y.shape[0], self.table, self.width,
                           self.lens_device, stream)
@@ -71,6 +80,7 @@ class AttentionBlock:
 
     def prefill(self, x: torch.Tensor, lens, causal: bool = True) -> torch.Tensor:
         """x [sum(lens), qkv.K]: the next lens[b] tokens of every sequence (0 for none), packed.  Returns [sum(lens), o.N]."""
+        self._check(x, lens)
         stream = torch.cuda.current_stream()
         total, fresh = sum(lens), not any(self.lens)
         cu = self._ints([sum(lens[:b]) for b in range(self.batch + 1)])
@@ -92,11 +102,12 @@ class AttentionBlock:
 
     def step(self, x: torch.Tensor, causal: bool = True) -> torch.Tensor:
         """x [batch * n, qkv.K]: the next n tokens of every sequence.  Returns [batch * n, o.N]."""
-        stream = torch.cuda.current_stream()
         total = x.shape[0]
         n = total // self.batch
         if n * self.batch != total:
             raise ValueError("x holds the same number of tokens of every sequence")
+        self._check(x, [n] * self.batch)
+        stream = torch.cuda.current_stream()
         cu = self._ints([b * n for b in range(self.batch + 1)])
         y = self._linear(self.qkv, x, stream)
         self._store(y, [n] * self.batch, cu, stream)
