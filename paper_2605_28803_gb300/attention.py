@@ -1,8 +1,9 @@
 """One attention block of the language backbone or the action head, as it is served: the fused Q/K/V linear (W4A4), attention, the
 output linear (W4A4), and a 4-bit key/value cache of its tokens.
 
-``prefill`` takes packed prompts: attention over the fresh keys and values (and over what the cache gives back where a
-sequence has tokens already), which then enter the cache.  ``step`` takes the next token or tokens of every sequence: they
+``prefill`` takes packed prompts.  A sequence without earlier tokens attends to its fresh keys and values, which then enter the
+cache; one that has tokens already attends to what the cache gives back of all its tokens, the new ones included, as it does in
+``step``.  What a sequence gets does not depend on the others.  ``step`` takes the next token or tokens of every sequence: they
 enter the cache and attend to it.  Every step of the computation is a libqvla call on the current stream; this file only
 places buffers and pages.
 """
@@ -82,19 +83,23 @@ class AttentionBlock:
         """x [sum(lens), qkv.K]: the next lens[b] tokens of every sequence (0 for none), packed.  Returns [sum(lens), o.N]."""
         self._check(x, lens)
         stream = torch.cuda.current_stream()
-        total, fresh = sum(lens), not any(self.lens)
+        total, earlier = sum(lens), self.lens
         cu = self._ints([sum(lens[:b]) for b in range(self.batch + 1)])
         y = self._linear(self.qkv, x, stream)
         q, k, v = self._split(y)
         ks = vs = y.stride(0)
         self._store(y, lens, cu, stream)
         cu_k, total_k = cu, total
-        if not fresh:  # earlier tokens come from the cache, and the new ones with them
-            total_k = sum(self.lens)
-            cu_k = self._ints([sum(self.lens[:b]) for b in range(self.batch + 1)])
-            k, v = (torch.empty(total_k, self.kv_heads * self.dim, dtype=self.torch_dt, device=self.device) for _ in range(2))
-            ks = vs = self.kv_heads * self.dim
+        if any(m and n for m, n in zip(earlier, lens)):
+            fresh, width = (k, v), self.kv_heads * self.dim
+            at = [sum(m for m, n in zip(self.lens[:b], lens) if n) for b in range(self.batch + 1)]  # keys only where there are queries
+            cu_k, total_k, ks, vs = self._ints(at), at[-1], width, width
+            k, v = (torch.empty(total_k, width, dtype=self.torch_dt, device=self.device) for _ in range(2))
             Q.qvla_kv4_gather(self.cache, self.batch, cu_k, total_k, self.table, self.width, None, k, v, self.dt, stream)
+            for b, (m, n) in enumerate(zip(earlier, lens)):
+                if n and not m:
+                    new = slice(sum(lens[:b]), sum(lens[:b]) + n)
+                    k[at[b]: at[b + 1]], v[at[b]: at[b + 1]] = fresh[0][new], fresh[1][new]
         a = torch.empty(total, self.heads * self.dim, dtype=self.torch_dt, device=self.device)
         Q.qvla_attention_prompt(q, k, v, self.dt, self.heads, self.kv_heads, self.dim, y.stride(0), ks, vs, self.batch, cu, total,
                                 cu_k, total_k, self.scale, causal, a, stream)

@@ -1,0 +1,37 @@
+"""The attention block's sequences are apart: what one gets does not depend on its neighbours' pasts."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_28803_gb300 import qvla as Q
+from tests import attention_helpers as H
+from tests.test_gpu_attention_block import DIM, K, KV, heads_of, linear, make_block
+
+pytestmark = pytest.mark.gpu
+
+
+def tokens(seed, n):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal((n, K), dtype=np.float32)).to(torch.bfloat16).to(H.DEV)
+
+
+def read_back(block, b, n):
+    k, v = (torch.empty(n, KV, DIM, dtype=torch.bfloat16, device=H.DEV) for _ in range(2))
+    Q.qvla_kv4_gather(block.cache, 1, H.ints([0, n]), n, block.table[b: b + 1], block.width, None, k, v, Q.BF16, H.stream())
+    return k, v
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_prompt_that_starts_beside_one_that_continues(causal):
+    block = make_block(5, 4)
+    block.prefill(tokens(6, 61), [20, 0, 41, 0], causal)
+    x = tokens(7, 45)
+    got = block.prefill(x, [5, 30, 0, 10], causal)
+    assert block.lens == [25, 30, 41, 10]
+    q, k, v = heads_of(linear(block.qkv, x))
+    a = [H.prompt(q[:5], *read_back(block, 0, 25), [5], [25], causal)]  # continues: over what the cache gives back
+    for new in (slice(5, 35), slice(35, 45)):                           # start: over their own keys and values
+        n = new.stop - new.start
+        a.append(H.prompt(q[new], k[new], v[new], [n], [n], causal))
+    assert torch.equal(got, linear(block.o, torch.cat(a).reshape(45, -1)))
+    Q.qvla_check_device(H.stream())
