@@ -5,7 +5,7 @@ output linear (W4A4), and a 4-bit key/value cache of its tokens.
 cache; one that has tokens already attends to what the cache gives back of all its tokens, the new ones included, as it does in
 ``step``.  What a sequence gets does not depend on the others.  ``step`` takes the next token or tokens of every sequence: they
 enter the cache and attend to it.  Every step of the computation is a libqvla call on the current stream; this file only
-places buffers and pages.
+places buffers and pages.  Calls run one after the other, also where they are made on different streams.
 """
 
 from __future__ import annotations
@@ -40,6 +40,17 @@ class AttentionBlock:
         self.lens = [0] * batch  # cached tokens, and the same on the device
         self.lens_device = torch.zeros(batch, dtype=torch.int32, device=self.device)
         self._ws = torch.empty(256, dtype=torch.uint8, device=self.device)
+        self._last = torch.cuda.current_stream() if self.pool.is_cuda else None  # of the latest call
+
+    def _stream(self) -> torch.cuda.Stream:
+        """The current stream, behind the block's latest call: the cache, the lengths and the workspace serve all calls."""
+        stream = torch.cuda.current_stream()
+        if stream != self._last:
+            stream.wait_stream(self._last)
+            for t in (self.pool, self.table, self.lens_device, self._ws):
+                t.record_stream(stream)
+            self._last = stream
+        return stream
 
     def _workspace(self, nbytes: int) -> torch.Tensor:
         if self._ws.numel() < nbytes:
@@ -82,7 +93,7 @@ class AttentionBlock:
     def prefill(self, x: torch.Tensor, lens, causal: bool = True) -> torch.Tensor:
         """x [sum(lens), qkv.K]: the next lens[b] tokens of every sequence (0 for none), packed.  Returns [sum(lens), o.N]."""
         self._check(x, lens)
-        stream = torch.cuda.current_stream()
+        stream = self._stream()
         total, earlier = sum(lens), self.lens
         cu = self._ints([sum(lens[:b]) for b in range(self.batch + 1)])
         y = self._linear(self.qkv, x, stream)
@@ -112,7 +123,7 @@ class AttentionBlock:
         if n * self.batch != total:
             raise ValueError("x holds the same number of tokens of every sequence")
         self._check(x, [n] * self.batch)
-        stream = torch.cuda.current_stream()
+        stream = self._stream()
         cu = self._ints([b * n for b in range(self.batch + 1)])
         y = self._linear(self.qkv, x, stream)
         self._store(y, [n] * self.batch, cu, stream)

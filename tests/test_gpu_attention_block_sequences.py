@@ -35,3 +35,20 @@ def test_a_prompt_that_starts_beside_one_that_continues(causal):
         a.append(H.prompt(q[new], k[new], v[new], [n], [n], causal))
     assert torch.equal(got, linear(block.o, torch.cat(a).reshape(45, -1)))
     Q.qvla_check_device(H.stream())
+
+
+def test_calls_on_different_streams_run_one_after_the_other():
+    """A call on a stream of its own finds what the latest one stored, although that one's stream is still held up."""
+    x = [tokens(8 + i, 3 * n) for i, n in enumerate((40, 1, 1, 30, 2))]
+    block, want = make_block(9, 3), []
+    for i, t in enumerate(x):
+        want.append(block.prefill(t, [len(t) // 3] * 3) if i in (0, 3) else block.step(t))
+    block, got = make_block(9, 3), []
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in x]
+    for i, (t, stream) in enumerate(zip(x, streams)):
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(20_000_000)  # some 10 ms
+            got.append(block.prefill(t, [len(t) // 3] * 3) if i in (0, 3) else block.step(t))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
