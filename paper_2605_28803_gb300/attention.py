@@ -116,6 +116,15 @@ class AttentionBlock:
                                 cu_k, total_k, self.scale, causal, a, stream)
         return self._linear(self.o, a, stream)
 
+    def rewind(self, lens) -> None:
+        """Back to the first lens[b] cached tokens of every sequence: those behind them are forgotten, and the next ones take their
+        places.  A denoising loop goes back to its observation after each step; 0 ends a sequence."""
+        if len(lens) != self.batch or any(not 0 <= n <= m for n, m in zip(lens, self.lens)):
+            raise ValueError(f"lens must hold, of {self.batch} sequences, at most the cached tokens {self.lens}")
+        self._stream()
+        self.lens = list(lens)
+        self.lens_device = self._ints(self.lens)
+
     def step(self, x: torch.Tensor, causal: bool = True) -> torch.Tensor:
         """x [batch * n, qkv.K]: the next n tokens of every sequence.  Returns [batch * n, o.N]."""
         total = x.shape[0]

@@ -40,3 +40,12 @@ def test_steps_that_do_not_fit_are_refused(x):
     with pytest.raises(ValueError):
         block.step(x)
     assert block.lens == [0, 0]
+
+
+@pytest.mark.parametrize("lens", [[11, 4], [10, 5], [10], [10, 4, 0], [-1, 4]])
+def test_rewinds_to_tokens_that_are_not_there_are_refused(lens):
+    block = make_block()
+    block.lens = [10, 4]
+    with pytest.raises(ValueError):
+        block.rewind(lens)
+    assert block.lens == [10, 4]

@@ -52,3 +52,21 @@ def test_calls_on_different_streams_run_one_after_the_other():
             got.append(block.prefill(t, [len(t) // 3] * 3) if i in (0, 3) else block.step(t))
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+def test_a_denoising_loop_over_one_observation():
+    """Every step's action tokens see the observation and one another, and none of an earlier step."""
+    observation, steps = tokens(20, 60 + 33), [tokens(21 + t, 2 * 9) for t in range(4)]
+    block = make_block(11, 2)
+    block.prefill(observation, [60, 33], causal=False)
+    for x in steps:
+        got = block.step(x, causal=False)
+        block.rewind([60, 33])
+        alone = make_block(11, 2)
+        alone.prefill(observation, [60, 33], causal=False)
+        assert torch.equal(got, alone.step(x, causal=False))
+    block.rewind([0, 33])  # a sequence ends, and another takes its place
+    x = tokens(30, 17)
+    assert torch.equal(block.prefill(x, [17, 0]), make_block(11, 2).prefill(x, [17, 0]))
+    assert block.lens == [17, 33]
+    Q.qvla_check_device(H.stream())
