@@ -395,7 +395,8 @@ qvla_status qvla_gemm_w4a8(const qvla_layer* layer, const int8_t* xq, const floa
  *    and sum, and the sum over the values are held in float32.
  *  - Indices in device memory (cu_q, cu_k, page tables, lengths) that leave the buffers they index are
  *    caught on the device: the tokens concerned are skipped, and qvla_check_device() reports
- *    QVLA_ERR_INVALID_ARG.  Offsets beyond total_q / total_k are cut off.
+ *    QVLA_ERR_INVALID_ARG.  Offsets below 0 or beyond total_q / total_k are cut off, a sequence whose
+ *    offsets decrease has no tokens, and either is reported too.
  * ------------------------------------------------------------------------------------------ */
 
 /* Attention over packed prompts.

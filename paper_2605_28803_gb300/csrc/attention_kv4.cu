@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();  // the queries, lengths and the cache may come from the previous kernel, which may still read o
   griddep_launch_dependents();
+  if (warp == 0) check_offsets(a.cu_q, a.batch, a.total_q);
   // this CTA's sequence b, chunk ch of it, key/value head and row tile
   const int unit = p.cluster ? static_cast<int>(blockIdx.x) / p.cluster : static_cast<int>(blockIdx.x);
   const int rest = unit % p.per, tile = rest % p.row_tiles, kvh = rest / p.row_tiles;
@@ -705,11 +706,11 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kv4_join_kernel(const _
     const int len = lane < a.batch ? usable_length(a, read_index<true>(a.kv_len + lane)) : 0;
     const bool found = find_sequence<true>(a.cu_q, a.batch, token, b, first);
     const Sequence seq = load_sequence<true>(a, b);
-    if (found && usable(a, seq) && seq.q0 == first) {
+    if (found && usable(a, seq) && token >= seq.q0 && token - seq.q0 < seq.n) {  // (offsets may be cut)
       const float per_length = split_of<true>(p, len);
       const int chunk = chunk_size(seq.len, chunks_of(seq.len, per_length));
       kvh = head / p.group;
-      r = (token - first) * p.group + head % p.group;
+      r = (token - seq.q0) * p.group + head % p.group;
       tile = r / p.rows;
       const int most = seen_by(seq, a.causal, (min((tile + 1) * p.rows, seq.n * p.group) - 1) / p.group);
       chunks = (most + chunk - 1) / max(chunk, 1);

@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
   const int64_t id0 = (kApart ? warp >> 1 : warp * sets) * kHeads;
   griddep_wait();  // tokens, cache, tables and offsets may come from the previous kernel, which may still read the outputs
   griddep_launch_dependents();
+  if (threadIdx.x < 32) check_offsets(a.cu, a.batch, a.total);
   if (id0 >= all) return;
   // this team's token and head, and what they move on by from set to set (no division by `heads` there)
   const int64_t id = id0 + team;
@@ -174,7 +175,7 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
     }
     if (t < first || t >= next) return;
     here = true;
-    const int64_t pos = static_cast<int64_t>(a.start ? __ldg(a.start + b) : 0) + (t - first);
+    const int64_t pos = static_cast<int64_t>(a.start ? __ldg(a.start + b) : 0) + (t - max(first, 0));
     uint8_t* const at = kv4_block(a.pool, a.table, a.max_pages, b, pos, head);
     if (at == nullptr) return;
     const int slot = static_cast<int>(pos) & ((1 << a.pool.log_page) - 1);
