@@ -140,10 +140,13 @@ __device__ __forceinline__ bool usable(const Kv4AttentionArgs& a, const Sequence
 // Cached tokens that query token i sees.
 __device__ __forceinline__ int seen_by(const Sequence& s, int causal, int i) { return causal ? max(0, s.len - s.n + i + 1) : s.len; }
 
-// The split: every sequence gets one chunk for each started `length` tokens, of equal size.
+// The split: every sequence gets one chunk for each started `length` tokens, of equal size.  The kernel that attends and the one that
+// joins both work it out, and a part placed elsewhere by one of them would be lost.  So every operation here has its rounding
+// stated (__fmul_rn, __fadd_rn; __fdividef is one approximate division of PTX), and the compiler may not contract products
+// and sums in one kernel and not in the other.
 __device__ __forceinline__ int usable_length(const Kv4AttentionArgs& a, int len) { return min(max(len, 0), a.max_len); }
 // (a quotient in float, never above the exact one)
-__device__ __forceinline__ int chunks_of(int len, float per_length) { return 1 + static_cast<int>(static_cast<float>(len - 1) * per_length); }
+__device__ __forceinline__ int chunks_of(int len, float per_length) { return 1 + static_cast<int>(__fmul_rn(static_cast<float>(len - 1), per_length)); }
 __device__ __forceinline__ int chunk_size(int len, int chunks) {
   const unsigned even = (static_cast<unsigned>(len) + chunks - 1u) / static_cast<unsigned>(chunks);
   return static_cast<int>((even + kLeastChunk - 1) / kLeastChunk * kLeastChunk);
@@ -162,18 +165,18 @@ __device__ __forceinline__ float split_of(const Kv4Params& p, int len) {
   }
   low = __reduce_add_sync(0xffffffffu, low);
   high = __reduce_add_sync(0xffffffffu, high);
-  const float all = (static_cast<float>(high) * 65536.0f + static_cast<float>(low)) * static_cast<float>(p.per);
-  const float target = static_cast<float>(all > static_cast<float>(p.target) * kLongChunk ? p.most_target : p.target);
+  const float all = __fmul_rn(__fadd_rn(__fmul_rn(static_cast<float>(high), 65536.0f), static_cast<float>(low)), static_cast<float>(p.per));
+  const float target = static_cast<float>(all > __fmul_rn(static_cast<float>(p.target), kLongChunk) ? p.most_target : p.target);
   auto inverse = [](float length) {  // of the length in whole kLeastChunk
-    return __fdividef(kLess, fmaxf(1.0f, ceilf(length * (1.0f / kLeastChunk))) * kLeastChunk);
+    return __fdividef(kLess, __fmul_rn(fmaxf(1.0f, ceilf(__fmul_rn(length, 1.0f / kLeastChunk))), kLeastChunk));
   };
-  float length = __fdividef(all, target * kLess), per_length = inverse(length);
+  float length = __fdividef(all, __fmul_rn(target, kLess)), per_length = inverse(length);
   // the remainders of the sequences come on top: lengthen the chunks until all fit the target, so that no CTA is left for a wave
   // of its own (a few tries, where the lengths are at hand)
   for (int i = 0; i < 4 && p.a.batch <= 32; ++i) {
     const float ctas = static_cast<float>(__reduce_add_sync(0xffffffffu, lane < p.a.batch ? chunks_of(len, per_length) : 0) * p.per);
     if (ctas <= target) break;
-    length = __fdividef(ctas, target * per_length) + 1.0f;
+    length = __fadd_rn(__fdividef(ctas, __fmul_rn(target, per_length)), 1.0f);
     per_length = inverse(length);
   }
   return per_length;
