@@ -43,7 +43,7 @@ cudaError_t read_and_clear_error_word_fused(unsigned int* out, cudaStream_t stre
   cudaError_t e = cudaStreamSynchronize(stream);
   if (e != cudaSuccess) return e;
   e = cudaMemcpyFromSymbol(out, g_error_word, sizeof(unsigned int));
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || *out == 0) return e;  // (cleared only where it is set: the check goes through every unit's word)
   const unsigned int zero = 0;
   return cudaMemcpyToSymbol(g_error_word, &zero, sizeof(unsigned int));
 }
