@@ -656,6 +656,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   if (!p.cluster) return;
 
   // ---- join the cluster: its CTAs take the rows in turn
+  __syncwarp();
   cluster_sync();
   const uint32_t mine = smem_u32(s_part);
   for (int r0 = 0; r0 < rows; r0 += kTeams * p.cluster) {
@@ -687,6 +688,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
       store_head<kTeam>(static_cast<T*>(a.o) + (static_cast<size_t>(token) * a.heads + head) * kDim, y, a.pool.rotate);
     }
   }
+  __syncwarp();
   cluster_sync();  // nobody leaves while its result is being read
 }
 

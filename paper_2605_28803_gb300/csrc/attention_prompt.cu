@@ -18,11 +18,11 @@
 // Keys that some row of the CTA does not see (the diagonal's blocks, a sequence's last block) need care on the value side, where
 // 0 * NaN would spread: two warps zero the rows behind the sequence's end and take NaN and infinities out of such
 // blocks; a row that does see one of those gets it back, exactly, when it is written out.
-#include <cuda.h>
 //
 // Measured: 8192 causal tokens, 16 heads of 128 channels on 4, 174 us (1580 TFLOP/s, tensor pipe 64% active: the exponentials
 // take as long as the products); 816 tokens, 8 heads of 256 on one, 15.3 us (a CTA's 13 blocks at 0.65 us, on 51 SMs); packed prompts of
 // up to 1500 over 2000 keys, 14 heads of 64 on 2, 22.2 us (the longest CTA's 16 blocks at 1.2 us).
+#include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
@@ -632,6 +632,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
 #pragma unroll 1
           for (int i = 0; i < kDim / 32; ++i) {
             uint32_t r[32];
+            __syncwarp();  // (rows add back as many values as they see; a load of TMEM wants the warp together)
             tmem_ld32(o_at + i * 32, r);
             tmem_ld_wait();
             float y[32];
@@ -651,6 +652,7 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
           float y[32];
           uint32_t r[32];
           if (n > 0) {
+            __syncwarp();
             tmem_ld32(o_at + i * 32, r);
             tmem_ld_wait();
           }
