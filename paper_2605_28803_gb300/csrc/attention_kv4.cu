@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   griddep_wait();  // the queries, lengths and the cache may come from the previous kernel, which may still read o
   griddep_launch_dependents();
-  if (warp == 0) check_offsets(a.cu_q, a.batch, a.total_q);
+  OffsetsCheck offsets(a.cu_q, a.batch, a.total_q);
   // this CTA's sequence b, chunk ch of it, key/value head and row tile
   const int unit = p.cluster ? static_cast<int>(blockIdx.x) / p.cluster : static_cast<int>(blockIdx.x);
   const int rest = unit % p.per, tile = rest % p.row_tiles, kvh = rest / p.row_tiles;
@@ -257,6 +257,7 @@ __global__ void __launch_bounds__(32 * kWarps, ctas_per_sm(kDim, 8 * kTiles)) at
       seq = {__shfl_sync(0xffffffffu, seq.q0, from), __shfl_sync(0xffffffffu, seq.n, from), __shfl_sync(0xffffffffu, seq.len, from)};
     }
   }
+  if (warp == 0) offsets.finish();
   if (b < 0) return;
   if (!usable(a, seq)) {
     if (threadIdx.x == 0) report_index();

@@ -293,8 +293,9 @@ __global__ void __launch_bounds__(Shape<kDim>::kThreads, 1)
     if (lane == 0) s_found = found ? 1 : 0;
   }
   if (warp == kWarpGuard) {
-    check_offsets(p.cu_q, p.batch, p.total_q);
-    check_offsets(p.cu_k, p.batch, p.total_k);
+    OffsetsCheck of_q(p.cu_q, p.batch, p.total_q), of_k(p.cu_k, p.batch, p.total_k);
+    of_q.finish();
+    of_k.finish();
     __syncwarp();
   }
   tc_fence_before();

@@ -38,16 +38,30 @@ __device__ __forceinline__ bool find_sequence(const int32_t* __restrict__ cu, in
 
 __device__ __forceinline__ void report_index() { atomicOr(&g_error_word, kErrIndex); }
 
-// Reports offsets that begin below 0, decrease or pass `total`; called by one warp of every CTA, which take 32 offsets in turn.  (What the
-// kernels make of them is safe without it: they are cut to [0, total], and a sequence whose offsets decrease has no tokens.)
-__device__ __forceinline__ void check_offsets(const int32_t* __restrict__ cu, int batch, int total) {
-  bool bad = false;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 32 + (threadIdx.x & 31); i <= batch; i += static_cast<int64_t>(gridDim.x) * 32) {
-    const int at = __ldg(cu + i), next = i < batch ? __ldg(cu + i + 1) : total;
-    bad |= at < 0 || next < at;
+// Reports offsets that begin below 0, decrease or pass `total`; one warp of every CTA, which take 32 offsets in turn.  (What the kernels
+// make of them is safe without it: they are cut to [0, total], and a sequence whose offsets decrease has no tokens.)  Made ahead of
+// the search for the sequence and finished after it, so that its loads run beside the search's.
+struct OffsetsCheck {
+  const int32_t* cu;
+  int batch, total, at, next;
+  int64_t i;
+  __device__ __forceinline__ OffsetsCheck(const int32_t* cu_, int batch_, int total_) : cu(cu_), batch(batch_), total(total_) {
+    i = static_cast<int64_t>(blockIdx.x) * 32 + (threadIdx.x & 31);
+    load();
   }
-  if (bad) report_index();
-}
+  __device__ __forceinline__ void load() {
+    at = i <= batch ? __ldg(cu + i) : 0;
+    next = i < batch ? __ldg(cu + i + 1) : i == batch ? total : 0;
+  }
+  __device__ __forceinline__ void finish() {
+    bool bad = at < 0 || next < at;
+    while ((i += static_cast<int64_t>(gridDim.x) * 32) <= batch) {
+      load();
+      bad |= at < 0 || next < at;
+    }
+    if (bad) report_index();
+  }
+};
 
 // Bytes of one head's tokens of a page, and the place of its parts.
 __device__ __forceinline__ size_t kv4_block_bytes(const Kv4Pool& p) { return static_cast<size_t>(p.head_dim + 8) << p.log_page; }

@@ -149,14 +149,15 @@ __global__ void __launch_bounds__(kThreads) kv4_rows_kernel(const __grid_constan
   const int64_t id0 = (kApart ? warp >> 1 : warp * sets) * kHeads;
   griddep_wait();  // tokens, cache, tables and offsets may come from the previous kernel, which may still read the outputs
   griddep_launch_dependents();
-  if (threadIdx.x < 32) check_offsets(a.cu, a.batch, a.total);
-  if (id0 >= all) return;
+  if (id0 >= all) return;  // (not a CTA's first warp)
+  OffsetsCheck offsets(a.cu, a.batch, a.total);
   // this team's token and head, and what they move on by from set to set (no division by `heads` there)
   const int64_t id = id0 + team;
   int t = static_cast<int>(all >> 31 ? id / heads : static_cast<uint32_t>(id) / static_cast<uint32_t>(heads));
   int head = static_cast<int>(id - static_cast<int64_t>(t) * heads), b, first, next;
   find_sequence(a.cu, a.batch, __shfl_sync(0xffffffffu, t, 0), b, first);
   next = __ldg(a.cu + b + 1);
+  if (threadIdx.x < 32) offsets.finish();
   const int t_on = kHeads / heads, head_on = kHeads % heads;
   const int plane = (kDim / 2) << a.pool.log_page;  // bytes of a block's key codes
 
