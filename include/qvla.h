@@ -402,7 +402,7 @@ qvla_status qvla_gemm_w4a8(const qvla_layer* layer, const int8_t* xq, const floa
 /* Attention over packed prompts.
  *   q [total_q], k and v [total_k] tokens as above; cu_k device int32 [batch + 1], may be cu_q.
  *   o device out [total_q][heads][head_dim]; rows outside every sequence are not written.
- * batch >= 0, total_q and total_k in [0, 2^24], heads <= 1024.
+ * batch in [0, 65535], total_q and total_k in [0, 2^24], heads <= 1024.
  * The probabilities are rounded to dt for the product with the values. */
 qvla_status qvla_attention_prompt(const void* q, const void* k, const void* v, qvla_dtype dt, int heads, int kv_heads,
                                   int head_dim, int64_t q_stride, int64_t k_stride, int64_t v_stride, int batch,

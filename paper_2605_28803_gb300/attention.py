@@ -3,9 +3,13 @@ output linear (W4A4), and a 4-bit key/value cache of its tokens.
 
 ``prefill`` takes packed prompts.  A sequence without earlier tokens attends to its fresh keys and values, which then enter the
 cache; one that has tokens already attends to what the cache gives back of all its tokens, the new ones included, as it does in
-``step``.  What a sequence gets does not depend on the others.  ``step`` takes the next token or tokens of every sequence: they
+``step``.  What a sequence gets does not depend on the others (but for last bits, as a call's sizes decide how it splits the
+keys).  ``step`` takes the next token or tokens of every sequence: they
 enter the cache and attend to it.  Every step of the computation is a libqvla call on the current stream; this file only
 places buffers and pages.  Calls run one after the other, also where they are made on different streams.
+
+Queries and keys reach attention as the linear gives them: a model with rotary positions makes the same calls itself, with its
+rotation between the linear and the cache.
 """
 
 from __future__ import annotations

@@ -17,8 +17,11 @@
 // float16 for the second product.  The row's reference r follows the largest w, not the largest p, so a weight has float16's
 // 11 bits whatever the scales' size; it moves when a w would pass 2^15 (or a p 2^96, where all scales are tiny).
 //   A query row is multiplied by a power of two that brings its largest entry to [0.5, 1) before it is rounded to
-// float16.  That is exact for a float16 query but for rotated ones; those are taken in two parts, or their rounding
-// would show beside a float16 output's (error 1.6 times that of float32 queries; beside a bfloat16 output's it does not).
+// float16.  A query that is not rotated keeps its bits so, but for entries that become float16 subnormals: below 2^-14 of that
+// power of two in even channels and 2^-10 in odd ones (which carry the factor 1/16), and then it is off by at most 2^-25 and 2^-21
+// of it, which is as far as a score's float32 sums resolve with the codes' offset in them.  A rotated float16 query is taken in two
+// parts, or its rounding would show beside a float16 output's (error 1.6 times that of float32 queries; beside a bfloat16
+// output's it does not).
 //
 // The cached tokens of a sequence are split into chunks over CTAs (of kWarps warps, each with every kWarps-th step).  The device
 // decides the chunks from the lengths it finds, so that a captured graph follows its lengths.  Two ways:
@@ -27,9 +30,10 @@
 //   - chunks of about equal length over all sequences, joined by a second kernel: long and short contexts of one call share
 //     the SMs evenly.
 //
-// Measured: eight contexts of 32768 to 65536 tokens, 32 heads of 128 channels on 8, 100 us (5.0 TB/s of codes; issue 61%, the reads
-// that 16 warps an SM have in flight are the bound); 23 contexts of 1 to 6001, 15.8 us, and 4 x 50 tokens over 866 with 8 heads of
-// 256 on one, 18.1 us (a CTA's own chain: finding its chunk, pages, first codes, a few steps, joins); one token over 817, 8.6 us.
+// Measured: eight contexts of 32768 to 65536 tokens, 32 heads of 128 channels on 8, 100 us (5.0 TB/s of codes; issue 62%, DRAM
+// 63%: a step's chain of products and exponentials on four warps a scheduler, and its 600 instructions); 23 contexts of 1 to 6001,
+// 15.8 us, and 4 x 50 tokens over 866 with 8 heads of 256 on one, 18.0 us (a CTA's own chain: finding its chunk, pages, first codes,
+// a few steps, joins); one token over 817, 8.6 us.
 #include <cuda_runtime.h>
 
 #include <atomic>

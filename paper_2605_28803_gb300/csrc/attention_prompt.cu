@@ -19,7 +19,7 @@
 // 0 * NaN would spread: two warps zero the rows behind the sequence's end and take NaN and infinities out of such
 // blocks; a row that does see one of those gets it back, exactly, when it is written out.
 //
-// Measured: 8192 causal tokens, 16 heads of 128 channels on 4, 174 us (1580 TFLOP/s, tensor pipe 64% active: the exponentials
+// Measured: 8192 causal tokens, 16 heads of 128 channels on 4, 174 us (1580 TFLOP/s, tensor pipe 65% active, up to 189 us under the power cap: the exponentials
 // take as long as the products); 816 tokens, 8 heads of 256 on one, 15.3 us (a CTA's 13 blocks at 0.65 us, on 51 SMs); packed prompts of
 // up to 1500 over 2000 keys, 14 heads of 64 on 2, 22.2 us (the longest CTA's 16 blocks at 1.2 us).
 #include <cuda.h>

@@ -12,8 +12,8 @@
 // A warp takes `sets` sets of 32 / team heads in a row, keys and then values of each (which lie in the same block of the cache), and
 // loads the next pass's data ahead of the present one's arithmetic; the search for the first token's sequence is made once.
 //
-// Measured, 8 heads of 128 channels: 7194 tokens in and out 24.4 us (on the way in the arithmetic's instruction issue, with the 20 warps
-// an SM that registers allow); 49611 tokens out 48.6 us, 203 MB written at 4.2 TB/s (a plain fill writes at 3.9).  Keys and
+// Measured, 8 heads of 128 channels: 7194 tokens in and out 24.8 us (on the way in the latency of a head's shuffles, maximum and rounding,
+// with the 20 warps an SM that registers allow: issue 52%, DRAM 18%); 49611 tokens out 48.9 us, 203 MB written at 4.2 TB/s (a plain fill writes at 3.9).  Keys and
 // values of a head by the same warp, which finds their block once, took 49611 tokens from 50.5 to 48.6 and 3000 tokens of 8 heads of
 // 256 from 9.9 to 7.8 us.
 #include <cuda_runtime.h>

@@ -13,14 +13,15 @@ independent their errors add up as sqrt(sum_j p_j^2 |v_j|^2); four times that is
 - the output's type: half an ulp of each channel, and half its smallest subnormal."""
 
 import numpy as np
+import torch
 
 from oracle import attention_oracle as A
 from tests import attention_helpers as H
 
 
 def rows_of(p, q, lens_q, lens_k, causal, scale=None, leave=None):
-    """Per sequence, head and query: (o in the cache's basis, probabilities, values), o [queries, heads, dim] float64; `leave`: tokens
-    (first, end) that are left out, as if a chunk of them had been lost."""
+    """Per sequence, head and query: row, head, the query, and the keys and values that it sees, float64 in the cache's basis, and the
+    scale; `leave`: tokens (first, end) that are left out, as if a chunk of them had been lost."""
     k, v = p.heads(lens_k)
     k, v, qd = k.astype(np.float64), v.astype(np.float64), H.f64(q)
     qd = qd @ A.hadamard(p.dim) if p.rotate else qd
@@ -41,7 +42,7 @@ def rows_of(p, q, lens_q, lens_k, causal, scale=None, leave=None):
 def statement(p, q, lens_q, lens_k, causal, scale=None, q_unit=0.0, warps=4, floor=2.0 ** -32, leave=None):
     """(o, bound): o [queries, heads, dim] float64 in the model's basis, and the bound of a row's 2-norm [queries, heads]."""
     o, tol = np.zeros(q.shape), np.zeros(q.shape[:2])
-    out = "f16" if str(q.dtype).endswith("float16") and "b" not in str(q.dtype).split(".")[-1] else "bf16"
+    out = "f16" if q.dtype == torch.float16 else "bf16"
     for i, h, qi, k, v, scale_ in rows_of(p, q, lens_q, lens_k, causal, scale, leave):
         if len(k) == 0:
             continue
