@@ -28,8 +28,7 @@
 
 #include <atomic>
 #include <mutex>
-#include <set>
-#include <utility>
+#include <type_traits>
 
 #include "griddep.cuh"
 #include "kv4.cuh"
@@ -718,17 +717,17 @@ cudaError_t make_tmap_heads(CUtensorMap* m, const void* base, int bf16, int dim,
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// Raise a kernel's dynamic shared-memory limit, once per kernel and device.
-cudaError_t prepare_kernel(const void* kern, int smem) {
-  static std::mutex mu;
-  static std::set<std::pair<const void*, int>> done;
+// Raise a kernel's dynamic shared-memory limit, once per kernel and device.  (A set of them could throw, through the C entry.)
+template <typename T, int kDim, bool kSplit>
+cudaError_t prepare_kernel() {
+  static std::atomic<uint64_t> raised{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  std::lock_guard<std::mutex> lock(mu);
-  if (done.count({kern, dev})) return cudaSuccess;
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess) done.insert({kern, dev});
+  const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
+  if (raised.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(attention_prompt_kernel<T, kDim, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<kDim>::kSmem);
+  if (e == cudaSuccess) raised.fetch_or(bit, std::memory_order_relaxed);
   return e;
 }
 
@@ -755,7 +754,7 @@ int resident_clusters(int size) {
   cfg.numAttrs = 1;
   int n = 0;
   auto kern = attention_prompt_kernel<T, kDim, true>;
-  if (prepare_kernel(reinterpret_cast<const void*>(kern), C::kSmem) != cudaSuccess ||
+  if (prepare_kernel<T, kDim, true>() != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
     cudaGetLastError();  // (plain launches do without)
     n = 0;
@@ -809,7 +808,7 @@ cudaError_t launch(const PromptArgs& a) {
   while (split > 1 && resident_clusters<T, kDim>(static_cast<int>(split)) < ctas) --split;
   p.split = split < 2 ? 1 : static_cast<int>(split);
   auto kern = p.split > 1 ? attention_prompt_kernel<T, kDim, true> : attention_prompt_kernel<T, kDim, false>;
-  e = prepare_kernel(reinterpret_cast<const void*>(kern), C::kSmem);
+  e = p.split > 1 ? prepare_kernel<T, kDim, true>() : prepare_kernel<T, kDim, false>();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ctas * p.split));
