@@ -476,9 +476,138 @@ qvla_status qvla_attention_kv4(const qvla_kv4_cache* cache, const void* q, qvla_
                                int max_pages, const int32_t* kv_len, int max_len, float scale, int causal, void* o,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: the linear with codes that sm_103a's tensor cores take as they are.
+ *
+ * A code is E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 to 7) and their negatives (bit 3); byte j of a row holds code 2j in its low
+ * nibble and 2j + 1 in its high one.  Consecutive channels share a block scale:
+ *   QVLA_MXFP4  32 channels, E8M0 (byte b: 2^(b - 127), 255 NaN).
+ *               e = floor(log2 max |z|) - 2, at least -127; codes E2M1(z / 2^e), values above 6 becoming 6.
+ *   QVLA_NVFP4  16 channels, E4M3, and a float32 scale Delta of the row.
+ *               Delta = max_row |z| / 2688 (rounded to float32), or the step's scale; s = E4M3(max_block |z| / (6 Delta)), at most
+ *               448; codes E2M1(z / D), D = s Delta rounded to float32; an entry stands for code * s * Delta.
+ * Roundings are to nearest, ties to the even code, decided on the exact quotient of the float32 numbers.  z is the row, or with
+ * had_block > 1 the row times BlockDiag(H_b / sqrt(b)) (Sec. 4.1 Eq. 3): float32 butterflies of distance b/2, b/4, ..., 1,
+ * then one float32 product.  A block of zeros has codes 0 (of either sign) and scale 0.  A row with a NaN or an infinity has
+ * no finite meaning: an MX block that holds one has scale 255; in NV it makes Delta NaN, and with a step's scale a NaN
+ * makes its block's scale NaN and an infinity is clamped.
+ *   Block scales lie in tiles of 128 rows x 4 blocks, 512 bytes each, tile (m / 128, b / 4) of a row-major grid of
+ * ceil(rows / 128) x (blocks / 4): the scale of row m and block b is byte (m % 32) * 16 + (m / 32 % 4) * 4 + b % 4 of its tile.
+ * Bytes of rows past the last one are neither written nor used.  Shapes as above: K % 128 == 0, K <= 16384, N % 16 == 0, b up to 4096.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { QVLA_MXFP4 = 0, QVLA_NVFP4 = 1 } qvla_fp4_format;
+
+/* Bytes of the block scales of `rows` rows; 0 for a format or shape that the calls below refuse. */
+size_t qvla_fp4_scale_bytes(qvla_fp4_format fmt, int rows, int K);
+
+/* Rotate and quantise rows.  x device [M] rows of K, x_stride elements apart (a multiple of 8, at least K; x 16-byte aligned).
+ *   step_scale  device, one positive float32 in the place of every row's Delta, or NULL (NULL for MX)
+ *   xq          device out [M][K/2], 16-byte aligned;  xs  device out, 16-byte aligned, qvla_fp4_scale_bytes(fmt, M, K) bytes
+ *   xscale      device out [M] float32: Delta.  Not touched for MX, and may be NULL then. */
+qvla_status qvla_fp4_quantize_rows(const void* x, qvla_dtype xdt, int64_t x_stride, int M, int K, int had_block,
+                                   qvla_fp4_format fmt, const float* step_scale, uint8_t* xq, uint8_t* xs, float* xscale,
+                                   void* stream);
+
+/* What the codes stand for, in the rotated basis: code * block scale * Delta in float32, rounded to odt (F16, BF16 or F32).
+ *   out device [M][K], 16-byte aligned; xscale is not read for MX. */
+qvla_status qvla_fp4_dequantize_rows(const uint8_t* xq, const uint8_t* xs, const float* xscale, qvla_fp4_format fmt, int M,
+                                     int K, void* out, qvla_dtype odt, void* stream);
+
+/* Fold and quantise weights on the host: the fold is qvla_pack_weights_host's (P, U_b and the Hadamard block in float64, one
+ * rounding to float32), the codes those of a row above.
+ *   wq host out [N][K/2];  ws host out, qvla_fp4_scale_bytes(fmt, N, K) bytes (bytes of no row become 0);
+ *   wscale host out [N] float32: Delta of each output channel.  Not touched for MX, and may be NULL then. */
+qvla_status qvla_fp4_pack_weights_host(const void* W, qvla_dtype wdt, int N, int K, const double* rot, int rot_block,
+                                       const int32_t* perm, int had_block, qvla_fp4_format fmt, uint8_t* wq, uint8_t* ws,
+                                       float* wscale);
+
+/* A device-resident layer of such weights.  Its device must be current in the calls that take it (QVLA_ERR_INVALID_ARG). */
+typedef struct qvla_fp4_layer qvla_fp4_layer;
+
+/* Upload packed weights (synchronous; the layer owns what it allocates).  Arrays as qvla_fp4_pack_weights_host writes them;
+ * wscale NULL for MX; bias host [N] float32 or NULL.  xdt (F16, BF16 or F32) is what qvla_fp4_linear takes, ydt (F16 or BF16)
+ * the output.  A NaN or negative block scale, or a wscale that is not finite and non-negative, is refused. */
+qvla_status qvla_fp4_layer_create(int N, int K, int had_block, qvla_fp4_format fmt, qvla_dtype xdt, qvla_dtype ydt,
+                                  const uint8_t* wq, const uint8_t* ws, const float* wscale, const float* bias,
+                                  qvla_fp4_layer** out);
+
+/* The gate and up projections of a gated MLP as one layer, H output channels (H % 128 == 0): the arrays hold 2H rows, H gate
+ * rows and then H up rows.  Its output is ydt(gelu_tanh(gate) * up) [M][H], gate and up in float32. */
+qvla_status qvla_fp4_layer_create_gated(int H, int K, int had_block, qvla_fp4_format fmt, qvla_dtype xdt, qvla_dtype ydt,
+                                        const uint8_t* wq, const uint8_t* ws, const float* wscale, const float* bias,
+                                        qvla_fp4_layer** out);
+
+/* Free a layer (synchronises the device first).  NULL is a no-op. */
+qvla_status qvla_fp4_layer_destroy(qvla_fp4_layer* layer);
+
+/* The product of quantised rows and a layer: y[m,n] = ydt(fma(acc, xscale[m] * wscale[n], bias[n])), acc the float32 sum over
+ * k of (code * block scale) of both; with MX xscale and wscale are 1.
+ *   xq, xs, xscale  as qvla_fp4_quantize_rows writes them (16-byte aligned; xscale is not read for MX)
+ *   y               device out [M][N] (gated: [M][H]) of ydt, 16-byte aligned
+ * The sums' order depends on the call's sizes; the same call gives the same bits. */
+qvla_status qvla_gemm_fp4(const qvla_fp4_layer* layer, const uint8_t* xq, const uint8_t* xs, const float* xscale, int M,
+                          void* y, void* stream);
+
+/* Bytes of device workspace of qvla_fp4_linear for M rows (a multiple of 256). */
+size_t qvla_fp4_linear_workspace_bytes(const qvla_fp4_layer* layer, int M);
+
+/* The whole linear: the layer's rotation and quantiser on x (device [M][K] of xdt, dense), then the product.  step_scale as
+ * in qvla_fp4_quantize_rows; workspace as in qvla_w4a4_linear. */
+qvla_status qvla_fp4_linear(const qvla_fp4_layer* layer, const void* x, int M, const float* step_scale, void* y,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * What runs between two blocks (attention, MLP) of a layer: the residual takes a block's output, gated and normalised where
+ * the model does so, and the next block's input is the residual's norm, modulated where the model conditions it.
+ *   u  = y, or with post_norm != 0  norm(y) * (post_weight + weight_offset)
+ *   r' = residual_scale * r + gate * u                         rounded to the residual's type, stored
+ *   h  = (norm(r') * (pre_weight + weight_offset) + pre_bias) * (1 + scale) + shift     rounded to dt
+ * with norm(x) = x / sqrt(mean(x^2) + eps)                 (QVLA_NORM_RMS)
+ *        norm(x) = (x - mean x) / sqrt(mean((x - mean x)^2) + eps)  (QVLA_NORM_LAYER)
+ * in float32 over a row's K channels.  A norm reads r' as it is stored.  A factor or term whose pointer is NULL is left out.
+ * Squares that leave float32's range make a row's norm 0 or NaN.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { QVLA_NORM_RMS = 0, QVLA_NORM_LAYER = 1 } qvla_norm_kind;
+
+typedef struct {
+  qvla_norm_kind kind;      /* of both norms */
+  float eps;                /* positive */
+  float weight_offset;      /* added to both weights: 1 where a model stores them less one */
+  float residual_scale;
+  int post_norm;
+  const void* post_weight;  /* device [K] of dt, as pre_weight and pre_bias, or NULL */
+  const void* pre_weight;
+  const void* pre_bias;
+  const void* gate;         /* device, mod_rows rows of K of dt, mod_stride elements apart (a multiple of 8), or NULL */
+  const void* scale;
+  const void* shift;
+  int64_t mod_stride;
+  int mod_rows;
+  int mod_tokens;             /* token m takes row m / mod_tokens, */
+  const int32_t* mod_index;   /* or, where this is not NULL, row mod_index[m] (device int32 [M]): a token whose row is not
+                                 in [0, mod_rows) is skipped, nothing of it is written, and qvla_check_device() reports
+                                 QVLA_ERR_INVALID_ARG */
+} qvla_block_norm_params;
+
+/* One junction with its output in 16 bits.
+ *   r  device [M] rows of K of rdt (dt, or F32), r_stride elements apart (a multiple of 8)
+ *   y  device, the block's output, rows of dt y_stride elements apart, or NULL: no block has run yet
+ *   r_out  device, rows r_stride apart; may be r.  NULL where y is NULL and residual_scale is 1: r is left as it is
+ *   h  device out [M][K] of dt (F16 or BF16), dense, or NULL: the residual alone
+ * Pointers are 16-byte aligned; K % 8 == 0, K <= 16384, M in [0, 2^20].  h and r_out overlap no input (r_out may be r itself). */
+qvla_status qvla_block_norm(const qvla_block_norm_params* norm, qvla_dtype dt, const void* r, qvla_dtype rdt, int64_t r_stride,
+                            const void* y, int64_t y_stride, int M, int K, void* r_out, void* h, void* stream);
+
+/* The same with h rotated and quantised as by qvla_fp4_quantize_rows (which it equals, on h rounded to dt): hq, hs and hscale
+ * are that call's xq, xs and xscale.  h may be NULL.  K % 128 == 0. */
+qvla_status qvla_block_norm_fp4(const qvla_block_norm_params* norm, qvla_dtype dt, const void* r, qvla_dtype rdt,
+                                int64_t r_stride, const void* y, int64_t y_stride, int M, int K, void* r_out, void* h,
+                                int had_block, qvla_fp4_format fmt, const float* step_scale, uint8_t* hq, uint8_t* hs,
+                                float* hscale, void* stream);
+
 /* Synchronise `stream`, then report (and clear) the device-side error words: QVLA_OK,
  * QVLA_ERR_TIMEOUT if a kernel gave up waiting since the last check, or QVLA_ERR_INVALID_ARG if an
- * attention or cache kernel met an index in device memory that it had to skip. */
+ * attention, cache or norm kernel met an index in device memory that it had to skip. */
 qvla_status qvla_check_device(void* stream);
 
 #ifdef __cplusplus

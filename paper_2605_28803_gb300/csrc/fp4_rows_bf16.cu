@@ -1,0 +1,8 @@
+// Rows of bf16 to 4-bit floating point (fp4_rows.cuh).
+#include "fp4_rows.cuh"
+
+namespace qvla {
+
+cudaError_t launch_fp4_quantize_bf16(const RowsArgs& a) { return fp4::launch_quant<__nv_bfloat16, __nv_bfloat16, false>(a); }
+
+}  // namespace qvla

@@ -213,4 +213,61 @@ size_t attention_kv4_workspace(const Kv4AttentionArgs& a);
 cudaError_t launch_attention_kv4(const Kv4AttentionArgs& a);
 cudaError_t read_and_clear_error_word_attention_kv4(unsigned int* out, cudaStream_t stream);
 
+// Rows to 4-bit floating point, and the norms around a block (fp4_rows.cuh).  A token's conditioning (gate, scale and shift of
+// one type with the branch) is row mod_index[m], or m / mod_tokens, of [mod_rows] rows mod_stride elements apart.
+struct NormArgs {
+  int layer;  // subtract the mean
+  float eps, weight_offset, residual_scale;
+  int post_norm;
+  const void *post_weight, *pre_weight, *pre_bias, *gate, *scale, *shift;
+  int64_t mod_stride;
+  int mod_rows, mod_tokens;
+  const int32_t* mod_index;
+};
+struct RowsArgs {
+  const void* x;       // the rows, or the residual
+  int xdt, dt;         // their type; the branch's and h's
+  int64_t x_stride;
+  int M, K;
+  NormArgs norm;
+  const void* y;       // branch, or null
+  int64_t y_stride;
+  void* residual_out;  // or null
+  void* h;             // or null
+  // the quantiser
+  int log_b, fmt;
+  float inv_sqrt_b;
+  const float* step_scale;
+  uint8_t *codes, *scales;
+  float* row_scale;
+  int row_warps, rows_per_cta;  // set by the launch
+  int num_sms;
+  cudaStream_t stream;
+};
+cudaError_t launch_fp4_quantize_f16(const RowsArgs& a);
+cudaError_t launch_fp4_quantize_bf16(const RowsArgs& a);
+cudaError_t launch_fp4_quantize_f32(const RowsArgs& a);
+cudaError_t launch_norm_f16(const RowsArgs& a);   // codes null: h only
+cudaError_t launch_norm_bf16(const RowsArgs& a);
+cudaError_t read_and_clear_error_word_norm_f16(unsigned int* out, cudaStream_t stream);
+cudaError_t read_and_clear_error_word_norm_bf16(unsigned int* out, cudaStream_t stream);
+cudaError_t launch_fp4_dequantize(const uint8_t* codes, const uint8_t* scales, const float* row_scale, int fmt, int M, int K,
+                                  void* out, int odt, cudaStream_t stream);
+
+// y = x W^T of 4-bit floating point (fp4_gemm.cu).
+struct Fp4GemmArgs {
+  const uint8_t *xq, *xs;  // [M][K/2] codes, scale tiles
+  const float* xrow;       // [M], or null (MX)
+  const uint8_t *wq, *ws;  // the layer's: [N][K/2] codes, scale tiles of N rows rounded up to 256
+  const float *wrow, *bias;  // [N]
+  int fmt, ydt, gated;     // gated: rows in turns of 32 gate rows and the 32 up rows that go with them
+  int M, N, K;             // N = weight rows
+  void* y;                 // [M][N] (gated: N / 2)
+  int num_sms;
+  cudaStream_t stream;
+};
+cudaError_t launch_fp4_gemm(const Fp4GemmArgs& a);
+cudaError_t read_and_clear_error_word_fp4(unsigned int* out, cudaStream_t stream);
+cudaError_t set_debug_hooks_fp4(unsigned long long wait_limit_ns, int hold_loads);
+
 }  // namespace qvla

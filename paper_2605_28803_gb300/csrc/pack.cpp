@@ -19,6 +19,8 @@
 #include <cfenv>
 #include <cmath>
 #include <cstring>
+#include <functional>
+#include <system_error>
 #include <thread>
 #include <vector>
 
@@ -138,6 +140,65 @@ void pack_row(const void* W, int wdt, int K, int n, const double* rot, int rot_b
   if (wsum) wsum[n] = sum;
 }
 
+// A non-negative number to the nearest of 1 + bits significant bits, half to even, with the spacing of exponent `low` below it,
+// and at most `high`.  A quotient of float32 numbers that is no tie lies further from every tie than its float64 rounding moves it.
+double round_float(double x, int bits, int low, double high) {
+  if (!(x > 0.0)) return 0.0;
+  int e;
+  std::frexp(x, &e);  // x = f 2^e, f in [1/2, 1)
+  const double step = std::ldexp(1.0, std::max(e - 1, low) - bits);
+  return std::min(std::nearbyint(x / step) * step, high);
+}
+
+// The bits of a non-negative value that a small float with `bits` mantissa bits and exponent bias `bias` holds exactly.
+int small_float_bits(double v, int bits, int bias) {
+  if (v == 0.0) return 0;
+  int e;
+  std::frexp(v, &e);
+  const int biased = std::max(e - 1 + bias, 0);
+  const int scale = std::max(biased, 1) - bias;
+  const int significand = static_cast<int>(std::ldexp(v, bits - scale));  // with the leading one of a normal number
+  return biased > 0 ? (biased << bits) + significand - (1 << bits) : significand;
+}
+
+// A row of n float32 values to 4-bit floating point; put(block, byte) takes the block scales.
+template <typename Put>
+void fp4_row(const float* f, int n, int fmt, uint8_t* codes, float* delta, Put put) {
+  const int per = fmt == 0 ? 32 : 16;
+  float top = 0.0f;
+  for (int k = 0; k < n; ++k) top = std::max(top, std::fabs(f[k]));
+  const float d = top / 2688.0f;
+  if (fmt == 1) *delta = d;
+  for (int b = 0; b < n / per; ++b) {
+    float a = 0.0f;
+    for (int k = b * per; k < (b + 1) * per; ++k) a = std::max(a, std::fabs(f[k]));
+    double unit = 0.0;  // what a code of 1 stands for
+    int byte = 0;
+    if (fmt == 0) {
+      if (a > 0.0f) {
+        int e;
+        std::frexp(a, &e);
+        const int x = std::max(e - 1 - 2, -127);
+        byte = x + 127;
+        unit = std::ldexp(1.0, x);
+      }
+    } else if (d > 0.0f) {
+      const double s = round_float(static_cast<double>(a) / (6.0 * static_cast<double>(d)), 3, -6, 448.0);
+      byte = small_float_bits(s, 3, 7);
+      unit = static_cast<double>(static_cast<float>(s) * d);
+    }
+    put(b, static_cast<uint8_t>(byte));
+    for (int k = b * per; k < (b + 1) * per; k += 2) {
+      int c[2];
+      for (int i = 0; i < 2; ++i) {
+        const double q = unit > 0.0 ? std::fabs(static_cast<double>(f[k + i])) / unit : 0.0;
+        c[i] = small_float_bits(round_float(q, 1, 0, 6.0), 1, 1) | (std::signbit(f[k + i]) ? 8 : 0);
+      }
+      codes[k / 2] = static_cast<uint8_t>(c[0] | (c[1] << 4));
+    }
+  }
+}
+
 }  // namespace
 
 void pack_weights_host_impl(const void* W, int wdt, int N, int K, const double* rot, int rot_block,
@@ -160,6 +221,57 @@ void pack_weights_host_impl(const void* W, int wdt, int N, int K, const double* 
   for (unsigned i = 1; i < nt; ++i) pool.emplace_back(worker);
   worker();
   for (auto& t : pool) t.join();
+}
+
+bool fp4_pack_weights_host_impl(const void* W, int wdt, int N, int K, const double* rot, int rot_block, const int32_t* perm,
+                                int had_block, int fmt, uint8_t* wq, uint8_t* ws, float* wscale) {
+  const int groups = K / (fmt == 0 ? 128 : 64);  // scale tiles side by side
+  std::memset(ws, 0, static_cast<size_t>((N + 127) / 128) * groups * 512);
+  unsigned nt = std::max(1u, std::min(32u, std::thread::hardware_concurrency()));
+  nt = std::min<unsigned>(nt, static_cast<unsigned>(N));
+  std::atomic<int> next{0};
+  std::atomic<bool> finite{true};
+  struct Scratch {
+    std::vector<double> a, b;
+    std::vector<float> f;
+  };
+  std::vector<Scratch> scratch(nt);  // allocated here, where a failure can be caught: a worker allocates nothing
+  for (auto& s : scratch) {
+    s.a.resize(K);
+    s.b.resize(K);
+    s.f.resize(K);
+  }
+  auto worker = [&](Scratch& s) {
+    std::fesetround(FE_TONEAREST);
+    for (;;) {
+      const int n = next.fetch_add(1);
+      if (n >= N) break;
+      fold_row(W, wdt, K, n, rot, rot_block, perm, had_block, s.a, s.b);
+      bool ok = true;
+      for (int k = 0; k < K; ++k) {
+        s.f[k] = static_cast<float>(s.a[k]);
+        ok = ok && std::isfinite(s.f[k]);
+      }
+      if (!ok) {
+        finite = false;
+        break;
+      }
+      fp4_row(s.f.data(), K, fmt, wq + static_cast<size_t>(n) * (K / 2), wscale ? wscale + n : nullptr, [&](int block, uint8_t byte) {
+        ws[(static_cast<size_t>(n / 128) * groups + block / 4) * 512 + (n % 32) * 16 + (n / 32 % 4) * 4 + block % 4] = byte;
+      });
+    }
+  };
+  std::vector<std::thread> pool;
+  pool.reserve(nt);
+  try {
+    for (unsigned i = 1; i < nt; ++i) pool.emplace_back(worker, std::ref(scratch[i]));
+  } catch (const std::system_error&) {  // fewer threads then
+  }
+  const int rounding = std::fegetround();
+  worker(scratch[0]);
+  std::fesetround(rounding);
+  for (auto& t : pool) t.join();
+  return finite;
 }
 
 namespace {

@@ -16,6 +16,8 @@ import numpy as np
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libqvla.so")
 
 F16, BF16, F32 = 0, 1, 2
+MXFP4, NVFP4 = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
 DTYPE_CODES = {"f16": F16, "bf16": BF16, "f32": F32}
 
 STATUS = {0: "QVLA_OK", 1: "QVLA_ERR_INVALID_ARG", 2: "QVLA_ERR_UNSUPPORTED", 3: "QVLA_ERR_CUDA",
@@ -64,6 +66,18 @@ SIGNATURES = {
     "qvla_kv4_gather": (_I, [_P, _I, _P, _I, _P, _I, _P, _P, _P, _I, _P]),
     "qvla_attention_kv4_workspace_bytes": (_S, [_I, _I, _I, _I, _I, _I, _I]),
     "qvla_attention_kv4": (_I, [_P, _P, _I, _I, _L, _I, _P, _I, _I, _P, _I, _P, _I, _F, _I, _P, _P, _S, _P]),
+    "qvla_fp4_scale_bytes": (_S, [_I, _I, _I]),
+    "qvla_fp4_quantize_rows": (_I, [_P, _I, _L, _I, _I, _I, _I, _P, _P, _P, _P, _P]),
+    "qvla_fp4_dequantize_rows": (_I, [_P, _P, _P, _I, _I, _I, _P, _I, _P]),
+    "qvla_fp4_pack_weights_host": (_I, [_P, _I, _I, _I, _P, _I, _P, _I, _I, _P, _P, _P]),
+    "qvla_fp4_layer_create": (_I, [_I, _I, _I, _I, _I, _I, _P, _P, _P, _P, ctypes.POINTER(_P)]),
+    "qvla_fp4_layer_create_gated": (_I, [_I, _I, _I, _I, _I, _I, _P, _P, _P, _P, ctypes.POINTER(_P)]),
+    "qvla_fp4_layer_destroy": (_I, [_P]),
+    "qvla_gemm_fp4": (_I, [_P, _P, _P, _P, _I, _P, _P]),
+    "qvla_fp4_linear_workspace_bytes": (_S, [_P, _I]),
+    "qvla_fp4_linear": (_I, [_P, _P, _I, _P, _P, _P, _S, _P]),
+    "qvla_block_norm": (_I, [_P, _I, _P, _I, _L, _P, _L, _I, _I, _P, _P, _P]),
+    "qvla_block_norm_fp4": (_I, [_P, _I, _P, _I, _L, _P, _L, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P]),
     "qvla_debug_gemm_plan_codes": (_I, [_I, _I, _I, _I, _I, _I, _I, _P, _P]),
 }
 
@@ -370,6 +384,135 @@ def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, b
                                      page_table.data_ptr(), max_pages, kv_len.data_ptr(), max_len, scale, 1 if causal else 0,
                                      o.data_ptr(), None if workspace is None else workspace.data_ptr(), workspace_bytes,
                                      _stream(stream))
+    if status:
+        _check(status)
+
+
+# 4-bit floating point and the norms around a block
+
+def qvla_fp4_scale_bytes(fmt: int, rows: int, K: int) -> int:
+    return int(_lib.qvla_fp4_scale_bytes(fmt, rows, K))
+
+
+def qvla_fp4_quantize_rows(x, xdt: int, x_stride: int, M: int, K: int, had_block: int, fmt: int, step_scale, xq, xs, xscale=None,
+                           stream=None) -> None:
+    """Rotate and quantise rows to E2M1 codes and block scales (NVFP4: and a float32 scale a row)."""
+    status = _lib.qvla_fp4_quantize_rows(x.data_ptr(), xdt, x_stride, M, K, had_block, fmt, _ptr(step_scale), xq.data_ptr(),
+                                         xs.data_ptr(), _ptr(xscale), _stream(stream))
+    if status:
+        _check(status)
+
+
+def qvla_fp4_dequantize_rows(xq, xs, xscale, fmt: int, M: int, K: int, out, odt: int, stream=None) -> None:
+    """What the codes stand for, in the rotated basis."""
+    status = _lib.qvla_fp4_dequantize_rows(xq.data_ptr(), xs.data_ptr(), _ptr(xscale), fmt, M, K, out.data_ptr(), odt,
+                                           _stream(stream))
+    if status:
+        _check(status)
+
+
+def qvla_fp4_pack_weights_host(W: np.ndarray, wdt: int, N: int, K: int, rot=None, rot_block: int = 0, perm=None,
+                               had_block: int = 1, fmt: int = NVFP4, wq=None, ws=None, wscale=None) -> None:
+    """Host-only fold + quantise + pack into caller-provided numpy buffers."""
+    _check(_lib.qvla_fp4_pack_weights_host(_ptr(W), wdt, N, K, _ptr(rot), rot_block, _ptr(perm), had_block, fmt, _ptr(wq), _ptr(ws),
+                                           _ptr(wscale)))
+
+
+class Fp4Layer:
+    """Owner of a qvla_fp4_layer handle; ``close()`` (or garbage collection) destroys it."""
+
+    def __init__(self, handle: int, N: int, K: int, had_block: int, fmt: int, xdt: int, ydt: int, gated: bool):
+        self.handle, self.N, self.K, self.had_block, self.fmt, self.xdt, self.ydt = handle, N, K, had_block, fmt, xdt, ydt
+        self.gated = gated  # N is the output width (H); the weight rows are 2H
+
+    def close(self) -> None:
+        if self.handle:
+            _check(_lib.qvla_fp4_layer_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _fp4_layer(create, N, K, had_block, fmt, xdt, ydt, wq, ws, wscale, bias, gated):
+    h = ctypes.c_void_p()
+    _check(create(N, K, had_block, fmt, xdt, ydt, _ptr(wq), _ptr(ws), _ptr(wscale), _ptr(bias), ctypes.byref(h)))
+    return Fp4Layer(h.value, N, K, had_block, fmt, xdt, ydt, gated)
+
+
+def qvla_fp4_layer_create(N: int, K: int, had_block: int, fmt: int, xdt: int, ydt: int, wq: np.ndarray, ws: np.ndarray,
+                          wscale=None, bias=None) -> Fp4Layer:
+    return _fp4_layer(_lib.qvla_fp4_layer_create, N, K, had_block, fmt, xdt, ydt, wq, ws, wscale, bias, False)
+
+
+def qvla_fp4_layer_create_gated(H: int, K: int, had_block: int, fmt: int, xdt: int, ydt: int, wq: np.ndarray, ws: np.ndarray,
+                                wscale=None, bias=None) -> Fp4Layer:
+    """Gate + up projections as one layer (arrays of H gate rows, then H up rows) whose output is gelu(gate) * up."""
+    return _fp4_layer(_lib.qvla_fp4_layer_create_gated, H, K, had_block, fmt, xdt, ydt, wq, ws, wscale, bias, True)
+
+
+def qvla_gemm_fp4(layer: Fp4Layer, xq, xs, xscale, M: int, y, stream=None) -> None:
+    status = _lib.qvla_gemm_fp4(layer.handle, xq.data_ptr(), xs.data_ptr(), _ptr(xscale), M, y.data_ptr(), _stream(stream))
+    if status:
+        _check(status)
+
+
+def qvla_fp4_linear_workspace_bytes(layer: Fp4Layer, M: int) -> int:
+    return int(_lib.qvla_fp4_linear_workspace_bytes(layer.handle, M))
+
+
+def qvla_fp4_linear(layer: Fp4Layer, x, M: int, step_scale, y, workspace, workspace_bytes: int, stream=None) -> None:
+    status = _lib.qvla_fp4_linear(layer.handle, x.data_ptr(), M, _ptr(step_scale), y.data_ptr(), _ptr(workspace), workspace_bytes,
+                                  _stream(stream))
+    if status:
+        _check(status)
+
+
+class _NormStruct(ctypes.Structure):
+    _fields_ = [("kind", _I), ("eps", _F), ("weight_offset", _F), ("residual_scale", _F), ("post_norm", _I),
+                ("post_weight", _P), ("pre_weight", _P), ("pre_bias", _P), ("gate", _P), ("scale", _P), ("shift", _P),
+                ("mod_stride", _L), ("mod_rows", _I), ("mod_tokens", _I), ("mod_index", _P)]
+
+
+class BlockNorm:
+    """The norms, gate and modulation of one place between two blocks (qvla_block_norm_params), of type dt.  gate, scale and
+    shift are 2-D tensors of the same rows and row stride (slices of one conditioning output, say) or None; token m takes row
+    m // mod_tokens, or mod_index[m] (int32).  The tensors are kept alive and read at each call."""
+
+    __slots__ = ("dt", "tensors", "struct", "ref")
+
+    def __init__(self, kind: int, dt: int, eps: float = 1e-6, weight_offset: float = 0.0, residual_scale: float = 1.0,
+                 post_norm: bool = False, post_weight=None, pre_weight=None, pre_bias=None, gate=None, scale=None, shift=None,
+                 mod_tokens: int = 0, mod_index=None):
+        mods = [t for t in (gate, scale, shift) if t is not None]
+        if any(t.dim() != 2 or t.stride(1) != 1 or t.shape != mods[0].shape or t.stride(0) != mods[0].stride(0) for t in mods):
+            raise ValueError("gate, scale and shift must be 2-D with the same rows, row stride and contiguous channels")
+        self.dt = dt
+        self.tensors = (post_weight, pre_weight, pre_bias, gate, scale, shift, mod_index)
+        rows = mods[0].shape[0] if mods else 0
+        stride = (mods[0].stride(0) if rows > 1 else max(mods[0].stride(0), mods[0].shape[1])) if mods else 0
+        self.struct = _NormStruct(kind, eps, weight_offset, residual_scale, 1 if post_norm else 0, _ptr(post_weight), _ptr(pre_weight),
+                                  _ptr(pre_bias), _ptr(gate), _ptr(scale), _ptr(shift), stride, rows, mod_tokens, _ptr(mod_index))
+        self.ref = ctypes.addressof(self.struct)
+
+
+def qvla_block_norm(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: int, M: int, K: int, r_out, h, stream=None) -> None:
+    """Residual + gated branch, then the norm; y, r_out or h may be None as in include/qvla.h."""
+    status = _lib.qvla_block_norm(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, _ptr(y), y_stride, M, K, _ptr(r_out), _ptr(h),
+                                  _stream(stream))
+    if status:
+        _check(status)
+
+
+def qvla_block_norm_fp4(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: int, M: int, K: int, r_out, h, had_block: int,
+                        fmt: int, step_scale, hq, hs, hscale=None, stream=None) -> None:
+    """The same with its output rotated and quantised."""
+    status = _lib.qvla_block_norm_fp4(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, _ptr(y), y_stride, M, K, _ptr(r_out), _ptr(h),
+                                      had_block, fmt, _ptr(step_scale), hq.data_ptr(), hs.data_ptr(), _ptr(hscale),
+                                      _stream(stream))
     if status:
         _check(status)
 
