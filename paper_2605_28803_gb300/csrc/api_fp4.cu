@@ -18,7 +18,7 @@ using qvla::fail;
 struct qvla_fp4_layer {
   int N = 0, K = 0, had_block = 1;  // N = weight rows (2H when gated)
   int fmt = 0, xdt = 0, ydt = 0, gated = 0, device = 0;
-  uint8_t* wq = nullptr;    // device [N][K/2]; a gated layer's rows in turns of 32 gate rows and their 32 up rows
+  uint8_t* wq = nullptr;    // device [N][K/2]; a gated layer's rows in turns of 16 gate rows and their 16 up rows
   uint8_t* ws = nullptr;    // device, scale tiles of the rows in that order, rows up to a multiple of 256
   float* wscale = nullptr;  // device [N] (ones for MX)
   float* bias = nullptr;    // device [N] (zeros without one)
@@ -136,7 +136,7 @@ qvla_status multiply(const qvla_fp4_layer* L, const uint8_t* xq, const uint8_t* 
 int device_row(int n, int N, int gated) {
   if (!gated) return n;
   const int h = N / 2, unit = n % h;
-  return unit / 32 * 64 + (n >= h ? 32 : 0) + unit % 32;
+  return unit / 16 * 32 + (n >= h ? 16 : 0) + unit % 16;
 }
 
 qvla_status create(int N, int K, int had_block, qvla_fp4_format fmt, qvla_dtype xdt, qvla_dtype ydt, const uint8_t* wq, const uint8_t* ws,

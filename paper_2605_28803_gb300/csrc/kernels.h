@@ -260,7 +260,7 @@ struct Fp4GemmArgs {
   const float* xrow;       // [M], or null (MX)
   const uint8_t *wq, *ws;  // the layer's: [N][K/2] codes, scale tiles of N rows rounded up to 256
   const float *wrow, *bias;  // [N]
-  int fmt, ydt, gated;     // gated: rows in turns of 32 gate rows and the 32 up rows that go with them
+  int fmt, ydt, gated;     // gated: rows in turns of 16 gate rows and the 16 up rows that go with them
   int M, N, K;             // N = weight rows
   void* y;                 // [M][N] (gated: N / 2)
   int num_sms;
