@@ -6,17 +6,20 @@
 //   rotation z = h BlockDiag(H_b / sqrt b): float32 butterflies, the longest distance first, one product with 1/sqrt(b)
 //   codes    MX and NV as in fp4.cuh
 //
-// A row takes whole warps, 32 channels a thread, in registers from the loads to the stores.  The norm and the rotation's first
-// stages do not care which channels a thread holds, so the loads already bring them as those stages want them:
-//   kPieces   norm only: pieces of 8 channels, neighbouring threads neighbouring pieces
+// The norm wants many loads in flight and few registers: 8 channels a thread (16 beyond 8192), every operand of a row asked
+// for before the first sum over it.  The rotation and the quantiser want many channels a thread: 32, the loads taking
+// them as the rotation's first stages want them,
 //   kPlain    b <= 32: 32 consecutive channels
 //   kFour     b = 64, 128: of the 4 lines (32 channels each) of 128 channels, thread p of 4 holds quads 2p, 2p + 1 of each
-//   kEight    b = 256 .. 2048: thread q of 8 holds quad q of 8 lines, which differ in the high bits of the block's index
-//   kSixteen  b = 4096: half a quad of 16 lines
+//   256 ..    b = 256 to 2048: thread q of 8 holds quad q of 8 lines, which differ in the high bits of the block's index
+//   4096      half a quad of 16 lines
 // and one or two exchanges through shared memory (128 bytes a thread) end with 32 consecutive channels a thread, which is what
 // the quantiser wants: one MX block or two NV blocks, 16 bytes of codes.  Running the stages from the longest distance
-// down is what makes that the end and not the beginning.
+// down is what makes that the end and not the beginning.  Where both run, a group of threads norms 4 rows (2 beyond 8192
+// channels) into shared memory, and then each quarter of it rotates and quantises one.
 #pragma once
+
+#include <algorithm>
 
 #include "fp4.cuh"
 #include "griddep.cuh"
@@ -27,11 +30,12 @@
 namespace qvla {
 namespace fp4 {
 
-enum Layout { kPieces, kPlain, kFour, kEight, kSixteen };
+// Layouts of the rotation by log2 of the block: 8 .. 12 stand for themselves.
+constexpr int kPlain = 5, kFour = 7;
 
-constexpr int kRowThreads = 512;  // most threads of a CTA (K = 16384: one row)
-constexpr int kMaxWarps = kRowThreads / 32;
-constexpr int kSlots = 5;  // reductions over a row: two norms of two sums each, and the maximum
+constexpr int kRowThreads = 512;   // most threads of a quantised row's CTA (K = 16384)
+constexpr int kNormThreads = 1024;
+constexpr int kMaxWarps = 32;
 
 // N consecutive channels as float2 pairs.
 template <int N>
@@ -78,6 +82,7 @@ __device__ __forceinline__ uint32_t narrow(float2 f, __nv_bfloat16) {
 }
 template <int N>
 __device__ __forceinline__ void store_unit(float* p, float2* v) {
+  if (p == nullptr) return;
   if constexpr (N >= 4) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i)
@@ -107,7 +112,7 @@ __device__ __forceinline__ void store_unit(T* p, float2* v) {
 
 // A row's place among the CTA's warps, and sums and maxima over it.  Every thread of the CTA makes the same calls.
 struct RowGroup {
-  float* slots;  // [kSlots][kMaxWarps]
+  float* slots;      // [slot][kMaxWarps]
   int warps, first;  // of the row
   __device__ __forceinline__ float sum(float v, int slot) const {
 #pragma unroll
@@ -116,8 +121,11 @@ struct RowGroup {
     float* const s = slots + slot * kMaxWarps;
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = s[first];
-    for (int i = 1; i < warps; ++i) v += s[first + i];  // one order for every thread
+    // every warp adds the warps' sums in the same order
+    const int lane = threadIdx.x & 31;
+    v = lane < warps ? s[first + lane] : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
   // The largest; NaN if one is (bit patterns of non-negative floats order like the numbers, NaN above infinity).
@@ -127,32 +135,207 @@ struct RowGroup {
     float* const s = slots + slot * kMaxWarps;
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = __uint_as_float(w);
     __syncthreads();
-    for (int i = 0; i < warps; ++i) w = ::max(w, __float_as_uint(s[first + i]));
-    return __uint_as_float(w);
+    const int lane = threadIdx.x & 31;
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, lane < warps ? __float_as_uint(s[first + lane]) : 0u));
+  }
+};
+
+// ---- the norms ----------------------------------------------------------------------------------------------------------
+
+// N 16-byte pieces of a row of T (float32: 2 N of them), 8 channels each, as they lie in memory.
+template <typename T, int N>
+struct Raw {
+  static constexpr int kPer = sizeof(T) == 4 ? 2 : 1;
+  uint4 q[N * kPer];
+  __device__ __forceinline__ void load(int i, const T* p) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) q[i * kPer + k] = reinterpret_cast<const uint4*>(p)[k];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int k = 0; k < N * kPer; ++k) q[k] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ float2 pair(int i) const {  // channels 2 i and 2 i + 1
+    if constexpr (kPer == 2) {
+      const uint4 w = q[i >> 1];
+      return (i & 1) ? make_float2(__uint_as_float(w.z), __uint_as_float(w.w)) : make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+    } else {
+      const uint4 w = q[i >> 2];
+      return widen((i & 3) == 0 ? w.x : (i & 3) == 1 ? w.y : (i & 3) == 2 ? w.z : w.w, T());
+    }
   }
 };
 
 // v to (v - mean) / sqrt(var + eps), or v / sqrt(mean v^2 + eps); the variance from the deviations, in a second pass over the
 // registers.  Channels that are not there hold 0 and are left 0.
-template <typename Valid>
-__device__ __forceinline__ void normalize(float2 (&v)[16], const RowGroup& row, int slot, bool layer, float inv_k, float eps, Valid valid) {
+template <int N, typename Valid>
+__device__ __forceinline__ void normalize(float2 (&v)[4 * N], const RowGroup& row, int slot, bool layer, float k, float eps, Valid valid) {
   if (layer) {
     float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += v[i].x + v[i].y;
-    const float mean = row.sum(s, slot) * inv_k;
+    for (int i = 0; i < 4 * N; ++i) s += v[i].x + v[i].y;
+    const float mean = __fdiv_rn(row.sum(s, slot), k);  // (a quotient: of equal channels it is their value)
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (valid(i)) v[i] = make_float2(v[i].x - mean, v[i].y - mean);
+    for (int i = 0; i < 4 * N; ++i)
+      if (valid(i >> 2)) v[i] = make_float2(v[i].x - mean, v[i].y - mean);
   }
   float s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s = fmaf(v[i].x, v[i].x, fmaf(v[i].y, v[i].y, s));
-  const float var = row.sum(s, slot + 1) * inv_k + eps;
-  const float scale = 1.0f / sqrtf(var);
+  for (int i = 0; i < 4 * N; ++i) s = fmaf(v[i].x, v[i].x, fmaf(v[i].y, v[i].y, s));
+  const float scale = 1.0f / sqrtf(__fdiv_rn(row.sum(s, slot + 1), k) + eps);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = make_float2(v[i].x * scale, v[i].y * scale);
+  for (int i = 0; i < 4 * N; ++i) v[i] = make_float2(v[i].x * scale, v[i].y * scale);
 }
+
+// A group of threads takes rows m, m + step, ... (`rows` of them, those below M): thread j its pieces j, j + threads, ...  h goes
+// to global memory where it is wanted, and with `store` (row number, channel, 8 values as T) to the caller.
+template <typename R, typename T, int N, typename Store>
+__device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row, int j, int m, int step, int rows, Store store) {
+  const int threads = row.warps * 32;
+  const float width = static_cast<float>(a.K), off = a.norm.weight_offset, alpha = a.norm.residual_scale;
+  const bool layer = a.norm.layer != 0, norm_h = a.h != nullptr || a.codes != nullptr;
+  const T* const gate = static_cast<const T*>(a.norm.gate);
+  const T* const scale = static_cast<const T*>(a.norm.scale);
+  const T* const shift = static_cast<const T*>(a.norm.shift);
+  auto channel = [&](int i) { return (j + i * threads) * 8; };
+  auto there = [&](int i) { return channel(i) < a.K; };
+  constexpr bool kHold = N == 1;  // weights and conditioning stay in registers from the row's start (with two pieces: loaded at their use)
+  auto take = [&](Raw<T, N>& to, const void* from) {
+    to.zero();
+    if (from == nullptr) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (there(i)) to.load(i, static_cast<const T*>(from) + channel(i));
+  };
+  Raw<T, N> post_w, pre_w, pre_b;  // the same for every row
+  if constexpr (kHold) {
+    take(post_w, a.norm.post_weight);
+    take(pre_w, a.norm.pre_weight);
+    take(pre_b, a.norm.pre_bias);
+  }
+  griddep_wait();  // rows (and the conditioning) come from earlier kernels, which may still read what this one writes
+  griddep_launch_dependents();
+
+  Raw<R, N> r;
+  Raw<T, N> y;
+  auto fetch = [&](int at) {
+    r.zero();
+    y.zero();
+    if (at >= a.M) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (!there(i)) continue;
+      r.load(i, static_cast<const R*>(a.x) + static_cast<size_t>(at) * a.x_stride + channel(i));
+      if (a.y != nullptr) y.load(i, static_cast<const T*>(a.y) + static_cast<size_t>(at) * a.y_stride + channel(i));
+    }
+  };
+  fetch(m);
+  for (int k = 0; k < rows; ++k, m += step) {
+    const int slot = (k & 1) * 4;
+    // the token's row of the conditioning; a token whose index is out of range is skipped: nothing of it is written
+    bool live = m < a.M;
+    size_t mod = 0;
+    if (gate != nullptr || scale != nullptr || shift != nullptr) {
+      const int c = !live ? 0 : a.norm.mod_index != nullptr ? a.norm.mod_index[m] : m / a.norm.mod_tokens;
+      if (c < 0 || c >= a.norm.mod_rows) {
+        if (live && j == 0) atomicOr(&g_error_word, kErrIndex);
+        live = false;
+      } else {
+        mod = static_cast<size_t>(c) * a.norm.mod_stride;
+      }
+    }
+    auto row_of = [&](const T* t) { return t != nullptr && live ? t + mod : static_cast<const T*>(nullptr); };
+    Raw<T, N> g, sc, sh;
+    if constexpr (kHold) {
+      take(g, a.y != nullptr ? row_of(gate) : nullptr);
+      take(sc, row_of(scale));
+      take(sh, row_of(shift));
+    }
+    float2 v[4 * N];
+    if (a.y != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) v[i] = y.pair(i);
+      if (a.norm.post_norm) {
+        normalize<N>(v, row, slot, layer, width, a.norm.eps, there);
+        if (a.norm.post_weight != nullptr) {
+          if constexpr (!kHold) take(post_w, a.norm.post_weight);
+#pragma unroll
+          for (int i = 0; i < 4 * N; ++i) {
+            const float2 w = post_w.pair(i);
+            v[i] = make_float2(v[i].x * (w.x + off), v[i].y * (w.y + off));
+          }
+        }
+      }
+      if (gate != nullptr) {
+        if constexpr (!kHold) take(g, row_of(gate));
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) {
+          const float2 w = g.pair(i);
+          v[i] = make_float2(v[i].x * w.x, v[i].y * w.y);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float2 w = r.pair(i);
+        v[i] = make_float2(fmaf(alpha, w.x, v[i].x), fmaf(alpha, w.y, v[i].y));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float2 w = r.pair(i);
+        v[i] = make_float2(alpha * w.x, alpha * w.y);
+      }
+    }
+    R* const out = a.residual_out != nullptr && live ? static_cast<R*>(a.residual_out) + static_cast<size_t>(m) * a.x_stride : nullptr;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (there(i)) store_unit<8>(out == nullptr ? static_cast<R*>(nullptr) : out + channel(i), v + 4 * i);
+    if (k + 1 < rows) fetch(m + step);  // (after this row's stores: a caller may update the residual in place)
+    if (!norm_h) continue;
+    normalize<N>(v, row, slot + 2, layer, width, a.norm.eps, there);
+    T* const h = a.h != nullptr && live ? static_cast<T*>(a.h) + static_cast<size_t>(m) * a.K : nullptr;
+    if (a.norm.pre_weight != nullptr) {
+      if constexpr (!kHold) take(pre_w, a.norm.pre_weight);
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float2 w = pre_w.pair(i);
+        v[i] = make_float2(v[i].x * (w.x + off), v[i].y * (w.y + off));
+      }
+    }
+    if (a.norm.pre_bias != nullptr) {
+      if constexpr (!kHold) take(pre_b, a.norm.pre_bias);
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float2 w = pre_b.pair(i);
+        v[i] = make_float2(v[i].x + w.x, v[i].y + w.y);
+      }
+    }
+    if (scale != nullptr) {
+      if constexpr (!kHold) take(sc, row_of(scale));
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float2 w = sc.pair(i);
+        v[i] = make_float2(v[i].x * (1.0f + w.x), v[i].y * (1.0f + w.y));
+      }
+    }
+    if (shift != nullptr) {
+      if constexpr (!kHold) take(sh, row_of(shift));
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) {
+        const float2 w = sh.pair(i);
+        v[i] = make_float2(v[i].x + w.x, v[i].y + w.y);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (!there(i)) continue;
+      store_unit<8>(h == nullptr ? static_cast<T*>(nullptr) : h + channel(i), v + 4 * i);
+      store(k, channel(i), v + 4 * i, live);
+    }
+  }
+}
+
+// ---- rotation and quantiser -----------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void butterflies(float2 (&v)[16], int distance) {  // between registers `distance` apart
 #pragma unroll
@@ -170,161 +353,35 @@ __device__ __forceinline__ void sts_half(uint32_t a, float2 v) {
   asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v.x), "f"(v.y) : "memory");
 }
 
-// R: the residual's type (Norm only); T: the rows', or the branch's and the outputs'.  kQuant: codes leave (else h only).
-template <typename R, typename T, bool kNorm, bool kQuant, int kLayout, int kFmt>
-__global__ void __launch_bounds__(kRowThreads, kNorm ? 1 : 2) rows_kernel(const RowsArgs a) {
-  constexpr int kUnit = kLayout == kSixteen ? 2 : kLayout == kEight ? 4 : 8;  // channels a load moves
-  constexpr int kUnits = 32 / kUnit, kPer = kUnit / 2;
-  extern __shared__ __align__(128) uint8_t row_smem[];  // a line of 128 bytes per thread
-  __shared__ float s_red[kSlots * kMaxWarps];
-
-  const int tpr = a.row_warps * 32;
-  const int rloc = static_cast<int>(threadIdx.x) / tpr, j = static_cast<int>(threadIdx.x) - rloc * tpr;
-  const RowGroup row = {s_red, a.row_warps, rloc * a.row_warps};
-  const int m = blockIdx.x * a.rows_per_cta + rloc;
-  const bool here = m < a.M;
-  const bool active = here && (kLayout == kPieces || j * 32 < a.K);
-
-  // channel of unit u: first of kUnit consecutive ones
-  const int log_c = a.log_b - 8;                        // kEight: index bits above a 256-channel group
-  const int keep = kLayout == kEight ? 3 - log_c : 0;   // line bits that a thread keeps
-  int base = 0;
-  if constexpr (kLayout == kPlain) base = j * 32;
-  if constexpr (kLayout == kFour) base = (j & ~3) * 32 + (j & 3) * 8;
-  if constexpr (kLayout == kEight) {
-    const int group = 8 << log_c;
-    base = (j & ~(group - 1)) * 32 + (((j >> 3) & ((1 << log_c) - 1)) << (keep + 5)) + (j & 7) * 4;
+// Where the thread's channels of a row lie ahead of the rotation.
+template <int kLayout>
+struct Place {
+  static constexpr int kUnit = kLayout == 12 ? 2 : kLayout > kFour ? 4 : 8;  // channels a load moves
+  static constexpr int kUnits = 32 / kUnit, kPer = kUnit / 2;
+  static constexpr int kLogC = kLayout - 8, kKeep = kLayout > kFour && kLayout < 12 ? 3 - kLogC : 0;  // 256 ..: index bits above a 256-channel group, line bits that a thread keeps
+  int base;
+  __device__ __forceinline__ explicit Place(int j) {
+    if constexpr (kLayout == kPlain) base = j * 32;
+    if constexpr (kLayout == kFour) base = (j & ~3) * 32 + (j & 3) * 8;
+    if constexpr (kLayout > kFour && kLayout < 12) {
+      constexpr int kGroup = 8 << kLogC;
+      base = (j & ~(kGroup - 1)) * 32 + (((j >> 3) & ((1 << kLogC) - 1)) << (kKeep + 5)) + (j & 7) * 4;
+    }
+    if constexpr (kLayout == 12) base = (j & ~127) * 32 + ((j >> 4) & 7) * 32 + (j & 15) * 2;
   }
-  if constexpr (kLayout == kSixteen) base = (j & ~127) * 32 + ((j >> 4) & 7) * 32 + (j & 15) * 2;
-  auto channel = [&](int u) {
-    if constexpr (kLayout == kPieces) return (j + u * tpr) * 8;
+  __device__ __forceinline__ int channel(int u) const {  // of unit u
     if constexpr (kLayout == kPlain) return base + u * 8;
     if constexpr (kLayout == kFour) return base + u * 32;
-    if constexpr (kLayout == kEight) return base + (u >> keep) * 256 + (u & ((1 << keep) - 1)) * 32;
-    return base + u * 256;
-  };
-  auto valid = [&](int u) { return kLayout == kPieces ? here && channel(u) < a.K : active; };
-
-  bool write = active;  // of codes: 32 channels of a row that is there
-
-  griddep_wait();  // rows come from the previous kernel, which may still read what this one writes
-  griddep_launch_dependents();
-
-  float2 v[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = make_float2(0.0f, 0.0f);
-  if constexpr (!kNorm) {
-    const T* const src = static_cast<const T*>(a.x) + static_cast<size_t>(m) * a.x_stride;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-      if (valid(u)) load_unit<kUnit>(src + channel(u), v + u * kPer);
-  } else {
-    const float inv_k = 1.0f / static_cast<float>(a.K);
-    const bool layer = a.norm.layer != 0;
-    auto there = [&](int i) { return valid(i / kPer); };
-    const R* const r = static_cast<const R*>(a.x) + static_cast<size_t>(m) * a.x_stride;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-      if (valid(u)) load_unit<kUnit>(r + channel(u), v + u * kPer);
-    // the token's row of the conditioning
-    size_t mod = 0;
-    bool mod_ok = here;
-    if (a.norm.gate != nullptr || a.norm.scale != nullptr || a.norm.shift != nullptr) {
-      int c = 0;
-      if (here) c = a.norm.mod_index != nullptr ? a.norm.mod_index[m] : m / a.norm.mod_tokens;
-      if (c < 0 || c >= a.norm.mod_rows) {
-        mod_ok = false;
-        if (here && j == 0) atomicOr(&g_error_word, kErrIndex);
-      } else {
-        mod = static_cast<size_t>(c) * a.norm.mod_stride;
-      }
-    }
-    const bool live = mod_ok;  // a token whose index is out of range is skipped: nothing of it is written
-    const T* const gate = static_cast<const T*>(a.norm.gate);
-    const T* const scale = static_cast<const T*>(a.norm.scale);
-    const T* const shift = static_cast<const T*>(a.norm.shift);
-    const float off = a.norm.weight_offset;
-    if (a.y != nullptr) {
-      float2 w[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = make_float2(0.0f, 0.0f);
-      const T* const y = static_cast<const T*>(a.y) + static_cast<size_t>(m) * a.y_stride;
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u)
-        if (valid(u)) load_unit<kUnit>(y + channel(u), w + u * kPer);
-      if (a.norm.post_norm) normalize(w, row, 0, layer, inv_k, a.norm.eps, there);
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        if (!valid(u) || !live) continue;
-        float2 t[kPer];
-        if (a.norm.post_weight != nullptr) {
-          load_unit<kUnit>(static_cast<const T*>(a.norm.post_weight) + channel(u), t);
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) w[u * kPer + i] = make_float2(w[u * kPer + i].x * (t[i].x + off), w[u * kPer + i].y * (t[i].y + off));
-        }
-        if (gate != nullptr) {
-          load_unit<kUnit>(gate + mod + channel(u), t);
-#pragma unroll
-          for (int i = 0; i < kPer; ++i) w[u * kPer + i] = make_float2(w[u * kPer + i].x * t[i].x, w[u * kPer + i].y * t[i].y);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        v[i] = make_float2(fmaf(a.norm.residual_scale, v[i].x, w[i].x), fmaf(a.norm.residual_scale, v[i].y, w[i].y));
-    } else if (a.norm.residual_scale != 1.0f) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = make_float2(a.norm.residual_scale * v[i].x, a.norm.residual_scale * v[i].y);
-    }
-    R* const out = static_cast<R*>(a.residual_out) + static_cast<size_t>(m) * a.x_stride;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      if (!valid(u)) continue;
-      if constexpr (sizeof(R) == 4) {
-        if (a.residual_out != nullptr && live) store_unit<kUnit>(out + channel(u), v + u * kPer);
-      } else {
-        store_unit<kUnit>(a.residual_out != nullptr && live ? out + channel(u) : static_cast<R*>(nullptr), v + u * kPer);
-      }
-    }
-    if (!kQuant && a.h == nullptr) return;  // the residual alone (the same for every thread)
-    normalize(v, row, 2, layer, inv_k, a.norm.eps, there);
-    T* const h = static_cast<T*>(a.h) + static_cast<size_t>(m) * a.K;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      if (!valid(u) || !live) continue;
-      float2 t[kPer];
-      float2* const p = v + u * kPer;
-      if (a.norm.pre_weight != nullptr) {
-        load_unit<kUnit>(static_cast<const T*>(a.norm.pre_weight) + channel(u), t);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) p[i] = make_float2(p[i].x * (t[i].x + off), p[i].y * (t[i].y + off));
-      }
-      if (a.norm.pre_bias != nullptr) {
-        load_unit<kUnit>(static_cast<const T*>(a.norm.pre_bias) + channel(u), t);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) p[i] = make_float2(p[i].x + t[i].x, p[i].y + t[i].y);
-      }
-      if (scale != nullptr) {
-        load_unit<kUnit>(scale + mod + channel(u), t);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) p[i] = make_float2(p[i].x * (1.0f + t[i].x), p[i].y * (1.0f + t[i].y));
-      }
-      if (shift != nullptr) {
-        load_unit<kUnit>(shift + mod + channel(u), t);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) p[i] = make_float2(p[i].x + t[i].x, p[i].y + t[i].y);
-      }
-      store_unit<kUnit>(a.h != nullptr ? h + channel(u) : static_cast<T*>(nullptr), p);  // the quantiser reads what is stored
-    }
-    if (!live) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = make_float2(0.0f, 0.0f);
-      write = false;
-    }
+    if constexpr (kLayout == 12) return base + u * 256;
+    return base + (u >> kKeep) * 256 + (u & ((1 << kKeep) - 1)) * 32;
   }
-  if constexpr (!kQuant) return;
+};
 
-  // ---- rotation, to 32 consecutive channels a thread ----
-  const uint32_t lines = smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128);  // of this row
+// Thread j of a row holds v as Place<kLayout> says; `lines` is the row's shared memory.  Leaves codes, block scales and the row's.
+// write: the row and the thread's channels are there.  Every thread of the CTA calls this.
+template <int kLayout, int kFmt>
+__device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGroup& row, int slot, int j, int m, bool write, uint32_t lines,
+                                                float2 (&v)[16]) {
   if constexpr (kLayout == kFour) {
     if (a.log_b == 7) butterflies(v, 8);
     butterflies(v, 4);
@@ -343,9 +400,9 @@ __global__ void __launch_bounds__(kRowThreads, kNorm ? 1 : 2) rows_kernel(const 
 #pragma unroll
     for (int i = 0; i < 8; ++i) lds_quad(own + ((i ^ f) << 4), v + 2 * i);
   }
-  if constexpr (kLayout == kEight || kLayout == kSixteen) {
+  if constexpr (kLayout > kFour) {
     const int q = j & 7;
-    if (kLayout == kSixteen) {
+    if constexpr (kLayout == 12) {
 #pragma unroll
       for (int s = 3; s >= 0; --s) butterflies(v, 1 << s);
       const int l = (j >> 4) & 7, qq = (j >> 1) & 7;
@@ -353,26 +410,29 @@ __global__ void __launch_bounds__(kRowThreads, kNorm ? 1 : 2) rows_kernel(const 
 #pragma unroll
       for (int h = 0; h < 16; ++h) sts_half(at + h * 1024, v[h]);
       __syncthreads();
-    } else if (log_c > 0) {
+    } else if constexpr (kLayout > 8) {
+      using P = Place<kLayout>;
+      constexpr int log_c = P::kLogC, keep = P::kKeep;
       // stages over the group index, whose bits lie above the kept line bits of the unit
       butterflies(v, 8);
-      if (log_c > 1) butterflies(v, 4);
-      if (log_c > 2) butterflies(v, 2);
-      const int group = 8 << log_c, la = ((j >> 3) & ((1 << log_c) - 1)) << keep;
+      if constexpr (log_c > 1) butterflies(v, 4);
+      if constexpr (log_c > 2) butterflies(v, 2);
+      constexpr int group = 8 << log_c;
+      const int la = ((j >> 3) & ((1 << log_c) - 1)) << keep;
       const uint32_t block = lines + static_cast<uint32_t>((j & ~(group - 1)) * 128);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int l = la | (u & ((1 << keep) - 1));
         sts_quad(block + static_cast<uint32_t>(((u >> keep) * 8 + l) * 128 + ((q ^ l) << 4)), v + 2 * u);
       }
-      if (log_c > 2) {  // a block of 2048 is two warps
+      if constexpr (log_c > 2) {  // a block of 2048 is two warps
         __syncthreads();
       } else {
         __syncwarp();
       }
     }
     const uint32_t grp = lines + static_cast<uint32_t>((j & ~7) * 128);
-    if (kLayout == kSixteen || log_c > 0) {
+    if constexpr (kLayout > 8) {
 #pragma unroll
       for (int l = 0; l < 8; ++l) lds_quad(grp + static_cast<uint32_t>(l * 128 + ((q ^ l) << 4)), v + 2 * l);
     }
@@ -438,7 +498,7 @@ __global__ void __launch_bounds__(kRowThreads, kNorm ? 1 : 2) rows_kernel(const 
     if (a.step_scale != nullptr) {
       delta = __ldg(a.step_scale);
     } else {
-      delta = __fdiv_rn(row.max(rq::max_nan(top[0], top[1]), 4), kRowMax);
+      delta = __fdiv_rn(row.max(rq::max_nan(top[0], top[1]), slot), kRowMax);
       if (isinf(delta)) delta = __int_as_float(0x7FC00000);
     }
     if (write && j == 0) a.row_scale[m] = delta;
@@ -461,12 +521,9 @@ __global__ void __launch_bounds__(kRowThreads, kNorm ? 1 : 2) rows_kernel(const 
           l[i] = make_float2(v[4 * c + i].x * dn, v[4 * c + i].y * dn);
         }
         uint32_t w = e2m1x8(h[0], h[1], h[2], h[3]);
-        if (w != e2m1x8(l[0], l[1], l[2], l[3]) || (!easy && d > 0.0f)) {
-          w = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w |= (code_exact(v[4 * c + i].x, d) << (8 * i)) | (code_exact(v[4 * c + i].y, d) << (8 * i + 4));
-        }
+        const uint32_t low = e2m1x8(l[0], l[1], l[2], l[3]);
+        if (w != low) w = decide_codes(low, w, v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3], d);
+        if (!easy && d > 0.0f) w = codes_exact(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3], d);
         code[c] = w;
       }
     }
@@ -477,31 +534,95 @@ __global__ void __launch_bounds__(kRowThreads, kNorm ? 1 : 2) rows_kernel(const 
   if (write) *reinterpret_cast<uint4*>(a.codes + static_cast<size_t>(m) * (a.K >> 1) + j * 16) = make_uint4(code[0], code[1], code[2], code[3]);
 }
 
-template <typename R, typename T, bool kNorm, bool kQuant, int kLayout, int kFmt>
-cudaError_t launch_rows(RowsArgs a) {
-  const int threads = kLayout == kPieces ? (a.K + 31) / 32 : a.K / 32;
-  a.row_warps = (threads + 31) / 32;
-  int rows = a.row_warps >= 8 ? 1 : 8 / a.row_warps;
-  while (rows > 1 && (a.M + rows - 1) / rows < a.num_sms) rows /= 2;  // few rows: more CTAs
-  a.rows_per_cta = rows;
-  const int tpb = rows * a.row_warps * 32;
-  auto kern = rows_kernel<R, T, kNorm, kQuant, kLayout, kFmt>;
-  const size_t smem = kQuant && kLayout != kPlain && kLayout != kPieces ? static_cast<size_t>(tpb) * 128 : 0;
-  if (smem > 40 * 1024) {
-    static std::atomic<unsigned long long> raised{0};  // devices whose limit has been raised to the most any K asks for
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    const unsigned long long bit = 1ull << (dev & 63);
-    if (!(raised.load() & bit)) {
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowThreads * 128);
-      if (e != cudaSuccess) return e;
-      raised.fetch_or(bit);
-    }
+
+template <typename T, int kLayout, int kFmt>
+__global__ void __launch_bounds__(kRowThreads, 2) quantize_rows_kernel(const RowsArgs a) {
+  using P = Place<kLayout>;
+  extern __shared__ __align__(128) uint8_t row_smem[];
+  __shared__ float s_red[kMaxWarps];
+  const int tpr = a.row_warps * 32;
+  const int rloc = static_cast<int>(threadIdx.x) / tpr, j = static_cast<int>(threadIdx.x) - rloc * tpr;
+  const RowGroup row = {s_red, a.row_warps, rloc * a.row_warps};
+  const int m = blockIdx.x * a.group_rows + rloc;
+  const bool active = m < a.M && j * 32 < a.K;
+  const P place(j);
+  griddep_wait();  // rows come from the previous kernel, which may still read what this one writes
+  griddep_launch_dependents();
+  float2 v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = make_float2(0.0f, 0.0f);
+  if (active) {
+    const T* const src = static_cast<const T*>(a.x) + static_cast<size_t>(m) * a.x_stride;
+#pragma unroll
+    for (int u = 0; u < P::kUnits; ++u) load_unit<P::kUnit>(src + place.channel(u), v + u * P::kPer);
   }
+  rotate_quantize<kLayout, kFmt>(a, row, 0, j, m, active, smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128), v);
+}
+
+// Norm, rotation and quantiser.  A group of a.row_warps warps norms a.group_rows rows into shared memory (as T), one after the
+// other; then the CTA's warps are dealt to the rows anew, K / 32 threads each.
+template <typename R, typename T, int N, int kLayout, int kFmt>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const RowsArgs a) {
+  using P = Place<kLayout>;
+  extern __shared__ __align__(128) uint8_t row_smem[];  // the rows as T; then a line of 128 bytes per thread
+  __shared__ float s_red[8 * kMaxWarps];
+  const int tpg = a.row_warps * 32;
+  const int g = static_cast<int>(threadIdx.x) / tpg, j1 = static_cast<int>(threadIdx.x) - g * tpg;
+  const int groups = static_cast<int>(blockDim.x) / tpg, m0 = blockIdx.x * groups * a.group_rows;
+  T* const hs = reinterpret_cast<T*>(row_smem);
+  __shared__ unsigned int s_live;  // rows that are there and whose conditioning is
+  if (threadIdx.x == 0) s_live = 0u;
+  __syncthreads();
+  {
+    const RowGroup group = {s_red, a.row_warps, g * a.row_warps};
+    // (rows of a group lie next to one another)
+    norm_rows<R, T, N>(a, group, j1, m0 + g * a.group_rows, 1, a.group_rows, [&](int k, int channel, const float2* p, bool live) {
+      const int r = g * a.group_rows + k;
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = narrow(p[i], T());
+      *reinterpret_cast<uint4*>(hs + static_cast<size_t>(r) * a.K + channel) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (channel == 0 && live) atomicOr(&s_live, 1u << r);
+    });
+  }
+  __syncthreads();
+  // the second dealing: quant_warps warps a row
+  const int quant_warps = (a.K + 1023) / 1024, tpr = quant_warps * 32;
+  const int rloc = static_cast<int>(threadIdx.x) / tpr, j = static_cast<int>(threadIdx.x) - rloc * tpr;
+  const RowGroup row = {s_red, quant_warps, rloc * quant_warps};
+  const bool active = rloc < groups * a.group_rows && ((s_live >> (rloc & 31)) & 1u) && j * 32 < a.K;
+  const P place(j);
+  float2 v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = make_float2(0.0f, 0.0f);
+  if (active) {
+    const T* const src = hs + static_cast<size_t>(rloc) * a.K;
+#pragma unroll
+    for (int u = 0; u < P::kUnits; ++u) load_unit<P::kUnit>(src + place.channel(u), v + u * P::kPer);
+  }
+  __syncthreads();  // the rows have been read: their place now takes the rotation's lines
+  rotate_quantize<kLayout, kFmt>(a, row, 0, j, m0 + rloc, active, smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128), v);
+}
+
+// Norm alone: the CTAs that run at once go through the rows.
+template <typename R, typename T, int N>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const RowsArgs a) {
+  __shared__ float s_red[8 * kMaxWarps];
+  const int tpg = a.row_warps * 32;
+  const int g = static_cast<int>(threadIdx.x) / tpg, j = static_cast<int>(threadIdx.x) - g * tpg;
+  const int groups = static_cast<int>(blockDim.x) / tpg, step = static_cast<int>(gridDim.x) * groups;
+  const RowGroup group = {s_red, a.row_warps, g * a.row_warps};
+  const int first = blockIdx.x * groups;  // every group of the CTA makes as many turns
+  norm_rows<R, T, N>(a, group, j, first + g, step, first < a.M ? (a.M - first + step - 1) / step : 0, [](int, int, const float2*, bool) {});
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------------------
+
+template <typename K>
+cudaError_t start(K kern, const RowsArgs& a, int grid, int threads, size_t smem) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((a.M + rows - 1) / rows));
-  cfg.blockDim = dim3(static_cast<unsigned>(tpb));
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = a.stream;
   cudaLaunchAttribute attr[1];
@@ -513,17 +634,102 @@ cudaError_t launch_rows(RowsArgs a) {
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <typename R, typename T, bool kNorm, int kFmt>
-cudaError_t launch_quant_layout(const RowsArgs& a) {
-  if (a.log_b <= 5) return launch_rows<R, T, kNorm, true, kPlain, kFmt>(a);
-  if (a.log_b <= 7) return launch_rows<R, T, kNorm, true, kFour, kFmt>(a);
-  if (a.log_b <= 11) return launch_rows<R, T, kNorm, true, kEight, kFmt>(a);
-  return launch_rows<R, T, kNorm, true, kSixteen, kFmt>(a);
+// Raises the kernel's limit of dynamic shared memory once per device; `done` holds the devices where it is.
+template <typename K>
+cudaError_t raise_limit(K kern, size_t smem, size_t most, std::atomic<unsigned long long>* done) {
+  if (smem <= 40 * 1024) return cudaSuccess;  // (48 KB without it, the kernel's own few words included)
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (done->load() & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
+  if (e == cudaSuccess) done->fetch_or(bit);
+  return e;
 }
 
-template <typename R, typename T, bool kNorm>
-cudaError_t launch_quant(const RowsArgs& a) {
-  return a.fmt == kMx ? launch_quant_layout<R, T, kNorm, kMx>(a) : launch_quant_layout<R, T, kNorm, kNv>(a);
+template <typename T, int kLayout, int kFmt>
+cudaError_t launch_quantize(RowsArgs a) {
+  a.row_warps = (a.K / 32 + 31) / 32;
+  int rows = a.row_warps >= 8 ? 1 : 8 / a.row_warps;
+  while (rows > 1 && (a.M + rows - 1) / rows < a.num_sms) rows /= 2;  // few rows: more CTAs
+  a.group_rows = rows;
+  const int threads = rows * a.row_warps * 32;
+  auto kern = quantize_rows_kernel<T, kLayout, kFmt>;
+  const size_t smem = kLayout != kPlain ? static_cast<size_t>(threads) * 128 : 0;
+  static std::atomic<unsigned long long> raised{0};
+  if (cudaError_t e = raise_limit(kern, smem, kRowThreads * 128, &raised)) return e;
+  return start(kern, a, (a.M + rows - 1) / rows, threads, smem);
+}
+
+template <typename R, typename T, int N, int kLayout, int kFmt>
+cudaError_t launch_norm_quantize(RowsArgs a) {
+  a.row_warps = (a.K + N * 256 - 1) / (N * 256);
+  const int quant_warps = (a.K + 1023) / 1024;
+  // Rows of a CTA: as many as its warps quantise at once; fewer where that would leave SMs without any.
+  int groups = a.row_warps >= 8 ? 1 : 8 / a.row_warps;
+  a.group_rows = a.row_warps / quant_warps;
+  while (groups > 1 && (a.M + groups * a.group_rows - 1) / (groups * a.group_rows) < a.num_sms) groups /= 2;
+  while (a.group_rows > 1 && (a.M + groups * a.group_rows - 1) / (groups * a.group_rows) < 2 * a.num_sms) a.group_rows /= 2;
+  const int threads = groups * a.row_warps * 32, rows = groups * a.group_rows;
+  auto kern = norm_quantize_kernel<R, T, N, kLayout, kFmt>;
+  const size_t lines = kLayout != kPlain ? static_cast<size_t>(threads) * 128 : 0, kept = static_cast<size_t>(rows) * a.K * sizeof(T);
+  const size_t smem = std::max(lines, kept);
+  static std::atomic<unsigned long long> raised{0};
+  if (cudaError_t e = raise_limit(kern, smem, kNormThreads * 128, &raised)) return e;
+  return start(kern, a, (a.M + rows - 1) / rows, threads, smem);
+}
+
+template <typename R, typename T, int N>
+cudaError_t launch_norm_only(RowsArgs a) {
+  a.row_warps = (a.K + N * 256 - 1) / (N * 256);
+  int groups = a.row_warps >= 8 ? 1 : 8 / a.row_warps;
+  while (groups > 1 && (a.M + groups - 1) / groups < a.num_sms) groups /= 2;
+  const int threads = groups * a.row_warps * 32, blocks = (a.M + groups - 1) / groups;
+  const int at_once = a.num_sms * (threads >= 1024 ? 1 : 1024 / threads);
+  return start(norm_kernel<R, T, N>, a, blocks < at_once ? blocks : at_once, threads, 0);
+}
+
+template <typename R, typename T, int N, int kFmt>
+cudaError_t launch_norm_layout(const RowsArgs& a) {
+  if (a.log_b <= 5) return launch_norm_quantize<R, T, N, kPlain, kFmt>(a);
+  if (a.log_b <= 7) return launch_norm_quantize<R, T, N, kFour, kFmt>(a);
+  switch (a.log_b) {
+    case 8: return launch_norm_quantize<R, T, N, 8, kFmt>(a);
+    case 9: return launch_norm_quantize<R, T, N, 9, kFmt>(a);
+    case 10: return launch_norm_quantize<R, T, N, 10, kFmt>(a);
+    case 11: return launch_norm_quantize<R, T, N, 11, kFmt>(a);
+    default: return launch_norm_quantize<R, T, N, 12, kFmt>(a);
+  }
+}
+
+// R: the residual's type, T: everything else's.
+template <typename R, typename T>
+cudaError_t launch_norm(const RowsArgs& a) {
+  if (a.K > 8192) {
+    if (a.codes == nullptr) return launch_norm_only<R, T, 2>(a);
+    return a.fmt == kMx ? launch_norm_layout<R, T, 2, kMx>(a) : launch_norm_layout<R, T, 2, kNv>(a);
+  }
+  if (a.codes == nullptr) return launch_norm_only<R, T, 1>(a);
+  return a.fmt == kMx ? launch_norm_layout<R, T, 1, kMx>(a) : launch_norm_layout<R, T, 1, kNv>(a);
+}
+
+template <typename T, int kFmt>
+cudaError_t launch_quantize_layout(const RowsArgs& a) {
+  if (a.log_b <= 5) return launch_quantize<T, kPlain, kFmt>(a);
+  if (a.log_b <= 7) return launch_quantize<T, kFour, kFmt>(a);
+  switch (a.log_b) {
+    case 8: return launch_quantize<T, 8, kFmt>(a);
+    case 9: return launch_quantize<T, 9, kFmt>(a);
+    case 10: return launch_quantize<T, 10, kFmt>(a);
+    case 11: return launch_quantize<T, 11, kFmt>(a);
+    default: return launch_quantize<T, 12, kFmt>(a);
+  }
+}
+
+template <typename T>
+cudaError_t launch_quantize_fmt(const RowsArgs& a) {
+  return a.fmt == kMx ? launch_quantize_layout<T, kMx>(a) : launch_quantize_layout<T, kNv>(a);
 }
 
 }  // namespace fp4

@@ -3,6 +3,6 @@
 
 namespace qvla {
 
-cudaError_t launch_fp4_quantize_bf16(const RowsArgs& a) { return fp4::launch_quant<__nv_bfloat16, __nv_bfloat16, false>(a); }
+cudaError_t launch_fp4_quantize_bf16(const RowsArgs& a) { return fp4::launch_quantize_fmt<__nv_bfloat16>(a); }
 
 }  // namespace qvla

@@ -3,6 +3,6 @@
 
 namespace qvla {
 
-cudaError_t launch_fp4_quantize_f16(const RowsArgs& a) { return fp4::launch_quant<__half, __half, false>(a); }
+cudaError_t launch_fp4_quantize_f16(const RowsArgs& a) { return fp4::launch_quantize_fmt<__half>(a); }
 
 }  // namespace qvla

@@ -3,6 +3,6 @@
 
 namespace qvla {
 
-cudaError_t launch_fp4_quantize_f32(const RowsArgs& a) { return fp4::launch_quant<float, float, false>(a); }
+cudaError_t launch_fp4_quantize_f32(const RowsArgs& a) { return fp4::launch_quantize_fmt<float>(a); }
 
 }  // namespace qvla

@@ -240,7 +240,7 @@ struct RowsArgs {
   const float* step_scale;
   uint8_t *codes, *scales;
   float* row_scale;
-  int row_warps, rows_per_cta;  // set by the launch
+  int row_warps, group_rows;  // set by the launch: warps that share a row, and rows of such a group
   int num_sms;
   cudaStream_t stream;
 };

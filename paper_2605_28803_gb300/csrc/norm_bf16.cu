@@ -5,8 +5,7 @@ namespace qvla {
 
 cudaError_t launch_norm_bf16(const RowsArgs& a) {
   using T = __nv_bfloat16;
-  if (a.codes != nullptr) return a.xdt == 2 ? fp4::launch_quant<float, T, true>(a) : fp4::launch_quant<T, T, true>(a);
-  return a.xdt == 2 ? fp4::launch_rows<float, T, true, false, fp4::kPieces, 0>(a) : fp4::launch_rows<T, T, true, false, fp4::kPieces, 0>(a);
+  return a.xdt == 2 ? fp4::launch_norm<float, T>(a) : fp4::launch_norm<T, T>(a);
 }
 
 cudaError_t read_and_clear_error_word_norm_bf16(unsigned int* out, cudaStream_t stream) {

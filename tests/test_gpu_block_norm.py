@@ -106,10 +106,11 @@ class Case:
         assert_within(got, want, off + HALF[self.dtype] * (np.abs(want) + off) + tiny)
 
 
-def norm_off(x, n, layer):
+def norm_off(x, n, layer, eps=1e-5):
     off = 28 * U * np.abs(n)
-    if layer:  # the mean is off by 40 roundings of the mean magnitude, the difference by one more
-        off = off + (40 * np.abs(x).mean(-1, keepdims=True) + np.abs(x)) * U * np.abs(n).max(-1, keepdims=True) / (np.abs(x - x.mean(-1, keepdims=True)).max(-1, keepdims=True) + 1e-300)
+    if layer:  # the mean is off by 40 roundings of the mean magnitude, the difference by one more; the quotient passes that on
+        d = x - x.mean(-1, keepdims=True)
+        off = off + (40 * np.abs(x).mean(-1, keepdims=True) + np.abs(x)) * U / np.sqrt((d * d).mean(-1, keepdims=True) + eps)
     return off
 
 
