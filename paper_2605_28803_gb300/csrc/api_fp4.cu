@@ -22,6 +22,7 @@ struct qvla_fp4_layer {
   uint8_t* ws = nullptr;    // device, scale tiles of the rows in that order, rows up to a multiple of 256
   float* wscale = nullptr;  // device [N] (ones for MX)
   float* bias = nullptr;    // device [N] (zeros without one)
+  alignas(qvla::kFp4MapBytes) uint8_t maps[qvla::kFp4Maps * qvla::kFp4MapBytes] = {};  // tensor maps of wq and ws
 };
 
 namespace {
@@ -125,7 +126,7 @@ qvla_status quantize(const void* x, int xdt, int64_t x_stride, int M, int K, int
 }
 
 qvla_status multiply(const qvla_fp4_layer* L, const uint8_t* xq, const uint8_t* xs, const float* xscale, int M, void* y, void* stream) {
-  qvla::Fp4GemmArgs a = {xq, xs, L->fmt == QVLA_NVFP4 ? xscale : nullptr, L->wq, L->ws, L->wscale, L->bias, L->fmt, L->ydt, L->gated,
+  qvla::Fp4GemmArgs a = {xq, xs, L->fmt == QVLA_NVFP4 ? xscale : nullptr, L->wq, L->ws, L->maps, L->wscale, L->bias, L->fmt, L->ydt, L->gated,
                          M, L->N, L->K, y, 0, static_cast<cudaStream_t>(stream)};
   a.num_sms = qvla::num_sms(L->device);
   QVLA_CUDA(qvla::launch_fp4_gemm(a), "gemm_fp4 launch");
@@ -195,6 +196,7 @@ qvla_status create(int N, int K, int had_block, qvla_fp4_format fmt, qvla_dtype 
   if (e == cudaSuccess) e = cudaMemcpy(L->ws, scales.data(), sbytes, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(L->wscale, row.data(), fbytes, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(L->bias, add.data(), fbytes, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = qvla::fp4_weight_maps(L->wq, L->ws, L->fmt, N, K, L->maps);
   if (e != cudaSuccess) {
     qvla_fp4_layer_destroy(L);
     return qvla::cuda_fail(e, "layer upload");

@@ -423,6 +423,10 @@ cudaError_t make_tmap_y(CUtensorMap* m, void* base, int rows, int width) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+const CUtensorMap& weight_map(const Fp4GemmArgs& a, int i) {
+  return *reinterpret_cast<const CUtensorMap*>(static_cast<const uint8_t*>(a.maps) + i * kFp4MapBytes);
+}
+
 // Raises the kernel's limit of dynamic shared memory once per device; `done` holds the devices where it is.
 cudaError_t raise_smem(const void* kern, int bytes, std::atomic<unsigned long long>* done) {
   int dev = 0;
@@ -442,12 +446,11 @@ cudaError_t launch_pair(const Fp4GemmArgs& a) {
   static std::atomic<unsigned long long> raised{0};
   cudaError_t e = raise_smem(reinterpret_cast<const void*>(kern), C::kSmem, &raised);
   if (e != cudaSuccess) return e;
-  CUtensorMap tx = {}, txs = {}, tw = {}, tws = {}, ty = {};
+  CUtensorMap tx = {}, txs = {}, ty = {};
+  const CUtensorMap &tw = weight_map(a, 0), &tws = weight_map(a, C::kKb);
   const int tiles = a.K / C::kTileCodes;
   e = make_tmap_bytes(&tx, a.xq, a.M, a.K / 2, kBn / 2);
   if (e == cudaSuccess) e = make_tmap_scales(&txs, a.xs, (a.M + 127) / 128, tiles, C::kTiles, C::kAtoms);
-  if (e == cudaSuccess) e = make_tmap_bytes(&tw, a.wq, a.N, a.K / 2, 128);
-  if (e == cudaSuccess) e = make_tmap_scales(&tws, a.ws, (a.N + 255) / 256 * 2, tiles, C::kTiles, 1);
   if (e == cudaSuccess) e = make_tmap_y(&ty, a.y, a.M, kGated ? a.N / 2 : a.N);
   if (e != cudaSuccess) return e;
   PairParams p = {a.xrow, a.wrow, a.bias, a.M, a.N, a.K, (a.M + kBn - 1) / kBn, (a.N + 255) / 256, 0};
@@ -707,12 +710,11 @@ cudaError_t launch_split(const Fp4GemmArgs& a) {
   static std::atomic<unsigned long long> raised{0};
   cudaError_t e = raise_smem(reinterpret_cast<const void*>(kern), kMost * C::kStage + kRecv + 1024, &raised);
   if (e != cudaSuccess) return e;
-  CUtensorMap tx = {}, txs = {}, tw = {}, tws = {};
+  CUtensorMap tx = {}, txs = {};
+  const CUtensorMap &tw = weight_map(a, 0), &tws = weight_map(a, 1);
   const int tiles = a.K / C::kTileCodes, nkb = (a.K + 255) / 256;
   e = make_tmap_bytes(&tx, a.xq, a.M, a.K / 2, kBn);
   if (e == cudaSuccess) e = make_tmap_scales(&txs, a.xs, (a.M + 127) / 128, tiles, C::kTiles, 1);
-  if (e == cudaSuccess) e = make_tmap_bytes(&tw, a.wq, a.N, a.K / 2, 128);
-  if (e == cudaSuccess) e = make_tmap_scales(&tws, a.ws, (a.N + 255) / 256 * 2, tiles, C::kTiles, 1);
   if (e != cudaSuccess) return e;
   const int range = (nkb + kSplit - 1) / kSplit;
   const unsigned weight_tiles = static_cast<unsigned>((a.N + 127) / 128), token_tiles = static_cast<unsigned>((a.M + kBn - 1) / kBn);
@@ -816,6 +818,17 @@ cudaError_t launch_f4_t(const Fp4GemmArgs& a) {
 }
 
 }  // namespace
+
+static_assert(sizeof(CUtensorMap) <= kFp4MapBytes && alignof(CUtensorMap) <= kFp4MapBytes, "a map's place");
+
+cudaError_t fp4_weight_maps(const uint8_t* wq, const uint8_t* ws, int fmt, int N, int K, void* maps) {
+  uint8_t* const at = static_cast<uint8_t*>(maps);
+  const int codes = fmt == fp4::kMx ? 128 : 64, groups = (N + 255) / 256 * 2;
+  cudaError_t e = make_tmap_bytes(reinterpret_cast<CUtensorMap*>(at), wq, N, K / 2, 128);
+  for (int i = 1; i < kFp4Maps && e == cudaSuccess; ++i)
+    e = make_tmap_scales(reinterpret_cast<CUtensorMap*>(at + i * kFp4MapBytes), ws, groups, K / codes, i * 256 / codes, 1);
+  return e;
+}
 
 cudaError_t launch_fp4_gemm(const Fp4GemmArgs& a) {
   if (a.fmt == fp4::kMx) return a.gated ? launch_f4_t<fp4::kMx, true>(a) : launch_f4_t<fp4::kMx, false>(a);

@@ -259,6 +259,7 @@ struct Fp4GemmArgs {
   const uint8_t *xq, *xs;  // [M][K/2] codes, scale tiles
   const float* xrow;       // [M], or null (MX)
   const uint8_t *wq, *ws;  // the layer's: [N][K/2] codes, scale tiles of N rows rounded up to 256
+  const void* maps;        // their tensor maps (fp4_weight_maps)
   const float *wrow, *bias;  // [N]
   int fmt, ydt, gated;     // gated: rows in turns of 16 gate rows and the 16 up rows that go with them
   int M, N, K;             // N = weight rows
@@ -267,6 +268,9 @@ struct Fp4GemmArgs {
   cudaStream_t stream;
 };
 cudaError_t launch_fp4_gemm(const Fp4GemmArgs& a);
+// Tensor maps of a layer's weights, made once: codes; scales by 256 codes of K; scales by 512.
+constexpr int kFp4Maps = 3, kFp4MapBytes = 128;
+cudaError_t fp4_weight_maps(const uint8_t* wq, const uint8_t* ws, int fmt, int N, int K, void* maps);
 cudaError_t read_and_clear_error_word_fp4(unsigned int* out, cudaStream_t stream);
 cudaError_t set_debug_hooks_fp4(unsigned long long wait_limit_ns, int hold_loads);
 

@@ -388,7 +388,8 @@ def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, b
         _check(status)
 
 
-# 4-bit floating point and the norms around a block
+# 4-bit floating point and the norms around a block.  The calls of a step marshal their arguments inline, as above: what is
+# optional is None or a tensor, a stream None, an address or a torch stream.
 
 def qvla_fp4_scale_bytes(fmt: int, rows: int, K: int) -> int:
     return int(_lib.qvla_fp4_scale_bytes(fmt, rows, K))
@@ -397,16 +398,19 @@ def qvla_fp4_scale_bytes(fmt: int, rows: int, K: int) -> int:
 def qvla_fp4_quantize_rows(x, xdt: int, x_stride: int, M: int, K: int, had_block: int, fmt: int, step_scale, xq, xs, xscale=None,
                            stream=None) -> None:
     """Rotate and quantise rows to E2M1 codes and block scales (NVFP4: and a float32 scale a row)."""
-    status = _lib.qvla_fp4_quantize_rows(x.data_ptr(), xdt, x_stride, M, K, had_block, fmt, _ptr(step_scale), xq.data_ptr(),
-                                         xs.data_ptr(), _ptr(xscale), _stream(stream))
+    status = _lib.qvla_fp4_quantize_rows(x.data_ptr(), xdt, x_stride, M, K, had_block, fmt,
+                                         None if step_scale is None else step_scale.data_ptr(), xq.data_ptr(), xs.data_ptr(),
+                                         None if xscale is None else xscale.data_ptr(),
+                                         None if stream is None else stream if type(stream) is int else stream.cuda_stream)
     if status:
         _check(status)
 
 
 def qvla_fp4_dequantize_rows(xq, xs, xscale, fmt: int, M: int, K: int, out, odt: int, stream=None) -> None:
     """What the codes stand for, in the rotated basis."""
-    status = _lib.qvla_fp4_dequantize_rows(xq.data_ptr(), xs.data_ptr(), _ptr(xscale), fmt, M, K, out.data_ptr(), odt,
-                                           _stream(stream))
+    status = _lib.qvla_fp4_dequantize_rows(xq.data_ptr(), xs.data_ptr(), None if xscale is None else xscale.data_ptr(), fmt, M,
+                                           K, out.data_ptr(), odt,
+                                           None if stream is None else stream if type(stream) is int else stream.cuda_stream)
     if status:
         _check(status)
 
@@ -455,7 +459,8 @@ def qvla_fp4_layer_create_gated(H: int, K: int, had_block: int, fmt: int, xdt: i
 
 
 def qvla_gemm_fp4(layer: Fp4Layer, xq, xs, xscale, M: int, y, stream=None) -> None:
-    status = _lib.qvla_gemm_fp4(layer.handle, xq.data_ptr(), xs.data_ptr(), _ptr(xscale), M, y.data_ptr(), _stream(stream))
+    status = _lib.qvla_gemm_fp4(layer.handle, xq.data_ptr(), xs.data_ptr(), None if xscale is None else xscale.data_ptr(), M,
+                                y.data_ptr(), None if stream is None else stream if type(stream) is int else stream.cuda_stream)
     if status:
         _check(status)
 
@@ -465,8 +470,9 @@ def qvla_fp4_linear_workspace_bytes(layer: Fp4Layer, M: int) -> int:
 
 
 def qvla_fp4_linear(layer: Fp4Layer, x, M: int, step_scale, y, workspace, workspace_bytes: int, stream=None) -> None:
-    status = _lib.qvla_fp4_linear(layer.handle, x.data_ptr(), M, _ptr(step_scale), y.data_ptr(), _ptr(workspace), workspace_bytes,
-                                  _stream(stream))
+    status = _lib.qvla_fp4_linear(layer.handle, x.data_ptr(), M, None if step_scale is None else step_scale.data_ptr(),
+                                  y.data_ptr(), None if workspace is None else workspace.data_ptr(), workspace_bytes,
+                                  None if stream is None else stream if type(stream) is int else stream.cuda_stream)
     if status:
         _check(status)
 
@@ -501,8 +507,10 @@ class BlockNorm:
 
 def qvla_block_norm(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: int, M: int, K: int, r_out, h, stream=None) -> None:
     """Residual + gated branch, then the norm; y, r_out or h may be None as in include/qvla.h."""
-    status = _lib.qvla_block_norm(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, _ptr(y), y_stride, M, K, _ptr(r_out), _ptr(h),
-                                  _stream(stream))
+    status = _lib.qvla_block_norm(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, None if y is None else y.data_ptr(),
+                                  y_stride, M, K, None if r_out is None else r_out.data_ptr(),
+                                  None if h is None else h.data_ptr(),
+                                  None if stream is None else stream if type(stream) is int else stream.cuda_stream)
     if status:
         _check(status)
 
@@ -510,9 +518,12 @@ def qvla_block_norm(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: in
 def qvla_block_norm_fp4(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: int, M: int, K: int, r_out, h, had_block: int,
                         fmt: int, step_scale, hq, hs, hscale=None, stream=None) -> None:
     """The same with its output rotated and quantised."""
-    status = _lib.qvla_block_norm_fp4(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, _ptr(y), y_stride, M, K, _ptr(r_out), _ptr(h),
-                                      had_block, fmt, _ptr(step_scale), hq.data_ptr(), hs.data_ptr(), _ptr(hscale),
-                                      _stream(stream))
+    status = _lib.qvla_block_norm_fp4(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, None if y is None else y.data_ptr(),
+                                      y_stride, M, K, None if r_out is None else r_out.data_ptr(),
+                                      None if h is None else h.data_ptr(), had_block, fmt,
+                                      None if step_scale is None else step_scale.data_ptr(), hq.data_ptr(), hs.data_ptr(),
+                                      None if hscale is None else hscale.data_ptr(),
+                                      None if stream is None else stream if type(stream) is int else stream.cuda_stream)
     if status:
         _check(status)
 
