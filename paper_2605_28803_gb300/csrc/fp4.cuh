@@ -74,13 +74,20 @@ __device__ __forceinline__ void bring_near(float& a, float& d) {
   }
 }
 
+// 1 / x within 2^-23 of it, x and the quotient normal numbers.
+__device__ __forceinline__ float near_reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // The E4M3 byte nearest the exact quotient a / (6 delta), ties to the even byte; 448 at most.  a >= 0, delta > 0 finite.
 // The float32 quotient is within 2^-21 of the exact one: where its neighbours 2^-20 away round alike it decides; else the
 // midpoint between both bytes does, by the sign of a - midpoint * 6 delta (exact in one FMA: a midpoint has 5 bits, 6 of
 // them with the factor 3, and float32 holds the factor).
 __device__ __forceinline__ uint32_t block_scale_e4m3(float a, float delta) {
   bring_near(a, delta);
-  const float t = a * __frcp_rn(6.0f * delta);
+  const float t = a * near_reciprocal(6.0f * delta);
   const uint32_t both = e4m3x2(t * 0.99999904632568359375f, t * 1.00000095367431640625f);
   const uint32_t lo = both & 0xFFu, hi = both >> 8;
   if (lo == hi) return lo;

@@ -112,8 +112,11 @@ __device__ __forceinline__ void store_unit(T* p, float2* v) {
 
 // A row's place among the CTA's warps, and sums and maxima over it.  Every thread of the CTA makes the same calls.
 struct RowGroup {
-  float* slots;      // [slot][kMaxWarps]
-  int warps, first;  // of the row
+  float* slots;             // [slot][kMaxWarps]
+  int warps, first, span;   // of the row: its warps, the first, and their number rounded up to a power of two
+  __device__ __forceinline__ RowGroup(float* s, int w, int f) : slots(s), warps(w), first(f), span(1) {
+    while (span < w) span *= 2;
+  }
   __device__ __forceinline__ float sum(float v, int slot) const {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -122,10 +125,9 @@ struct RowGroup {
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
     // every warp adds the warps' sums in the same order
-    const int lane = threadIdx.x & 31;
-    v = lane < warps ? s[first + lane] : 0.0f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    const int w = static_cast<int>(threadIdx.x) & (span - 1);
+    v = w < warps ? s[first + w] : 0.0f;
+    for (int o = span >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
   // The largest; NaN if one is (bit patterns of non-negative floats order like the numbers, NaN above infinity).
@@ -151,10 +153,6 @@ struct Raw {
 #pragma unroll
     for (int k = 0; k < kPer; ++k) q[i * kPer + k] = reinterpret_cast<const uint4*>(p)[k];
   }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int k = 0; k < N * kPer; ++k) q[k] = make_uint4(0u, 0u, 0u, 0u);
-  }
   __device__ __forceinline__ float2 pair(int i) const {  // channels 2 i and 2 i + 1
     if constexpr (kPer == 2) {
       const uint4 w = q[i >> 1];
@@ -166,25 +164,27 @@ struct Raw {
   }
 };
 
-// v to (v - mean) / sqrt(var + eps), or v / sqrt(mean v^2 + eps); the variance from the deviations, in a second pass over the
-// registers.  Channels that are not there hold 0 and are left 0.
-template <int N, typename Valid>
-__device__ __forceinline__ void normalize(float2 (&v)[4 * N], const RowGroup& row, int slot, bool layer, float k, float eps, Valid valid) {
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// v to v - mean with `layer`, and what it then has to be multiplied by: 1 / sqrt(mean v^2 + eps), the variance from the
+// deviations in a second pass over the registers.  A thread without channels holds zeros, which stay.  k: the channels, and
+// their reciprocal.  (IEEE division and square root by every thread took 120 of a row's 430 instructions; the reciprocal square
+// root is within 2^-22.)
+template <int N>
+__device__ __forceinline__ float norm_scale(float2 (&v)[4 * N], const bool (&has)[N], const RowGroup& row, int slot, bool layer, float2 k, float eps) {
   if (layer) {
-    float s = 0.0f;
+    float2 s = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < 4 * N; ++i) s += v[i].x + v[i].y;
-    const float mean = __fdiv_rn(row.sum(s, slot), k);  // (a quotient: of equal channels it is their value)
+    for (int i = 0; i < 4 * N; ++i) s = __fadd2_rn(s, v[i]);
+    const float sum = row.sum(s.x + s.y, slot), near = sum * k.y;
+    const float mean = fmaf(fmaf(-near, k.x, sum), k.y, near);  // the quotient to its last bit: of equal channels it is their value
 #pragma unroll
-    for (int i = 0; i < 4 * N; ++i)
-      if (valid(i >> 2)) v[i] = make_float2(v[i].x - mean, v[i].y - mean);
+    for (int i = 0; i < 4 * N; ++i) v[i] = __fadd2_rn(v[i], both(has[i >> 2] ? -mean : 0.0f));
   }
-  float s = 0.0f;
+  float2 s = both(0.0f);
 #pragma unroll
-  for (int i = 0; i < 4 * N; ++i) s = fmaf(v[i].x, v[i].x, fmaf(v[i].y, v[i].y, s));
-  const float scale = 1.0f / sqrtf(__fdiv_rn(row.sum(s, slot + 1), k) + eps);
-#pragma unroll
-  for (int i = 0; i < 4 * N; ++i) v[i] = make_float2(v[i].x * scale, v[i].y * scale);
+  for (int i = 0; i < 4 * N; ++i) s = __ffma2_rn(v[i], v[i], s);
+  return rsqrtf(fmaf(row.sum(s.x + s.y, slot + 1), k.y, eps));
 }
 
 // A group of threads takes rows m, m + step, ... (`rows` of them, those below M): thread j its pieces j, j + threads, ...  h goes
@@ -192,41 +192,63 @@ __device__ __forceinline__ void normalize(float2 (&v)[4 * N], const RowGroup& ro
 template <typename R, typename T, int N, typename Store>
 __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row, int j, int m, int step, int rows, Store store) {
   const int threads = row.warps * 32;
-  const float width = static_cast<float>(a.K), off = a.norm.weight_offset, alpha = a.norm.residual_scale;
-  const bool layer = a.norm.layer != 0, norm_h = a.h != nullptr || a.codes != nullptr;
+  const float2 width = make_float2(static_cast<float>(a.K), 1.0f / static_cast<float>(a.K));
+  const float eps = a.norm.eps;
+  const float2 off = both(a.norm.weight_offset), alpha = both(a.norm.residual_scale);
+  const bool layer = a.norm.layer != 0, post = a.norm.post_norm != 0, norm_h = a.h != nullptr || a.codes != nullptr;
   const T* const gate = static_cast<const T*>(a.norm.gate);
   const T* const scale = static_cast<const T*>(a.norm.scale);
   const T* const shift = static_cast<const T*>(a.norm.shift);
-  auto channel = [&](int i) { return (j + i * threads) * 8; };
-  auto there = [&](int i) { return channel(i) < a.K; };
-  constexpr bool kHold = N == 1;  // weights and conditioning stay in registers from the row's start (with two pieces: loaded at their use)
-  auto take = [&](Raw<T, N>& to, const void* from) {
-    to.zero();
-    if (from == nullptr) return;
+  bool has[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (there(i)) to.load(i, static_cast<const T*>(from) + channel(i));
+  for (int i = 0; i < N; ++i) has[i] = (j + i * threads) * 8 < a.K;
+  auto channel = [&](int i) { return (j + i * threads) * 8; };
+  constexpr bool kHold = N == 1;  // weights and conditioning stay in registers from the row's start (with two pieces: loaded at their use)
+  auto take = [&](Raw<T, N>& to, const T* from) {  // what is not there reads as zeros
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (from != nullptr && has[i]) {
+        to.load(i, from + channel(i));
+      } else {
+        to.q[i] = make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
   };
-  Raw<T, N> post_w, pre_w, pre_b;  // the same for every row
+  // f(i, pair i) of a vector, held since the row's start or loaded now
+  auto with = [&](const auto& held, const T* from, auto f) {
+    if constexpr (kHold) {
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) f(i, held.pair(i));
+    } else {
+      Raw<T, N> t;
+      take(t, from);
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) f(i, t.pair(i));
+    }
+  };
+  const T* const post_weight = static_cast<const T*>(a.norm.post_weight);
+  const T* const pre_weight = static_cast<const T*>(a.norm.pre_weight);
+  const T* const pre_bias = static_cast<const T*>(a.norm.pre_bias);
+  Raw<T, kHold ? N : 1> post_w, pre_w, pre_b;  // the same for every row
   if constexpr (kHold) {
-    take(post_w, a.norm.post_weight);
-    take(pre_w, a.norm.pre_weight);
-    take(pre_b, a.norm.pre_bias);
+    take(post_w, post_weight);
+    take(pre_w, pre_weight);
+    take(pre_b, pre_bias);
   }
   griddep_wait();  // rows (and the conditioning) come from earlier kernels, which may still read what this one writes
   griddep_launch_dependents();
 
-  Raw<R, N> r;
-  Raw<T, N> y;
+  Raw<R, N> r = {};
+  Raw<T, N> y = {};
   auto fetch = [&](int at) {
-    r.zero();
-    y.zero();
     if (at >= a.M) return;
+    const R* const pr = static_cast<const R*>(a.x) + static_cast<size_t>(at) * a.x_stride;
+    const T* const py = static_cast<const T*>(a.y) + static_cast<size_t>(at) * a.y_stride;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (!there(i)) continue;
-      r.load(i, static_cast<const R*>(a.x) + static_cast<size_t>(at) * a.x_stride + channel(i));
-      if (a.y != nullptr) y.load(i, static_cast<const T*>(a.y) + static_cast<size_t>(at) * a.y_stride + channel(i));
+      if (!has[i]) continue;
+      r.load(i, pr + channel(i));
+      if (a.y != nullptr) y.load(i, py + channel(i));
     }
   };
   fetch(m);
@@ -245,7 +267,7 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row
       }
     }
     auto row_of = [&](const T* t) { return t != nullptr && live ? t + mod : static_cast<const T*>(nullptr); };
-    Raw<T, N> g, sc, sh;
+    Raw<T, kHold ? N : 1> g, sc, sh;
     if constexpr (kHold) {
       take(g, a.y != nullptr ? row_of(gate) : nullptr);
       take(sc, row_of(scale));
@@ -255,80 +277,44 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row
     if (a.y != nullptr) {
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) v[i] = y.pair(i);
-      if (a.norm.post_norm) {
-        normalize<N>(v, row, slot, layer, width, a.norm.eps, there);
-        if (a.norm.post_weight != nullptr) {
-          if constexpr (!kHold) take(post_w, a.norm.post_weight);
+      if (post) {
+        const float2 s = both(norm_scale<N>(v, has, row, slot, layer, width, eps));
+        if (post_weight != nullptr) {
+          with(post_w, post_weight, [&](int i, float2 w) { v[i] = __fmul2_rn(__fmul2_rn(v[i], s), __fadd2_rn(w, off)); });
+        } else {
 #pragma unroll
-          for (int i = 0; i < 4 * N; ++i) {
-            const float2 w = post_w.pair(i);
-            v[i] = make_float2(v[i].x * (w.x + off), v[i].y * (w.y + off));
-          }
+          for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(v[i], s);
         }
       }
       if (gate != nullptr) {
-        if constexpr (!kHold) take(g, row_of(gate));
-#pragma unroll
-        for (int i = 0; i < 4 * N; ++i) {
-          const float2 w = g.pair(i);
-          v[i] = make_float2(v[i].x * w.x, v[i].y * w.y);
-        }
+        with(g, row_of(gate), [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], w); });
       }
 #pragma unroll
-      for (int i = 0; i < 4 * N; ++i) {
-        const float2 w = r.pair(i);
-        v[i] = make_float2(fmaf(alpha, w.x, v[i].x), fmaf(alpha, w.y, v[i].y));
-      }
+      for (int i = 0; i < 4 * N; ++i) v[i] = __ffma2_rn(alpha, r.pair(i), v[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4 * N; ++i) {
-        const float2 w = r.pair(i);
-        v[i] = make_float2(alpha * w.x, alpha * w.y);
-      }
+      for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(alpha, r.pair(i));
     }
     R* const out = a.residual_out != nullptr && live ? static_cast<R*>(a.residual_out) + static_cast<size_t>(m) * a.x_stride : nullptr;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (there(i)) store_unit<8>(out == nullptr ? static_cast<R*>(nullptr) : out + channel(i), v + 4 * i);
+      if (has[i]) store_unit<8>(out == nullptr ? static_cast<R*>(nullptr) : out + channel(i), v + 4 * i);
     if (k + 1 < rows) fetch(m + step);  // (after this row's stores: a caller may update the residual in place)
     if (!norm_h) continue;
-    normalize<N>(v, row, slot + 2, layer, width, a.norm.eps, there);
+    const float2 s = both(norm_scale<N>(v, has, row, slot + 2, layer, width, eps));
     T* const h = a.h != nullptr && live ? static_cast<T*>(a.h) + static_cast<size_t>(m) * a.K : nullptr;
-    if (a.norm.pre_weight != nullptr) {
-      if constexpr (!kHold) take(pre_w, a.norm.pre_weight);
+    if (pre_weight != nullptr) {
+      with(pre_w, pre_weight, [&](int i, float2 w) { v[i] = __fmul2_rn(__fmul2_rn(v[i], s), __fadd2_rn(w, off)); });
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4 * N; ++i) {
-        const float2 w = pre_w.pair(i);
-        v[i] = make_float2(v[i].x * (w.x + off), v[i].y * (w.y + off));
-      }
+      for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(v[i], s);
     }
-    if (a.norm.pre_bias != nullptr) {
-      if constexpr (!kHold) take(pre_b, a.norm.pre_bias);
-#pragma unroll
-      for (int i = 0; i < 4 * N; ++i) {
-        const float2 w = pre_b.pair(i);
-        v[i] = make_float2(v[i].x + w.x, v[i].y + w.y);
-      }
-    }
-    if (scale != nullptr) {
-      if constexpr (!kHold) take(sc, row_of(scale));
-#pragma unroll
-      for (int i = 0; i < 4 * N; ++i) {
-        const float2 w = sc.pair(i);
-        v[i] = make_float2(v[i].x * (1.0f + w.x), v[i].y * (1.0f + w.y));
-      }
-    }
-    if (shift != nullptr) {
-      if constexpr (!kHold) take(sh, row_of(shift));
-#pragma unroll
-      for (int i = 0; i < 4 * N; ++i) {
-        const float2 w = sh.pair(i);
-        v[i] = make_float2(v[i].x + w.x, v[i].y + w.y);
-      }
-    }
+    if (pre_bias != nullptr) with(pre_b, pre_bias, [&](int i, float2 w) { v[i] = __fadd2_rn(v[i], w); });
+    if (scale != nullptr) with(sc, row_of(scale), [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], __fadd2_rn(w, both(1.0f))); });
+    if (shift != nullptr) with(sh, row_of(shift), [&](int i, float2 w) { v[i] = __fadd2_rn(v[i], w); });
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (!there(i)) continue;
+      if (!has[i]) continue;
       store_unit<8>(h == nullptr ? static_cast<T*>(nullptr) : h + channel(i), v + 4 * i);
       store(k, channel(i), v + 4 * i, live);
     }
@@ -509,7 +495,7 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
       bytes |= s << (8 * b);
       const float d = e4m3_value(s) * delta;
       const bool easy = d >= 8.673617379884035e-19f && d <= 1.152921504606846976e18f;  // 2^-60 .. 2^60
-      const float r = easy ? __frcp_rn(d) : 0.0f;
+      const float r = easy ? near_reciprocal(d) : 0.0f;
       // The float32 quotient is within 2^-22 of the exact one: where it rounds alike moved up and down by 2^-20 it decides.
       const float up = r * 1.00000095367431640625f, dn = r * 0.99999904632568359375f;
 #pragma unroll
@@ -542,7 +528,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) quantize_rows_kernel(const Row
   __shared__ float s_red[kMaxWarps];
   const int tpr = a.row_warps * 32;
   const int rloc = static_cast<int>(threadIdx.x) / tpr, j = static_cast<int>(threadIdx.x) - rloc * tpr;
-  const RowGroup row = {s_red, a.row_warps, rloc * a.row_warps};
+  const RowGroup row(s_red, a.row_warps, rloc * a.row_warps);
   const int m = blockIdx.x * a.group_rows + rloc;
   const bool active = m < a.M && j * 32 < a.K;
   const P place(j);
@@ -574,7 +560,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const Ro
   if (threadIdx.x == 0) s_live = 0u;
   __syncthreads();
   {
-    const RowGroup group = {s_red, a.row_warps, g * a.row_warps};
+    const RowGroup group(s_red, a.row_warps, g * a.row_warps);
     // (rows of a group lie next to one another)
     norm_rows<R, T, N>(a, group, j1, m0 + g * a.group_rows, 1, a.group_rows, [&](int k, int channel, const float2* p, bool live) {
       const int r = g * a.group_rows + k;
@@ -589,7 +575,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const Ro
   // the second dealing: quant_warps warps a row
   const int quant_warps = (a.K + 1023) / 1024, tpr = quant_warps * 32;
   const int rloc = static_cast<int>(threadIdx.x) / tpr, j = static_cast<int>(threadIdx.x) - rloc * tpr;
-  const RowGroup row = {s_red, quant_warps, rloc * quant_warps};
+  const RowGroup row(s_red, quant_warps, rloc * quant_warps);
   const bool active = rloc < groups * a.group_rows && ((s_live >> (rloc & 31)) & 1u) && j * 32 < a.K;
   const P place(j);
   float2 v[16];
@@ -611,7 +597,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const RowsArgs a)
   const int tpg = a.row_warps * 32;
   const int g = static_cast<int>(threadIdx.x) / tpg, j = static_cast<int>(threadIdx.x) - g * tpg;
   const int groups = static_cast<int>(blockDim.x) / tpg, step = static_cast<int>(gridDim.x) * groups;
-  const RowGroup group = {s_red, a.row_warps, g * a.row_warps};
+  const RowGroup group(s_red, a.row_warps, g * a.row_warps);
   const int first = blockIdx.x * groups;  // every group of the CTA makes as many turns
   norm_rows<R, T, N>(a, group, j, first + g, step, first < a.M ? (a.M - first + step - 1) / step : 0, [](int, int, const float2*, bool) {});
 }
