@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restri
       v[k].x = fp4::e2m1_value(w[i] >> (8 * k)) * s[i >> 1] * row;
       v[k].y = fp4::e2m1_value(w[i] >> (8 * k + 4)) * s[i >> 1] * row;
     }
-    fp4::store_unit<8>(out + at * 32 + i * 8, v);
+    fp4::write_unit(out + at * 32 + i * 8, v);
   }
 }
 

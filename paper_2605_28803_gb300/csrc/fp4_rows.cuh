@@ -80,34 +80,23 @@ __device__ __forceinline__ uint32_t narrow(float2 f, __nv_bfloat16) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-template <int N>
-__device__ __forceinline__ void store_unit(float* p, float2* v) {
-  if (p == nullptr) return;
-  if constexpr (N >= 4) {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-      *reinterpret_cast<float4*>(p + 4 * i) = make_float4(v[2 * i].x, v[2 * i].y, v[2 * i + 1].x, v[2 * i + 1].y);
-  } else {
-    *reinterpret_cast<float2*>(p) = v[0];
-  }
+// Eight values as T; rounded to T and back; in memory.
+template <typename T>
+__device__ __forceinline__ uint4 pack_unit(const float2* v, T t) {
+  return make_uint4(narrow(v[0], t), narrow(v[1], t), narrow(v[2], t), narrow(v[3], t));
 }
-// Stores the values rounded to T, and leaves the rounded ones in v; p may be null (rounding only).
-template <int N, typename T>
-__device__ __forceinline__ void store_unit(T* p, float2* v) {
-  uint32_t w[N / 2];
+template <typename T>
+__device__ __forceinline__ void round_unit(float2* v, T t) {
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    w[i] = narrow(v[i], T());
-    v[i] = widen(w[i], T());
-  }
-  if (p == nullptr) return;
-  if constexpr (N == 8) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else if constexpr (N == 4) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-  } else {
-    *reinterpret_cast<uint32_t*>(p) = w[0];
-  }
+  for (int i = 0; i < 4; ++i) v[i] = widen(narrow(v[i], t), t);
+}
+template <typename T>
+__device__ __forceinline__ void write_unit(T* p, const float2* v) {
+  *reinterpret_cast<uint4*>(p) = pack_unit(v, T());
+}
+__device__ __forceinline__ void write_unit(float* p, const float2* v) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
 }
 
 // A row's place among the CTA's warps, and sums and maxima over it.  Every thread of the CTA makes the same calls.
@@ -167,156 +156,155 @@ struct Raw {
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // v to v - mean with `layer`, and what it then has to be multiplied by: 1 / sqrt(mean v^2 + eps), the variance from the
-// deviations in a second pass over the registers.  A thread without channels holds zeros, which stay.  k: the channels, and
-// their reciprocal.  (IEEE division and square root by every thread took 120 of a row's 430 instructions; the reciprocal square
+// deviations in a second pass over the registers.  A thread without channels adds nothing, whatever it holds.  k: the channels,
+// and their reciprocal.  (IEEE division and square root by every thread took 120 of a row's 430 instructions; the reciprocal square
 // root is within 2^-22.)
 template <int N>
-__device__ __forceinline__ float norm_scale(float2 (&v)[4 * N], const bool (&has)[N], const RowGroup& row, int slot, bool layer, float2 k, float eps) {
-  if (layer) {
-    float2 s = both(0.0f);
+__device__ __forceinline__ float sum_there(const float2 (&s)[N], const bool (&has)[N]) {
+  float t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4 * N; ++i) s = __fadd2_rn(s, v[i]);
-    const float sum = row.sum(s.x + s.y, slot), near = sum * k.y;
+  for (int i = 0; i < N; ++i) t += has[i] ? s[i].x + s[i].y : 0.0f;
+  return t;
+}
+template <int N>
+__device__ __forceinline__ float norm_scale(float2 (&v)[4 * N], const bool (&has)[N], const RowGroup& row, int slot, bool layer, float2 k, float eps) {
+  float2 s[N];
+  if (layer) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = __fadd2_rn(__fadd2_rn(v[4 * i], v[4 * i + 1]), __fadd2_rn(v[4 * i + 2], v[4 * i + 3]));
+    const float sum = row.sum(sum_there<N>(s, has), slot), near = sum * k.y;
     const float mean = fmaf(fmaf(-near, k.x, sum), k.y, near);  // the quotient to its last bit: of equal channels it is their value
 #pragma unroll
-    for (int i = 0; i < 4 * N; ++i) v[i] = __fadd2_rn(v[i], both(has[i >> 2] ? -mean : 0.0f));
+    for (int i = 0; i < 4 * N; ++i) v[i] = __fadd2_rn(v[i], both(-mean));
   }
-  float2 s = both(0.0f);
 #pragma unroll
-  for (int i = 0; i < 4 * N; ++i) s = __ffma2_rn(v[i], v[i], s);
-  return rsqrtf(fmaf(row.sum(s.x + s.y, slot + 1), k.y, eps));
+  for (int i = 0; i < N; ++i) {
+    s[i] = __fmul2_rn(v[4 * i], v[4 * i]);
+#pragma unroll
+    for (int q = 1; q < 4; ++q) s[i] = __ffma2_rn(v[4 * i + q], v[4 * i + q], s[i]);
+  }
+  return rsqrtf(fmaf(row.sum(sum_there<N>(s, has), slot + 1), k.y, eps));
 }
 
 // A group of threads takes rows m, m + step, ... (`rows` of them, those below M): thread j its pieces j, j + threads, ...  h goes
 // to global memory where it is wanted, and with `store` (row number, channel, 8 values as T) to the caller.
-template <typename R, typename T, int N, typename Store>
+// kMods, kPost: conditioning and branch norm may be there (without, their code is not).
+template <typename R, typename T, int N, bool kMods, bool kPost, typename Store>
 __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row, int j, int m, int step, int rows, Store store) {
-  const int threads = row.warps * 32;
   const float2 width = make_float2(static_cast<float>(a.K), 1.0f / static_cast<float>(a.K));
-  const float eps = a.norm.eps;
   const float2 off = both(a.norm.weight_offset), alpha = both(a.norm.residual_scale);
-  const bool layer = a.norm.layer != 0, post = a.norm.post_norm != 0, norm_h = a.h != nullptr || a.codes != nullptr;
-  const T* const gate = static_cast<const T*>(a.norm.gate);
-  const T* const scale = static_cast<const T*>(a.norm.scale);
-  const T* const shift = static_cast<const T*>(a.norm.shift);
+  const bool layer = a.norm.layer != 0, norm_h = a.h != nullptr || a.codes != nullptr;
+  const bool branch = a.y != nullptr, gated = kMods && branch && a.norm.gate != nullptr;
+  const bool mods = kMods && (a.norm.gate != nullptr || a.norm.scale != nullptr || a.norm.shift != nullptr);
+  // Channels of the thread's pieces.  A piece beyond the row reads the row's first one, so that loads need no branch (with branches
+  // the values that are never there cost 200 to 400 bytes of spills), and adds nothing to sums.
+  const int first = j * 8, apart = row.warps * 256;
   bool has[N];
+  int at[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) has[i] = (j + i * threads) * 8 < a.K;
-  auto channel = [&](int i) { return (j + i * threads) * 8; };
-  constexpr bool kHold = N == 1;  // weights and conditioning stay in registers from the row's start (with two pieces: loaded at their use)
-  auto take = [&](Raw<T, N>& to, const T* from) {  // what is not there reads as zeros
+  for (int i = 0; i < N; ++i) {
+    has[i] = first + i * apart < a.K;
+    at[i] = has[i] ? first + i * apart : 0;
+  }
+  // Weights and conditioning stay in registers from the row's start; with two pieces a thread they are loaded at their use.
+  constexpr bool kHold = N == 1;
+  auto take = [&](Raw<T, N>& to, const void* from, size_t mod) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (from != nullptr && has[i]) {
-        to.load(i, from + channel(i));
-      } else {
-        to.q[i] = make_uint4(0u, 0u, 0u, 0u);
-      }
-    }
+    for (int i = 0; i < N; ++i) to.load(i, static_cast<const T*>(from) + mod + at[i]);
   };
-  // f(i, pair i) of a vector, held since the row's start or loaded now
-  auto with = [&](const auto& held, const T* from, auto f) {
+  // f(i, pair i) of a vector: held since the row's start, or loaded now
+  size_t mod = 0;
+  auto with = [&](const Raw<T, kHold ? N : 1>& held, const void* from, size_t place, auto f) {
     if constexpr (kHold) {
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) f(i, held.pair(i));
     } else {
       Raw<T, N> t;
-      take(t, from);
+      take(t, from, place);
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) f(i, t.pair(i));
     }
   };
-  const T* const post_weight = static_cast<const T*>(a.norm.post_weight);
-  const T* const pre_weight = static_cast<const T*>(a.norm.pre_weight);
-  const T* const pre_bias = static_cast<const T*>(a.norm.pre_bias);
   Raw<T, kHold ? N : 1> post_w, pre_w, pre_b;  // the same for every row
   if constexpr (kHold) {
-    take(post_w, post_weight);
-    take(pre_w, pre_weight);
-    take(pre_b, pre_bias);
+    if (kPost && a.norm.post_weight != nullptr) take(post_w, a.norm.post_weight, 0);
+    if (a.norm.pre_weight != nullptr) take(pre_w, a.norm.pre_weight, 0);
+    if (a.norm.pre_bias != nullptr) take(pre_b, a.norm.pre_bias, 0);
   }
   griddep_wait();  // rows (and the conditioning) come from earlier kernels, which may still read what this one writes
   griddep_launch_dependents();
 
-  Raw<R, N> r = {};
-  Raw<T, N> y = {};
-  auto fetch = [&](int at) {
-    if (at >= a.M) return;
-    const R* const pr = static_cast<const R*>(a.x) + static_cast<size_t>(at) * a.x_stride;
-    const T* const py = static_cast<const T*>(a.y) + static_cast<size_t>(at) * a.y_stride;
+  Raw<R, N> r;  // the operands of the row in work, soon those of the next
+  Raw<T, N> y;
+  auto fetch = [&](int number) {
+    const R* const px = static_cast<const R*>(a.x) + static_cast<size_t>(number) * a.x_stride;
+    const T* const py = static_cast<const T*>(a.y) + static_cast<size_t>(number) * a.y_stride;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (!has[i]) continue;
-      r.load(i, pr + channel(i));
-      if (a.y != nullptr) y.load(i, py + channel(i));
+      r.load(i, px + at[i]);
+      if (branch) y.load(i, py + at[i]);
     }
   };
-  fetch(m);
-  for (int k = 0; k < rows; ++k, m += step) {
+  if (m < a.M) fetch(m);
+  for (int k = 0; k < rows; ++k) {
     const int slot = (k & 1) * 4;
-    // the token's row of the conditioning; a token whose index is out of range is skipped: nothing of it is written
     bool live = m < a.M;
-    size_t mod = 0;
-    if (gate != nullptr || scale != nullptr || shift != nullptr) {
+    Raw<T, kHold ? N : 1> g, sc, sh;
+    if (mods) {  // the token's row of the conditioning; a token whose index is out of range is skipped: nothing of it is written
       const int c = !live ? 0 : a.norm.mod_index != nullptr ? a.norm.mod_index[m] : m / a.norm.mod_tokens;
       if (c < 0 || c >= a.norm.mod_rows) {
         if (live && j == 0) atomicOr(&g_error_word, kErrIndex);
         live = false;
-      } else {
-        mod = static_cast<size_t>(c) * a.norm.mod_stride;
       }
-    }
-    auto row_of = [&](const T* t) { return t != nullptr && live ? t + mod : static_cast<const T*>(nullptr); };
-    Raw<T, kHold ? N : 1> g, sc, sh;
-    if constexpr (kHold) {
-      take(g, a.y != nullptr ? row_of(gate) : nullptr);
-      take(sc, row_of(scale));
-      take(sh, row_of(shift));
+      mod = live ? static_cast<size_t>(c) * a.norm.mod_stride : 0;
+      if constexpr (kHold) {
+        if (gated) take(g, a.norm.gate, mod);
+        if (a.norm.scale != nullptr) take(sc, a.norm.scale, mod);
+        if (a.norm.shift != nullptr) take(sh, a.norm.shift, mod);
+      }
     }
     float2 v[4 * N];
-    if (a.y != nullptr) {
+    if (branch) {
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) v[i] = y.pair(i);
-      if (post) {
-        const float2 s = both(norm_scale<N>(v, has, row, slot, layer, width, eps));
-        if (post_weight != nullptr) {
-          with(post_w, post_weight, [&](int i, float2 w) { v[i] = __fmul2_rn(__fmul2_rn(v[i], s), __fadd2_rn(w, off)); });
-        } else {
+      if (kPost && a.norm.post_norm) {
+        const float2 s = both(norm_scale<N>(v, has, row, slot, layer, width, a.norm.eps));
 #pragma unroll
-          for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(v[i], s);
-        }
+        for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(v[i], s);
+        if (a.norm.post_weight != nullptr) with(post_w, a.norm.post_weight, 0, [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], __fadd2_rn(w, off)); });
       }
-      if (gate != nullptr) {
-        with(g, row_of(gate), [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], w); });
-      }
+      if (gated) with(g, a.norm.gate, mod, [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], w); });
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) v[i] = __ffma2_rn(alpha, r.pair(i), v[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(alpha, r.pair(i));
     }
-    R* const out = a.residual_out != nullptr && live ? static_cast<R*>(a.residual_out) + static_cast<size_t>(m) * a.x_stride : nullptr;
+    const bool write_r = a.residual_out != nullptr && live;
+    R* const po = static_cast<R*>(a.residual_out) + static_cast<size_t>(m) * a.x_stride;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (has[i]) store_unit<8>(out == nullptr ? static_cast<R*>(nullptr) : out + channel(i), v + 4 * i);
-    if (k + 1 < rows) fetch(m + step);  // (after this row's stores: a caller may update the residual in place)
-    if (!norm_h) continue;
-    const float2 s = both(norm_scale<N>(v, has, row, slot + 2, layer, width, eps));
-    T* const h = a.h != nullptr && live ? static_cast<T*>(a.h) + static_cast<size_t>(m) * a.K : nullptr;
-    if (pre_weight != nullptr) {
-      with(pre_w, pre_weight, [&](int i, float2 w) { v[i] = __fmul2_rn(__fmul2_rn(v[i], s), __fadd2_rn(w, off)); });
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(v[i], s);
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(R) == 2) round_unit(v + 4 * i, R());
+      if (write_r && has[i]) write_unit(po + at[i], v + 4 * i);
     }
-    if (pre_bias != nullptr) with(pre_b, pre_bias, [&](int i, float2 w) { v[i] = __fadd2_rn(v[i], w); });
-    if (scale != nullptr) with(sc, row_of(scale), [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], __fadd2_rn(w, both(1.0f))); });
-    if (shift != nullptr) with(sh, row_of(shift), [&](int i, float2 w) { v[i] = __fadd2_rn(v[i], w); });
+    T* const ph = static_cast<T*>(a.h) + static_cast<size_t>(m) * a.K;
+    m += step;
+    if (k + 1 < rows && m < a.M) fetch(m);  // (after this row's stores: a caller may update the residual in place)
+    if (!norm_h) continue;
+    const float2 s = both(norm_scale<N>(v, has, row, slot + 2, layer, width, a.norm.eps));
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) v[i] = __fmul2_rn(v[i], s);
+    if (a.norm.pre_weight != nullptr) with(pre_w, a.norm.pre_weight, 0, [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], __fadd2_rn(w, off)); });
+    if (a.norm.pre_bias != nullptr) with(pre_b, a.norm.pre_bias, 0, [&](int i, float2 w) { v[i] = __fadd2_rn(v[i], w); });
+    if (kMods && a.norm.scale != nullptr) with(sc, a.norm.scale, mod, [&](int i, float2 w) { v[i] = __fmul2_rn(v[i], __fadd2_rn(w, both(1.0f))); });
+    if (kMods && a.norm.shift != nullptr) with(sh, a.norm.shift, mod, [&](int i, float2 w) { v[i] = __fadd2_rn(v[i], w); });
+    const bool write_h = a.h != nullptr && live;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (!has[i]) continue;
-      store_unit<8>(h == nullptr ? static_cast<T*>(nullptr) : h + channel(i), v + 4 * i);
-      store(k, channel(i), v + 4 * i, live);
+      const uint4 h = pack_unit(v + 4 * i, T());
+      if (write_h) *reinterpret_cast<uint4*>(ph + at[i]) = h;
+      store(k, at[i], h, live);
     }
   }
 }
@@ -547,7 +535,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) quantize_rows_kernel(const Row
 
 // Norm, rotation and quantiser.  A group of a.row_warps warps norms a.group_rows rows into shared memory (as T), one after the
 // other; then the CTA's warps are dealt to the rows anew, K / 32 threads each.
-template <typename R, typename T, int N, int kLayout, int kFmt>
+template <typename R, typename T, int N, bool kPlainNorm, int kLayout, int kFmt>
 __global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const RowsArgs a) {
   using P = Place<kLayout>;
   extern __shared__ __align__(128) uint8_t row_smem[];  // the rows as T; then a line of 128 bytes per thread
@@ -562,12 +550,9 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const Ro
   {
     const RowGroup group(s_red, a.row_warps, g * a.row_warps);
     // (rows of a group lie next to one another)
-    norm_rows<R, T, N>(a, group, j1, m0 + g * a.group_rows, 1, a.group_rows, [&](int k, int channel, const float2* p, bool live) {
+    norm_rows<R, T, N, !kPlainNorm, !kPlainNorm>(a, group, j1, m0 + g * a.group_rows, 1, a.group_rows, [&](int k, int channel, uint4 h, bool live) {
       const int r = g * a.group_rows + k;
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = narrow(p[i], T());
-      *reinterpret_cast<uint4*>(hs + static_cast<size_t>(r) * a.K + channel) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(hs + static_cast<size_t>(r) * a.K + channel) = h;
       if (channel == 0 && live) atomicOr(&s_live, 1u << r);
     });
   }
@@ -591,7 +576,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const Ro
 }
 
 // Norm alone: the CTAs that run at once go through the rows.
-template <typename R, typename T, int N>
+template <typename R, typename T, int N, bool kMods, bool kPost>
 __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const RowsArgs a) {
   __shared__ float s_red[8 * kMaxWarps];
   const int tpg = a.row_warps * 32;
@@ -599,7 +584,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const RowsArgs a)
   const int groups = static_cast<int>(blockDim.x) / tpg, step = static_cast<int>(gridDim.x) * groups;
   const RowGroup group(s_red, a.row_warps, g * a.row_warps);
   const int first = blockIdx.x * groups;  // every group of the CTA makes as many turns
-  norm_rows<R, T, N>(a, group, j, first + g, step, first < a.M ? (a.M - first + step - 1) / step : 0, [](int, int, const float2*, bool) {});
+  norm_rows<R, T, N, kMods, kPost>(a, group, j, first + g, step, first < a.M ? (a.M - first + step - 1) / step : 0, [](int, int, uint4, bool) {});
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
@@ -648,7 +633,7 @@ cudaError_t launch_quantize(RowsArgs a) {
   return start(kern, a, (a.M + rows - 1) / rows, threads, smem);
 }
 
-template <typename R, typename T, int N, int kLayout, int kFmt>
+template <typename R, typename T, int N, bool kPlainNorm, int kLayout, int kFmt>
 cudaError_t launch_norm_quantize(RowsArgs a) {
   a.row_warps = (a.K + N * 256 - 1) / (N * 256);
   const int quant_warps = (a.K + 1023) / 1024;
@@ -658,7 +643,7 @@ cudaError_t launch_norm_quantize(RowsArgs a) {
   while (groups > 1 && (a.M + groups * a.group_rows - 1) / (groups * a.group_rows) < a.num_sms) groups /= 2;
   while (a.group_rows > 1 && (a.M + groups * a.group_rows - 1) / (groups * a.group_rows) < 2 * a.num_sms) a.group_rows /= 2;
   const int threads = groups * a.row_warps * 32, rows = groups * a.group_rows;
-  auto kern = norm_quantize_kernel<R, T, N, kLayout, kFmt>;
+  auto kern = norm_quantize_kernel<R, T, N, kPlainNorm, kLayout, kFmt>;
   const size_t lines = kLayout != kPlain ? static_cast<size_t>(threads) * 128 : 0, kept = static_cast<size_t>(rows) * a.K * sizeof(T);
   const size_t smem = std::max(lines, kept);
   static std::atomic<unsigned long long> raised{0};
@@ -673,20 +658,29 @@ cudaError_t launch_norm_only(RowsArgs a) {
   while (groups > 1 && (a.M + groups - 1) / groups < a.num_sms) groups /= 2;
   const int threads = groups * a.row_warps * 32, blocks = (a.M + groups - 1) / groups;
   const int at_once = a.num_sms * (threads >= 1024 ? 1 : 1024 / threads);
-  return start(norm_kernel<R, T, N>, a, blocks < at_once ? blocks : at_once, threads, 0);
+  const int grid = blocks < at_once ? blocks : at_once;
+  const bool mods = a.norm.gate != nullptr || a.norm.scale != nullptr || a.norm.shift != nullptr, post = a.norm.post_norm != 0;
+  if (mods) return post ? start(norm_kernel<R, T, N, true, true>, a, grid, threads, 0) : start(norm_kernel<R, T, N, true, false>, a, grid, threads, 0);
+  return post ? start(norm_kernel<R, T, N, false, true>, a, grid, threads, 0) : start(norm_kernel<R, T, N, false, false>, a, grid, threads, 0);
+}
+
+template <typename R, typename T, int N, bool kPlainNorm, int kFmt>
+cudaError_t launch_norm_layout(const RowsArgs& a) {
+  if (a.log_b <= 5) return launch_norm_quantize<R, T, N, kPlainNorm, kPlain, kFmt>(a);
+  if (a.log_b <= 7) return launch_norm_quantize<R, T, N, kPlainNorm, kFour, kFmt>(a);
+  switch (a.log_b) {
+    case 8: return launch_norm_quantize<R, T, N, kPlainNorm, 8, kFmt>(a);
+    case 9: return launch_norm_quantize<R, T, N, kPlainNorm, 9, kFmt>(a);
+    case 10: return launch_norm_quantize<R, T, N, kPlainNorm, 10, kFmt>(a);
+    case 11: return launch_norm_quantize<R, T, N, kPlainNorm, 11, kFmt>(a);
+    default: return launch_norm_quantize<R, T, N, kPlainNorm, 12, kFmt>(a);
+  }
 }
 
 template <typename R, typename T, int N, int kFmt>
-cudaError_t launch_norm_layout(const RowsArgs& a) {
-  if (a.log_b <= 5) return launch_norm_quantize<R, T, N, kPlain, kFmt>(a);
-  if (a.log_b <= 7) return launch_norm_quantize<R, T, N, kFour, kFmt>(a);
-  switch (a.log_b) {
-    case 8: return launch_norm_quantize<R, T, N, 8, kFmt>(a);
-    case 9: return launch_norm_quantize<R, T, N, 9, kFmt>(a);
-    case 10: return launch_norm_quantize<R, T, N, 10, kFmt>(a);
-    case 11: return launch_norm_quantize<R, T, N, 11, kFmt>(a);
-    default: return launch_norm_quantize<R, T, N, 12, kFmt>(a);
-  }
+cudaError_t launch_norm_kind(const RowsArgs& a) {
+  const bool plain = a.norm.gate == nullptr && a.norm.scale == nullptr && a.norm.shift == nullptr && a.norm.post_norm == 0;
+  return plain ? launch_norm_layout<R, T, N, true, kFmt>(a) : launch_norm_layout<R, T, N, false, kFmt>(a);
 }
 
 // R: the residual's type, T: everything else's.
@@ -694,10 +688,10 @@ template <typename R, typename T>
 cudaError_t launch_norm(const RowsArgs& a) {
   if (a.K > 8192) {
     if (a.codes == nullptr) return launch_norm_only<R, T, 2>(a);
-    return a.fmt == kMx ? launch_norm_layout<R, T, 2, kMx>(a) : launch_norm_layout<R, T, 2, kNv>(a);
+    return a.fmt == kMx ? launch_norm_kind<R, T, 2, kMx>(a) : launch_norm_kind<R, T, 2, kNv>(a);
   }
   if (a.codes == nullptr) return launch_norm_only<R, T, 1>(a);
-  return a.fmt == kMx ? launch_norm_layout<R, T, 1, kMx>(a) : launch_norm_layout<R, T, 1, kNv>(a);
+  return a.fmt == kMx ? launch_norm_kind<R, T, 1, kMx>(a) : launch_norm_kind<R, T, 1, kNv>(a);
 }
 
 template <typename T, int kFmt>
