@@ -43,6 +43,8 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
   return r;
 }
 
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // The value of a non-negative E4M3 byte: 1.mmm 2^(e - 7), or 0.mmm 2^-6 with e = 0.
 __device__ __forceinline__ float e4m3_value(uint32_t c) {
   if (c == 0x7Fu) return __int_as_float(0x7FC00000);

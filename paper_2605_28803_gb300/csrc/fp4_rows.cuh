@@ -153,8 +153,6 @@ struct Raw {
   }
 };
 
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-
 // v to v - mean with `layer`, and what it then has to be multiplied by: 1 / sqrt(mean v^2 + eps), the variance from the
 // deviations in a second pass over the registers.  A thread without channels adds nothing, whatever it holds.  k: the channels,
 // and their reciprocal.  (IEEE division and square root by every thread took 120 of a row's 430 instructions; the reciprocal square
@@ -351,9 +349,19 @@ struct Place {
   }
 };
 
+template <bool kNamed, int kThreads>
+__device__ __forceinline__ void block_sync() {
+  if constexpr (kNamed) {
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + static_cast<int>(threadIdx.x) / kThreads), "n"(kThreads) : "memory");
+  } else {
+    __syncthreads();
+  }
+}
+
 // Thread j of a row holds v as Place<kLayout> says; `lines` is the row's shared memory.  Leaves codes, block scales and the row's.
-// write: the row and the thread's channels are there.  Every thread of the CTA calls this.
-template <int kLayout, int kFmt>
+// write: the row and the thread's channels are there.  Every thread of the CTA calls this.  kNamed: the CTA has at most 512
+// threads, so that the 64 or 128 of a block of 2048 or 4096 have a barrier of their own.
+template <int kLayout, int kFmt, bool kNamed>
 __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGroup& row, int slot, int j, int m, bool write, uint32_t lines,
                                                 float2 (&v)[16]) {
   if constexpr (kLayout == kFour) {
@@ -383,7 +391,7 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
       const uint32_t at = lines + static_cast<uint32_t>(((j & ~127) + l) * 128 + ((qq ^ l) << 4) + (j & 1) * 8);
 #pragma unroll
       for (int h = 0; h < 16; ++h) sts_half(at + h * 1024, v[h]);
-      __syncthreads();
+      block_sync<kNamed, 128>();
     } else if constexpr (kLayout > 8) {
       using P = Place<kLayout>;
       constexpr int log_c = P::kLogC, keep = P::kKeep;
@@ -400,7 +408,7 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
         sts_quad(block + static_cast<uint32_t>(((u >> keep) * 8 + l) * 128 + ((q ^ l) << 4)), v + 2 * u);
       }
       if constexpr (log_c > 2) {  // a block of 2048 is two warps
-        __syncthreads();
+        block_sync<kNamed, 64>();
       } else {
         __syncwarp();
       }
@@ -428,8 +436,7 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
     if (n > 1) butterflies(v, 1);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float s = v[i].x + v[i].y, d = v[i].x - v[i].y;
-      v[i] = make_float2(s * a.inv_sqrt_b, d * a.inv_sqrt_b);
+      v[i] = __fmul2_rn(make_float2(v[i].x + v[i].y, v[i].x - v[i].y), both(a.inv_sqrt_b));
     }
   }
 
@@ -459,7 +466,7 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
     for (int c = 0; c < 4; ++c) {  // the products are exact
       float2 s[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = make_float2(v[4 * c + i].x * to_codes, v[4 * c + i].y * to_codes);
+      for (int i = 0; i < 4; ++i) s[i] = __fmul2_rn(v[4 * c + i], both(to_codes));
       code[c] = e2m1x8(s[0], s[1], s[2], s[3]);
     }
     // the four threads of a tile's group hand their bytes to the first
@@ -491,8 +498,8 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
         float2 h[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          h[i] = make_float2(v[4 * c + i].x * up, v[4 * c + i].y * up);
-          l[i] = make_float2(v[4 * c + i].x * dn, v[4 * c + i].y * dn);
+          h[i] = __fmul2_rn(v[4 * c + i], both(up));
+          l[i] = __fmul2_rn(v[4 * c + i], both(dn));
         }
         uint32_t w = e2m1x8(h[0], h[1], h[2], h[3]);
         const uint32_t low = e2m1x8(l[0], l[1], l[2], l[3]);
@@ -530,7 +537,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) quantize_rows_kernel(const Row
 #pragma unroll
     for (int u = 0; u < P::kUnits; ++u) load_unit<P::kUnit>(src + place.channel(u), v + u * P::kPer);
   }
-  rotate_quantize<kLayout, kFmt>(a, row, 0, j, m, active, smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128), v);
+  rotate_quantize<kLayout, kFmt, true>(a, row, 0, j, m, active, smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128), v);
 }
 
 // Norm, rotation and quantiser.  A group of a.row_warps warps norms a.group_rows rows into shared memory (as T), one after the
@@ -572,7 +579,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_quantize_kernel(const Ro
     for (int u = 0; u < P::kUnits; ++u) load_unit<P::kUnit>(src + place.channel(u), v + u * P::kPer);
   }
   __syncthreads();  // the rows have been read: their place now takes the rotation's lines
-  rotate_quantize<kLayout, kFmt>(a, row, 0, j, m0 + rloc, active, smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128), v);
+  rotate_quantize<kLayout, kFmt, false>(a, row, 0, j, m0 + rloc, active, smem_u32(row_smem) + static_cast<uint32_t>(rloc * tpr * 128), v);
 }
 
 // Norm alone: the CTAs that run at once go through the rows.
