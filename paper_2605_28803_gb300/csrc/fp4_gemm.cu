@@ -18,7 +18,8 @@
 // the one accumulator that fits); the 268 MB of outputs leave at 2.8 TB/s beside it.
 // Tried and dropped: clusters of two pairs that share the tokens by multicast (102 us to 106: four-CTA clusters leave 8 of the
 // 152 SMs idle, and the loads were not the bound), 16 epilogue warps (101 to 103), a second set of scale columns (the same),
-// output lines of 64 bytes (the same), an evict-first hint on the stores (the same).
+// output lines of 64 bytes (the same), an evict-first hint on the stores (the same), token tiles of even width instead of whole
+// ones and a remainder (816 tokens: 28.3 to 30.3), the gated epilogue without its GELU (0.7 us of 28).
 #include <algorithm>
 #include <atomic>
 
@@ -451,6 +452,7 @@ cudaError_t launch_pair(const Fp4GemmArgs& a) {
   const int tiles = a.K / C::kTileCodes;
   e = make_tmap_bytes(&tx, a.xq, a.M, a.K / 2, kBn / 2);
   if (e == cudaSuccess) e = make_tmap_scales(&txs, a.xs, (a.M + 127) / 128, tiles, C::kTiles, C::kAtoms);
+  static_assert(C::kSmem > 164 * 1024, "no CTA of a cluster of the split kernel beside this one (its launch says why)");
   if (e == cudaSuccess) e = make_tmap_y(&ty, a.y, a.M, kGated ? a.N / 2 : a.N);
   if (e != cudaSuccess) return e;
   PairParams p = {a.xrow, a.wrow, a.bias, a.M, a.N, a.K, (a.M + kBn - 1) / kBn, (a.N + 255) / 256, 0};
@@ -725,7 +727,12 @@ cudaError_t launch_split(const Fp4GemmArgs& a) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(weight_tiles * kSplit, token_tiles);
   cfg.blockDim = dim3(kSThreads);
-  cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * C::kStage + kRecv + 1024;
+  // CTAs that wait for one another must not wait for TMEM too, which a CTA of another stream's kernel could hold while it waits
+  // for one that these keep out: with 64 KB at least, none of them shares an SM with a pair kernel (177 KB and more), and the
+  // three that fit an SM find their columns (128 at most).
+  const size_t smem = static_cast<size_t>(p.stages) * C::kStage + kRecv + 1024;
+  static_assert(C::kTmem <= 128, "three CTAs' columns");
+  cfg.dynamicSmemBytes = kSplit > 1 ? std::max(smem, size_t{64} << 10) : smem;
   cfg.stream = a.stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -224,13 +224,13 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row
     }
   };
   Raw<T, kHold ? N : 1> post_w, pre_w, pre_b;  // the same for every row
+  griddep_wait();  // everything comes from earlier kernels, which may still read what this one writes
+  griddep_launch_dependents();
   if constexpr (kHold) {
     if (kPost && a.norm.post_weight != nullptr) take(post_w, a.norm.post_weight, 0);
     if (a.norm.pre_weight != nullptr) take(pre_w, a.norm.pre_weight, 0);
     if (a.norm.pre_bias != nullptr) take(pre_b, a.norm.pre_bias, 0);
   }
-  griddep_wait();  // rows (and the conditioning) come from earlier kernels, which may still read what this one writes
-  griddep_launch_dependents();
 
   Raw<R, N> r;  // the operands of the row in work, soon those of the next
   Raw<T, N> y;
