@@ -203,6 +203,7 @@ __global__ void __launch_bounds__(kPThreads, 1) fp4_pair_kernel(const __grid_con
       const int n = ta == p.tiles_m - 1 ? p.bn_last : kBn;
       const int token = ta * kBn + static_cast<int>(rank) * (n / 2), row = tb * 256 + static_cast<int>(rank) * 128;
       for (int kb = 0; kb < nkb; kb += C::kKb, ++it) {
+        if (warp == kPTmaW && it == S) griddep_wait();  // (the ring is full until there are tokens)
         if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_empty[s]), ph ^ 1u))) { ok = false; break; }
         const uint32_t full = smem_u32(&bar_full[s]), lead = mapa_shared(full, 0), dst = smem_u32(smem + s * C::kStage);
         if (elect_one()) {
@@ -224,12 +225,14 @@ __global__ void __launch_bounds__(kPThreads, 1) fp4_pair_kernel(const __grid_con
       }
     }
     // before leaving, let every load land: the products that read a stage release it
+    if (warp == kPTmaW && it < S) griddep_wait();
     for (int i = 0; i < S && i < it; ++i) {
       if (--s < 0) { s = S - 1; ph ^= 1u; }
       ok = ok && mbar_wait(smem_u32(&bar_empty[s]), ph);  // (after a time-out nothing will release the rest)
     }
     __syncwarp();
   } else if (warp == kPMma) {
+    griddep_wait();  // (nothing of its own to wait for: it would poll for tokens beside a kernel that is still running)
     if (rank == 0) {
       int s = 0, tile_iter = 0;
       uint32_t ph = 0;
@@ -436,6 +439,7 @@ cudaError_t raise_smem(const void* kern, int bytes, std::atomic<unsigned long lo
   const unsigned long long bit = 1ull << (dev & 63);
   if (done->load() & bit) return cudaSuccess;
   e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
   if (e == cudaSuccess) done->fetch_or(bit);
   return e;
 }
@@ -580,6 +584,7 @@ __global__ void __launch_bounds__(kSThreads, 1) fp4_split_kernel(const __grid_co
     for (int i = max(0, it - S); i < it; ++i) mbar_wait(smem_u32(&bar_full[i % S]), static_cast<uint32_t>(i / S) & 1u);
     __syncwarp();
   } else if (warp == kSMma) {
+    griddep_wait();  // (it would only poll)
     const int tokens = min(p.M - ta * kBn, kBn);
     const uint32_t idesc = idesc_e2m1_f32(kFmt, 128, (tokens + 15) / 16 * 16);
     // The address of scales in TMEM has to be even (an odd one is a misaligned address): tiles of 32 tokens begin at token 0.
