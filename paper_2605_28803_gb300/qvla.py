@@ -101,6 +101,8 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
 
 _lib = load_library()
 
+from . import _calls  # noqa: E402  (linked against libqvla.so, whose absence is reported above)
+
 
 def lib() -> ctypes.CDLL:
     return _lib
@@ -388,31 +390,19 @@ def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, b
         _check(status)
 
 
-# 4-bit floating point and the norms around a block.  The calls of a step marshal their arguments inline, as above: what is
-# optional is None or a tensor, a stream None, an address or a torch stream.
+# 4-bit floating point and the norms around a block.  The calls of a step come compiled (csrc/calls.c), as they cost no more than
+# their launch otherwise: what is optional is None or a tensor, a stream None, an address or a torch stream.
+_calls.set_check(_check)
+qvla_fp4_quantize_rows = _calls.qvla_fp4_quantize_rows
+qvla_fp4_dequantize_rows = _calls.qvla_fp4_dequantize_rows
+qvla_gemm_fp4 = _calls.qvla_gemm_fp4
+qvla_fp4_linear = _calls.qvla_fp4_linear
+qvla_block_norm = _calls.qvla_block_norm
+qvla_block_norm_fp4 = _calls.qvla_block_norm_fp4
+
 
 def qvla_fp4_scale_bytes(fmt: int, rows: int, K: int) -> int:
     return int(_lib.qvla_fp4_scale_bytes(fmt, rows, K))
-
-
-def qvla_fp4_quantize_rows(x, xdt: int, x_stride: int, M: int, K: int, had_block: int, fmt: int, step_scale, xq, xs, xscale=None,
-                           stream=None) -> None:
-    """Rotate and quantise rows to E2M1 codes and block scales (NVFP4: and a float32 scale a row)."""
-    status = _lib.qvla_fp4_quantize_rows(x.data_ptr(), xdt, x_stride, M, K, had_block, fmt,
-                                         None if step_scale is None else step_scale.data_ptr(), xq.data_ptr(), xs.data_ptr(),
-                                         None if xscale is None else xscale.data_ptr(),
-                                         None if stream is None else stream if type(stream) is int else stream.cuda_stream)
-    if status:
-        _check(status)
-
-
-def qvla_fp4_dequantize_rows(xq, xs, xscale, fmt: int, M: int, K: int, out, odt: int, stream=None) -> None:
-    """What the codes stand for, in the rotated basis."""
-    status = _lib.qvla_fp4_dequantize_rows(xq.data_ptr(), xs.data_ptr(), None if xscale is None else xscale.data_ptr(), fmt, M,
-                                           K, out.data_ptr(), odt,
-                                           None if stream is None else stream if type(stream) is int else stream.cuda_stream)
-    if status:
-        _check(status)
 
 
 def qvla_fp4_pack_weights_host(W: np.ndarray, wdt: int, N: int, K: int, rot=None, rot_block: int = 0, perm=None,
@@ -458,23 +448,8 @@ def qvla_fp4_layer_create_gated(H: int, K: int, had_block: int, fmt: int, xdt: i
     return _fp4_layer(_lib.qvla_fp4_layer_create_gated, H, K, had_block, fmt, xdt, ydt, wq, ws, wscale, bias, True)
 
 
-def qvla_gemm_fp4(layer: Fp4Layer, xq, xs, xscale, M: int, y, stream=None) -> None:
-    status = _lib.qvla_gemm_fp4(layer.handle, xq.data_ptr(), xs.data_ptr(), None if xscale is None else xscale.data_ptr(), M,
-                                y.data_ptr(), None if stream is None else stream if type(stream) is int else stream.cuda_stream)
-    if status:
-        _check(status)
-
-
 def qvla_fp4_linear_workspace_bytes(layer: Fp4Layer, M: int) -> int:
     return int(_lib.qvla_fp4_linear_workspace_bytes(layer.handle, M))
-
-
-def qvla_fp4_linear(layer: Fp4Layer, x, M: int, step_scale, y, workspace, workspace_bytes: int, stream=None) -> None:
-    status = _lib.qvla_fp4_linear(layer.handle, x.data_ptr(), M, None if step_scale is None else step_scale.data_ptr(),
-                                  y.data_ptr(), None if workspace is None else workspace.data_ptr(), workspace_bytes,
-                                  None if stream is None else stream if type(stream) is int else stream.cuda_stream)
-    if status:
-        _check(status)
 
 
 class _NormStruct(ctypes.Structure):
@@ -503,29 +478,6 @@ class BlockNorm:
         self.struct = _NormStruct(kind, eps, weight_offset, residual_scale, 1 if post_norm else 0, _ptr(post_weight), _ptr(pre_weight),
                                   _ptr(pre_bias), _ptr(gate), _ptr(scale), _ptr(shift), stride, rows, mod_tokens, _ptr(mod_index))
         self.ref = ctypes.addressof(self.struct)
-
-
-def qvla_block_norm(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: int, M: int, K: int, r_out, h, stream=None) -> None:
-    """Residual + gated branch, then the norm; y, r_out or h may be None as in include/qvla.h."""
-    status = _lib.qvla_block_norm(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, None if y is None else y.data_ptr(),
-                                  y_stride, M, K, None if r_out is None else r_out.data_ptr(),
-                                  None if h is None else h.data_ptr(),
-                                  None if stream is None else stream if type(stream) is int else stream.cuda_stream)
-    if status:
-        _check(status)
-
-
-def qvla_block_norm_fp4(norm: BlockNorm, r, rdt: int, r_stride: int, y, y_stride: int, M: int, K: int, r_out, h, had_block: int,
-                        fmt: int, step_scale, hq, hs, hscale=None, stream=None) -> None:
-    """The same with its output rotated and quantised."""
-    status = _lib.qvla_block_norm_fp4(norm.ref, norm.dt, r.data_ptr(), rdt, r_stride, None if y is None else y.data_ptr(),
-                                      y_stride, M, K, None if r_out is None else r_out.data_ptr(),
-                                      None if h is None else h.data_ptr(), had_block, fmt,
-                                      None if step_scale is None else step_scale.data_ptr(), hq.data_ptr(), hs.data_ptr(),
-                                      None if hscale is None else hscale.data_ptr(),
-                                      None if stream is None else stream if type(stream) is int else stream.cuda_stream)
-    if status:
-        _check(status)
 
 
 def qvla_check_device(stream=None) -> None:

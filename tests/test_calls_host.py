@@ -1,0 +1,73 @@
+"""The compiled part of the binding: how it takes its arguments, and that it keeps no reference to them."""
+import sys
+
+import numpy as np
+import pytest
+
+from paper_2605_28803_gb300 import qvla
+
+CALLS = ["qvla_fp4_quantize_rows", "qvla_fp4_dequantize_rows", "qvla_gemm_fp4", "qvla_fp4_linear", "qvla_block_norm", "qvla_block_norm_fp4"]
+
+
+class Address:
+    """Stands for a tensor: an address that the refused calls below never read."""
+
+    def __init__(self, value=1 << 20):
+        self.value = value
+
+    def data_ptr(self):
+        return self.value
+
+
+def rows(**changes):
+    args = dict(x=Address(), xdt=qvla.BF16, x_stride=128, M=1, K=128, had_block=1, fmt=qvla.MXFP4, step_scale=None, xq=Address(), xs=Address())
+    args.update(changes)
+    return args
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_a_call_without_arguments_names_the_first_missing_one(call):
+    with pytest.raises(TypeError, match=f"{call}\\(\\) needs the argument"):
+        getattr(qvla, call)()
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_too_many_unknown_and_repeated_arguments(call):
+    f = getattr(qvla, call)
+    with pytest.raises(TypeError, match="arguments but 40 were given"):
+        f(*[None] * 40)
+    with pytest.raises(TypeError, match="no argument 'nonsense'"):
+        f(nonsense=1)
+    with pytest.raises(TypeError, match="two values for argument"):
+        first = f.__text_signature__.strip("()").split(",")[0]
+        f(None, **{first: None})
+
+
+@pytest.mark.parametrize("changes, error", [
+    (dict(M="1"), TypeError), (dict(M=1.0), TypeError), (dict(M=1 << 31), OverflowError), (dict(K=-(1 << 31) - 1), OverflowError),
+    (dict(x_stride=1 << 63), OverflowError), (dict(x=3), AttributeError), (dict(x=Address("text")), TypeError), (dict(stream="s"), AttributeError),
+    (dict(xscale=Address(1 << 70)), OverflowError)])
+def test_arguments_of_the_wrong_kind(changes, error):
+    with pytest.raises(error):
+        qvla.qvla_fp4_quantize_rows(**rows(**changes))
+
+
+def test_the_librarys_own_refusals_arrive_as_its_errors():
+    with pytest.raises(qvla.QvlaError):
+        qvla.qvla_fp4_quantize_rows(**rows(K=63))
+    with pytest.raises(qvla.QvlaError):
+        qvla.qvla_fp4_quantize_rows(**rows(x=None))
+    qvla.qvla_fp4_quantize_rows(**rows(M=np.int64(0), K=np.int32(128), x_stride=np.int64(128)))  # no rows: nothing is launched
+
+
+def test_no_reference_is_kept():
+    x, stride = Address(), 123456789
+    before = sys.getrefcount(x), sys.getrefcount(stride)
+    for _ in range(100):
+        with pytest.raises(qvla.QvlaError):
+            qvla.qvla_fp4_quantize_rows(**rows(x=x, xs=x, K=63, x_stride=stride))
+        with pytest.raises(TypeError):
+            qvla.qvla_fp4_quantize_rows(x, nonsense=x)
+        with pytest.raises(TypeError):
+            qvla.qvla_fp4_quantize_rows(**rows(x=x, M="1"))
+    assert (sys.getrefcount(x), sys.getrefcount(stride)) == before
