@@ -9,8 +9,8 @@
 
 #include "../../include/qvla.h"
 
-static PyObject *s_data_ptr, *s_cuda_stream, *s_handle, *s_address, *s_dt; /* interned names */
-static PyObject* g_check; /* callable(status): raises */
+static PyObject *s_data_ptr, *s_cuda_stream, *s_handle, *s_address, *s_dt, *s_width, *s_tokens; /* interned names */
+static PyObject *g_check, *g_layer, *g_norm; /* callable(status): raises; the types Fp4Layer and BlockNorm */
 
 /* Positional and keyword arguments into slots; the last `optional` of n may be left out (None). */
 static int take(const char* call, const char* const* names, int n, int optional, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames,
@@ -80,6 +80,40 @@ static int get_size(PyObject* o, size_t* out) {
   return *out == (size_t)-1 && PyErr_Occurred() ? -1 : 0;
 }
 
+/* A layer's handle (a handle of another kind would be read as one). */
+static int get_layer(PyObject* o, void** out) {
+  if (!PyObject_TypeCheck(o, (PyTypeObject*)g_layer)) {
+    PyErr_Format(PyExc_TypeError, "an Fp4Layer is needed, not %s", Py_TYPE(o)->tp_name);
+    return -1;
+  }
+  return get_pointer(o, s_handle, 0, out);
+}
+static int get_attribute_int(PyObject* o, PyObject* name, int* out) {
+  PyObject* const v = PyObject_GetAttr(o, name);
+  int bad;
+  if (!v) return -1;
+  bad = get_int(v, out);
+  Py_DECREF(v);
+  return bad;
+}
+/* A norm's parameters and type, and whether its vectors and index reach over the call's M rows of K. */
+static int get_norm(PyObject* o, PyObject* rows, PyObject* channels, void** out, int* dt, int* M, int* K) {
+  int width, tokens;
+  if (!PyObject_TypeCheck(o, (PyTypeObject*)g_norm)) {
+    PyErr_Format(PyExc_TypeError, "a BlockNorm is needed, not %s", Py_TYPE(o)->tp_name);
+    return -1;
+  }
+  if (get_int(rows, M) || get_int(channels, K) || get_pointer(o, s_address, 0, out) || get_attribute_int(o, s_dt, dt) ||
+      get_attribute_int(o, s_width, &width) || get_attribute_int(o, s_tokens, &tokens))
+    return -1;
+  if (*K > width || *M > tokens) {
+    PyErr_Format(PyExc_ValueError, *K > width ? "the norm's vectors have %d channels, the call %d" : "mod_index has %d tokens, the call %d",
+                 *K > width ? width : tokens, *K > width ? *K : *M);
+    return -1;
+  }
+  return 0;
+}
+
 static PyObject* result(qvla_status s) {
   if (s == QVLA_OK) Py_RETURN_NONE;
   return PyObject_CallFunction(g_check, "i", (int)s);
@@ -124,7 +158,7 @@ static PyObject* gemm(PyObject* self, PyObject* const* args, Py_ssize_t nargs, P
   void *layer, *xq, *xs, *xscale, *y, *stream;
   int M;
   TAKE("qvla_gemm_fp4", 7, 1);
-  if (get_pointer(a[0], s_handle, 0, &layer) || get_tensor(a[1], &xq) || get_tensor(a[2], &xs) || get_tensor(a[3], &xscale) || get_int(a[4], &M) ||
+  if (get_layer(a[0], &layer) || get_tensor(a[1], &xq) || get_tensor(a[2], &xs) || get_tensor(a[3], &xscale) || get_int(a[4], &M) ||
       get_tensor(a[5], &y) || get_stream(a[6], &stream))
     return NULL;
   CALL(qvla_gemm_fp4(layer, xq, xs, xscale, M, y, stream));
@@ -136,7 +170,7 @@ static PyObject* linear(PyObject* self, PyObject* const* args, Py_ssize_t nargs,
   int M;
   size_t bytes;
   TAKE("qvla_fp4_linear", 8, 1);
-  if (get_pointer(a[0], s_handle, 0, &layer) || get_tensor(a[1], &x) || get_int(a[2], &M) || get_tensor(a[3], &step) || get_tensor(a[4], &y) ||
+  if (get_layer(a[0], &layer) || get_tensor(a[1], &x) || get_int(a[2], &M) || get_tensor(a[3], &step) || get_tensor(a[4], &y) ||
       get_tensor(a[5], &work) || get_size(a[6], &bytes) || get_stream(a[7], &stream))
     return NULL;
   CALL(qvla_fp4_linear(layer, x, M, step, y, work, bytes, stream));
@@ -145,15 +179,11 @@ static PyObject* linear(PyObject* self, PyObject* const* args, Py_ssize_t nargs,
 static PyObject* block_norm(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
   static const char* const names[] = {"norm", "r", "rdt", "r_stride", "y", "y_stride", "M", "K", "r_out", "h", "stream"};
   void *norm, *r, *y, *r_out, *h, *stream;
-  PyObject* dtype;
-  int dt, rdt, M, K, bad;
+  int dt, rdt, M, K;
   int64_t r_stride, y_stride;
   TAKE("qvla_block_norm", 11, 1);
-  if (get_pointer(a[0], s_address, 0, &norm) || !(dtype = PyObject_GetAttr(a[0], s_dt))) return NULL;
-  bad = get_int(dtype, &dt);
-  Py_DECREF(dtype);
-  if (bad || get_tensor(a[1], &r) || get_int(a[2], &rdt) || get_int64(a[3], &r_stride) || get_tensor(a[4], &y) || get_int64(a[5], &y_stride) ||
-      get_int(a[6], &M) || get_int(a[7], &K) || get_tensor(a[8], &r_out) || get_tensor(a[9], &h) || get_stream(a[10], &stream))
+  if (get_norm(a[0], a[6], a[7], &norm, &dt, &M, &K) || get_tensor(a[1], &r) || get_int(a[2], &rdt) || get_int64(a[3], &r_stride) || get_tensor(a[4], &y) || get_int64(a[5], &y_stride) ||
+      get_tensor(a[8], &r_out) || get_tensor(a[9], &h) || get_stream(a[10], &stream))
     return NULL;
   CALL(qvla_block_norm(norm, (qvla_dtype)dt, r, (qvla_dtype)rdt, r_stride, y, y_stride, M, K, r_out, h, stream));
 }
@@ -162,24 +192,26 @@ static PyObject* block_norm_fp4(PyObject* self, PyObject* const* args, Py_ssize_
   static const char* const names[] = {"norm", "r", "rdt", "r_stride", "y", "y_stride", "M", "K", "r_out", "h", "had_block", "fmt", "step_scale", "hq", "hs",
                                       "hscale", "stream"};
   void *norm, *r, *y, *r_out, *h, *step, *hq, *hs, *hscale, *stream;
-  PyObject* dtype;
-  int dt, rdt, M, K, had, fmt, bad;
+  int dt, rdt, M, K, had, fmt;
   int64_t r_stride, y_stride;
   TAKE("qvla_block_norm_fp4", 17, 2);
-  if (get_pointer(a[0], s_address, 0, &norm) || !(dtype = PyObject_GetAttr(a[0], s_dt))) return NULL;
-  bad = get_int(dtype, &dt);
-  Py_DECREF(dtype);
-  if (bad || get_tensor(a[1], &r) || get_int(a[2], &rdt) || get_int64(a[3], &r_stride) || get_tensor(a[4], &y) || get_int64(a[5], &y_stride) ||
-      get_int(a[6], &M) || get_int(a[7], &K) || get_tensor(a[8], &r_out) || get_tensor(a[9], &h) || get_int(a[10], &had) || get_int(a[11], &fmt) ||
+  if (get_norm(a[0], a[6], a[7], &norm, &dt, &M, &K) || get_tensor(a[1], &r) || get_int(a[2], &rdt) || get_int64(a[3], &r_stride) || get_tensor(a[4], &y) || get_int64(a[5], &y_stride) ||
+      get_tensor(a[8], &r_out) || get_tensor(a[9], &h) || get_int(a[10], &had) || get_int(a[11], &fmt) ||
       get_tensor(a[12], &step) || get_tensor(a[13], &hq) || get_tensor(a[14], &hs) || get_tensor(a[15], &hscale) || get_stream(a[16], &stream))
     return NULL;
   CALL(qvla_block_norm_fp4(norm, (qvla_dtype)dt, r, (qvla_dtype)rdt, r_stride, y, y_stride, M, K, r_out, h, had, (qvla_fp4_format)fmt, step, hq, hs, hscale,
                            stream));
 }
 
-static PyObject* set_check(PyObject* self, PyObject* callable) {
-  Py_INCREF(callable);
-  Py_XSETREF(g_check, callable);
+static PyObject* setup(PyObject* self, PyObject* args) {
+  PyObject *check, *layer, *norm;
+  if (!PyArg_ParseTuple(args, "OO!O!", &check, &PyType_Type, &layer, &PyType_Type, &norm)) return NULL;
+  Py_INCREF(check);
+  Py_INCREF(layer);
+  Py_INCREF(norm);
+  Py_XSETREF(g_check, check);
+  Py_XSETREF(g_layer, layer);
+  Py_XSETREF(g_norm, norm);
   Py_RETURN_NONE;
 }
 
@@ -198,7 +230,7 @@ static PyMethodDef methods[] = {
     METHOD("qvla_block_norm_fp4", block_norm_fp4,
            "(norm, r, rdt, r_stride, y, y_stride, M, K, r_out, h, had_block, fmt, step_scale, hq, hs, hscale=None, stream=None)",
            "The same with its output rotated and quantised."),
-    {"set_check", set_check, METH_O, "The callable that turns a non-zero status into an exception."},
+    {"setup", setup, METH_VARARGS, "The callable that turns a non-zero status into an exception, and the types of layers and norms; ahead of any call."},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "libqvla's calls of a served step.", -1, methods, NULL, NULL, NULL, NULL};
@@ -209,6 +241,8 @@ PyMODINIT_FUNC PyInit__calls(void) {
   s_handle = PyUnicode_InternFromString("handle");
   s_address = PyUnicode_InternFromString("ref");
   s_dt = PyUnicode_InternFromString("dt");
-  if (!s_data_ptr || !s_cuda_stream || !s_handle || !s_address || !s_dt) return NULL;
+  s_width = PyUnicode_InternFromString("width");
+  s_tokens = PyUnicode_InternFromString("tokens");
+  if (!s_data_ptr || !s_cuda_stream || !s_handle || !s_address || !s_dt || !s_width || !s_tokens) return NULL;
   return PyModule_Create(&module);
 }

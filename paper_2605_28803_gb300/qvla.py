@@ -392,7 +392,6 @@ def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, b
 
 # 4-bit floating point and the norms around a block.  The calls of a step come compiled (csrc/calls.c), as they cost no more than
 # their launch otherwise: what is optional is None or a tensor, a stream None, an address or a torch stream.
-_calls.set_check(_check)
 qvla_fp4_quantize_rows = _calls.qvla_fp4_quantize_rows
 qvla_fp4_dequantize_rows = _calls.qvla_fp4_dequantize_rows
 qvla_gemm_fp4 = _calls.qvla_gemm_fp4
@@ -458,12 +457,16 @@ class _NormStruct(ctypes.Structure):
                 ("mod_stride", _L), ("mod_rows", _I), ("mod_tokens", _I), ("mod_index", _P)]
 
 
+_NORM_DTYPES = {"torch.float16": F16, "torch.bfloat16": BF16}
+
+
 class BlockNorm:
     """The norms, gate and modulation of one place between two blocks (qvla_block_norm_params), of type dt.  gate, scale and
     shift are 2-D tensors of the same rows and row stride (slices of one conditioning output, say) or None; token m takes row
-    m // mod_tokens, or mod_index[m] (int32).  The tensors are kept alive and read at each call."""
+    m // mod_tokens, or mod_index[m] (int32).  The tensors are kept alive and read at each call, whose K and M may not exceed
+    ``width`` and ``tokens``, the channels and the indices that there are."""
 
-    __slots__ = ("dt", "tensors", "struct", "ref")
+    __slots__ = ("dt", "tensors", "struct", "ref", "width", "tokens")
 
     def __init__(self, kind: int, dt: int, eps: float = 1e-6, weight_offset: float = 0.0, residual_scale: float = 1.0,
                  post_norm: bool = False, post_weight=None, pre_weight=None, pre_bias=None, gate=None, scale=None, shift=None,
@@ -471,13 +474,25 @@ class BlockNorm:
         mods = [t for t in (gate, scale, shift) if t is not None]
         if any(t.dim() != 2 or t.stride(1) != 1 or t.shape != mods[0].shape or t.stride(0) != mods[0].stride(0) for t in mods):
             raise ValueError("gate, scale and shift must be 2-D with the same rows, row stride and contiguous channels")
+        vectors = [t for t in (post_weight, pre_weight, pre_bias) if t is not None]
+        if any(t.dim() != 1 or not t.is_contiguous() for t in vectors):
+            raise ValueError("the weights and the bias must be 1-D and contiguous")
+        if any(_NORM_DTYPES.get(str(t.dtype)) != dt for t in vectors + mods):
+            raise ValueError("weights, bias, gate, scale and shift must have the norm's type")
+        if mod_index is not None and (mod_index.dim() != 1 or not mod_index.is_contiguous() or str(mod_index.dtype) != "torch.int32"):
+            raise ValueError("mod_index must be 1-D, contiguous and int32")
         self.dt = dt
+        self.width = min((t.shape[-1] for t in vectors + mods), default=(1 << 31) - 1)
+        self.tokens = (1 << 31) - 1 if mod_index is None else mod_index.shape[0]
         self.tensors = (post_weight, pre_weight, pre_bias, gate, scale, shift, mod_index)
         rows = mods[0].shape[0] if mods else 0
         stride = (mods[0].stride(0) if rows > 1 else max(mods[0].stride(0), mods[0].shape[1])) if mods else 0
         self.struct = _NormStruct(kind, eps, weight_offset, residual_scale, 1 if post_norm else 0, _ptr(post_weight), _ptr(pre_weight),
                                   _ptr(pre_bias), _ptr(gate), _ptr(scale), _ptr(shift), stride, rows, mod_tokens, _ptr(mod_index))
         self.ref = ctypes.addressof(self.struct)
+
+
+_calls.setup(_check, Fp4Layer, BlockNorm)
 
 
 def qvla_check_device(stream=None) -> None:

@@ -71,3 +71,51 @@ def test_no_reference_is_kept():
         with pytest.raises(TypeError):
             qvla.qvla_fp4_quantize_rows(**rows(x=x, M="1"))
     assert (sys.getrefcount(x), sys.getrefcount(stride)) == before
+
+
+def norm(**vectors):
+    return qvla.BlockNorm(qvla.NORM_RMS, qvla.BF16, **vectors)
+
+
+def junction(n, K=128, M=0):
+    """Without rows nothing is launched."""
+    qvla.qvla_block_norm(n, Address(), qvla.BF16, K, None, 0, M, K, None, Address())
+    qvla.qvla_block_norm_fp4(n, Address(), qvla.BF16, K, None, 0, M, K, None, None, 1, qvla.MXFP4, None, Address(), Address())
+
+
+def test_norms_whose_vectors_do_not_fit():
+    torch = pytest.importorskip("torch")
+
+    def t(*shape, dtype=torch.bfloat16):
+        return torch.zeros(*shape, dtype=dtype)
+
+    junction(norm(post_norm=True, post_weight=t(128), pre_weight=t(128), pre_bias=t(256), gate=t(2, 128), mod_tokens=1))
+    for vectors in (dict(pre_weight=t(64)), dict(pre_weight=t(128), pre_bias=t(120)), dict(post_norm=True, post_weight=t(127)), dict(scale=t(2, 64), mod_tokens=1)):
+        with pytest.raises(ValueError, match="channels"):
+            junction(norm(**vectors))
+    index = dict(gate=t(2, 128), mod_index=t(5, dtype=torch.int32))
+    junction(norm(**index))
+    for call, args in ((qvla.qvla_block_norm, (None, Address())),
+                       (qvla.qvla_block_norm_fp4, (None, None, 1, qvla.MXFP4, None, Address(), Address()))):
+        with pytest.raises(ValueError, match="mod_index has 5 tokens, the call 6"):
+            call(norm(**index), Address(), qvla.BF16, 128, None, 0, 6, 128, *args)
+    for vectors in (dict(pre_weight=t(128, dtype=torch.float32)), dict(pre_bias=t(128, dtype=torch.float16)), dict(pre_weight=t(1, 128)),
+                    dict(pre_weight=t(256)[::2]), dict(gate=t(2, 128, dtype=torch.float32)), dict(gate=t(2, 128), mod_index=t(5, dtype=torch.int64)),
+                    dict(gate=t(2, 128), mod_index=t(10, dtype=torch.int32)[::2])):
+        with pytest.raises(ValueError):
+            norm(**vectors)
+
+
+def test_objects_of_another_kind():
+    class Handle:
+        handle, ref, dt, width, tokens = 1 << 20, 1 << 20, 0, 1 << 20, 1 << 20
+
+    for call, args in ((qvla.qvla_gemm_fp4, (Address(), Address(), None, 1, Address())), (qvla.qvla_fp4_linear, (Address(), 1, None, Address(), Address(), 0))):
+        for other in (Handle(), None, 1 << 20):
+            with pytest.raises(TypeError, match="an Fp4Layer is needed"):
+                call(other, *args)
+    with pytest.raises(TypeError, match="a BlockNorm is needed"):
+        junction(Handle())
+    closed = qvla.Fp4Layer(None, 128, 128, 1, qvla.MXFP4, qvla.BF16, qvla.BF16, False)
+    with pytest.raises(qvla.QvlaError, match="layer must not be NULL"):
+        qvla.qvla_gemm_fp4(closed, Address(), Address(), None, 1, Address())
