@@ -7,8 +7,8 @@ namespace qvla {
 namespace {
 
 template <typename T, int kFmt>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                         const float* __restrict__ row_scale, int M, int K, T* __restrict__ out) {
+__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* codes, const uint8_t* scales, const float* row_scale, int M, int K,
+                                                         T* out) {
   const int chunks = (K + 1023) / 1024;  // of a row, one to a warp
   const int w = static_cast<int>(blockIdx.x) * 8 + static_cast<int>(threadIdx.x >> 5), m = w / chunks;
   const int first = (w - m * chunks) * 128 + static_cast<int>(threadIdx.x & 31);  // this thread's words of 8 codes: 32 apart

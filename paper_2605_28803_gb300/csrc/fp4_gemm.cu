@@ -456,7 +456,7 @@ cudaError_t launch_pair(const Fp4GemmArgs& a) {
   const int tiles = a.K / C::kTileCodes;
   e = make_tmap_bytes(&tx, a.xq, a.M, a.K / 2, kBn / 2);
   if (e == cudaSuccess) e = make_tmap_scales(&txs, a.xs, (a.M + 127) / 128, tiles, C::kTiles, C::kAtoms);
-  static_assert(C::kSmem > 164 * 1024, "no CTA of a cluster of the split kernel beside this one (its launch says why)");
+  static_assert(C::kSmem >= 161 * 1024, "no CTA of a cluster of the split kernel beside this one (its launch says why)");
   if (e == cudaSuccess) e = make_tmap_y(&ty, a.y, a.M, kGated ? a.N / 2 : a.N);
   if (e != cudaSuccess) return e;
   PairParams p = {a.xrow, a.wrow, a.bias, a.M, a.N, a.K, (a.M + kBn - 1) / kBn, (a.N + 255) / 256, 0};
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(kSThreads, 1) fp4_split_kernel(const __grid_co
     const int n = tb * 128 + warp * 32 + lane;  // this thread's weight row
     const int nc = min(n, p.N - 1);
     const float ws = __ldg(p.wrow + nc), bs = __ldg(p.bias + nc);
-    griddep_wait();  // xrow comes from the previous kernel, which may still read y
+    griddep_wait();  // xrow comes from the previous kernel (so no read-only load of it), which may still read y
     const int m0 = ta * kBn + rank * kKeep;  // the first token that this CTA keeps
     const int row = warp * 32 + lane;
     bool done = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_done), 0) && *const_cast<volatile int*>(&s_abort) == 0);
@@ -689,7 +689,7 @@ __global__ void __launch_bounds__(kSThreads, 1) fp4_split_kernel(const __grid_co
 #pragma unroll
       for (int i = 0; i < kChunk; ++i) {
         const int m = m0 + c0 + i;
-        const float xs = kFmt == fp4::kMx ? 1.0f : __ldg(p.xrow + min(m, p.M - 1));
+        const float xs = kFmt == fp4::kMx ? 1.0f : p.xrow[min(m, p.M - 1)];
         float a = fmaf(v[i], xs * ws, bs);
         if constexpr (kGated) a = gelu_fast(a) * __shfl_down_sync(0xffffffffu, a, 16);
         if (store && m < p.M) {
@@ -733,11 +733,11 @@ cudaError_t launch_split(const Fp4GemmArgs& a) {
   cfg.gridDim = dim3(weight_tiles * kSplit, token_tiles);
   cfg.blockDim = dim3(kSThreads);
   // CTAs that wait for one another must not wait for TMEM too, which a CTA of another stream's kernel could hold while it waits
-  // for one that these keep out: with 64 KB at least, none of them shares an SM with a pair kernel (177 KB and more), and the
-  // three that fit an SM find their columns (128 at most).
+  // for one that these keep out: with 68 KB at least, none of them shares an SM with a kernel that takes all columns (the least
+  // of them the prompt attention's of 64 channels, 161 KB), and the three that fit an SM find theirs (128 at most).
   const size_t smem = static_cast<size_t>(p.stages) * C::kStage + kRecv + 1024;
   static_assert(C::kTmem <= 128, "three CTAs' columns");
-  cfg.dynamicSmemBytes = kSplit > 1 ? std::max(smem, size_t{64} << 10) : smem;
+  cfg.dynamicSmemBytes = kSplit > 1 ? std::max(smem, size_t{68} << 10) : smem;
   cfg.stream = a.stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -477,7 +477,7 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
   } else {
     float delta;
     if (a.step_scale != nullptr) {
-      delta = __ldg(a.step_scale);
+      delta = *a.step_scale;
     } else {
       delta = __fdiv_rn(row.max(rq::max_nan(top[0], top[1]), slot), kRowMax);
       if (isinf(delta)) delta = __int_as_float(0x7FC00000);
