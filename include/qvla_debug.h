@@ -24,8 +24,9 @@ extern "C" {
  *                   cluster) then sends nothing between its CTAs (no row maximum, no partial
  *                   sum), and neither do the passes of a row in the few-row rotate-quantise
  *                   kernel (no row maximum, no code sum), so their receiving waits run out the
- *                   same way.  The prompt attention then issues no copy either and leaves o
- *                   unwritten.  0 restores normal operation.
+ *                   same way.  The prompt attention and the products of 4-bit floating point
+ *                   then issue no copy either and leave their outputs unwritten.  0 restores
+ *                   normal operation.
  * Synchronises the device first; affects every later launch on the current device until called
  * again. */
 qvla_status qvla_debug_set_hooks(unsigned long long wait_limit_ns, int hold_gemm_loads);
