@@ -552,7 +552,8 @@ qvla_status qvla_gemm_fp4(const qvla_fp4_layer* layer, const uint8_t* xq, const 
 size_t qvla_fp4_linear_workspace_bytes(const qvla_fp4_layer* layer, int M);
 
 /* The whole linear: the layer's rotation and quantiser on x (device [M][K] of xdt, dense), then the product.  step_scale as
- * in qvla_fp4_quantize_rows; workspace as in qvla_w4a4_linear. */
+ * in qvla_fp4_quantize_rows; workspace as in qvla_w4a4_linear.  y may overlap x.  Up to 4 tokens are one launch where x has y's type
+ * and does not overlap it, and the workspace may then be left as it was. */
 qvla_status qvla_fp4_linear(const qvla_fp4_layer* layer, const void* x, int M, const float* step_scale, void* y,
                             void* workspace, size_t workspace_bytes, void* stream);
 

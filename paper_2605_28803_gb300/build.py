@@ -23,7 +23,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 SOURCES = ["rotate_quant_f16.cu", "rotate_quant_bf16.cu", "rotate_quant_f32.cu", "rotate_quant_wide.cu", "rotate_quant_wide_f32.cu", "rotate_quant_a8_f16.cu",
            "rotate_quant_a8_bf16.cu", "rotate_quant_a8_f32.cu", "rotate_quant.cu", "rotate_quant_pass.cu", "a8_planes.cu", "block_rotate.cu", "gemm.cu", "gemm_tmem.cu", "gemm_fused.cu", "gemv.cu", "attention_prompt.cu", "attention_kv4.cu", "kv4_cache.cu", "api.cu", "api_attention.cu",
-           "fp4_rows_f16.cu", "fp4_rows_bf16.cu", "fp4_rows_f32.cu", "norm_f16.cu", "norm_bf16.cu", "fp4_dequantize.cu", "fp4_gemm.cu", "api_fp4.cu",
+           "fp4_rows_f16.cu", "fp4_rows_bf16.cu", "fp4_rows_f32.cu", "norm_f16.cu", "norm_bf16.cu", "fp4_dequantize.cu", "fp4_gemm.cu", "fp4_token.cu", "api_fp4.cu",
            "pack.cpp"]
 
 

@@ -1016,6 +1016,7 @@ qvla_status qvla_debug_set_hooks(unsigned long long wait_limit_ns, int hold_gemm
   QVLA_CUDA(qvla::set_debug_hooks_rqp(limit, hold), "test hooks (rotate-quantise)");
   QVLA_CUDA(qvla::set_debug_hooks_prompt(limit, hold), "test hooks (prompt attention)");
   QVLA_CUDA(qvla::set_debug_hooks_fp4(limit, hold), "test hooks (4-bit floating point)");
+  QVLA_CUDA(qvla::set_debug_hooks_fp4_token(limit, hold), "test hooks (4-bit floating point, few tokens)");
   return QVLA_OK;
 }
 
@@ -1054,7 +1055,7 @@ qvla_status qvla_debug_gemm_plan_codes(int codes, int M, int K, int N, int gated
 qvla_status qvla_check_device(void* stream) {
   g_last_error.clear();
   unsigned int word = 0, word_tmem = 0, word_fused = 0, word_gemv = 0, word_rqp = 0, word_prompt = 0, word_kv4 = 0, word_akv4 = 0,
-               word_fp4 = 0, word_norm = 0, word_norm16 = 0;
+               word_fp4 = 0, word_token = 0, word_norm = 0, word_norm16 = 0;
   QVLA_CUDA(qvla::read_and_clear_error_word(&word, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_tmem(&word_tmem, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_fused(&word_fused, static_cast<cudaStream_t>(stream)), "device check");
@@ -1064,9 +1065,10 @@ qvla_status qvla_check_device(void* stream) {
   QVLA_CUDA(qvla::read_and_clear_error_word_kv4(&word_kv4, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_attention_kv4(&word_akv4, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_fp4(&word_fp4, static_cast<cudaStream_t>(stream)), "device check");
+  QVLA_CUDA(qvla::read_and_clear_error_word_fp4_token(&word_token, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_norm_f16(&word_norm, static_cast<cudaStream_t>(stream)), "device check");
   QVLA_CUDA(qvla::read_and_clear_error_word_norm_bf16(&word_norm16, static_cast<cudaStream_t>(stream)), "device check");
-  const unsigned int all = word_fp4 | word_norm | word_norm16 | word | word_tmem | word_fused | word_gemv | word_rqp | word_prompt | word_kv4 | word_akv4;
+  const unsigned int all = word_fp4 | word_token | word_norm | word_norm16 | word | word_tmem | word_fused | word_gemv | word_rqp | word_prompt | word_kv4 | word_akv4;
   if (all & 1u) return fail(QVLA_ERR_TIMEOUT, "a kernel wait ran out of its time limit");
   if (all & 2u)
     return fail(QVLA_ERR_INVALID_ARG, "an offset, length or page index in device memory was out of range; its tokens were skipped");

@@ -125,10 +125,13 @@ qvla_status quantize(const void* x, int xdt, int64_t x_stride, int M, int K, int
   return QVLA_OK;
 }
 
+qvla::Fp4GemmArgs product_args(const qvla_fp4_layer* L, const uint8_t* xq, const uint8_t* xs, const float* xscale, int M, void* y, void* stream) {
+  return {xq, xs, L->fmt == QVLA_NVFP4 ? xscale : nullptr, L->wq, L->ws, L->maps, L->wscale, L->bias, L->fmt, L->ydt, L->gated,
+          M, L->N, L->K, y, qvla::num_sms(L->device), static_cast<cudaStream_t>(stream)};
+}
+
 qvla_status multiply(const qvla_fp4_layer* L, const uint8_t* xq, const uint8_t* xs, const float* xscale, int M, void* y, void* stream) {
-  qvla::Fp4GemmArgs a = {xq, xs, L->fmt == QVLA_NVFP4 ? xscale : nullptr, L->wq, L->ws, L->maps, L->wscale, L->bias, L->fmt, L->ydt, L->gated,
-                         M, L->N, L->K, y, 0, static_cast<cudaStream_t>(stream)};
-  a.num_sms = qvla::num_sms(L->device);
+  const qvla::Fp4GemmArgs a = product_args(L, xq, xs, xscale, M, y, stream);
   QVLA_CUDA(qvla::launch_fp4_gemm(a), "gemm_fp4 launch");
   return QVLA_OK;
 }
@@ -389,6 +392,16 @@ qvla_status qvla_fp4_linear(const qvla_fp4_layer* layer, const void* x, int M, c
   uint8_t* const xq = static_cast<uint8_t*>(workspace);
   uint8_t* const xs = xq + round256(static_cast<size_t>(M) * (layer->K / 2));
   float* const xscale = reinterpret_cast<float*>(xs + round256(qvla_fp4_scale_bytes(fmt, M, layer->K)));
+  // In one launch a CTA may write y while others still read x.
+  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
+  const uintptr_t x1 = x0 + static_cast<size_t>(M) * layer->K * 2, y1 = y0 + static_cast<size_t>(M) * (layer->gated ? layer->N / 2 : layer->N) * 2;
+  if (layer->xdt == layer->ydt && (x1 <= y0 || y1 <= x0)) {
+    bool taken = false;
+    QVLA_CUDA(qvla::launch_fp4_token(product_args(layer, xq, xs, xscale, M, y, stream), x, ilog2_exact(layer->had_block),
+                                     static_cast<float>(1.0 / std::sqrt(static_cast<double>(layer->had_block))), step_scale, &taken),
+              "fp4_linear launch");
+    if (taken) return QVLA_OK;
+  }
   if (qvla_status s = quantize(x, layer->xdt, layer->K, M, layer->K, layer->had_block, fmt, step_scale, xq, xs, xscale, stream)) return s;
   return multiply(layer, xq, xs, xscale, M, y, stream);
 }

@@ -20,58 +20,10 @@
 // 152 SMs idle, and the loads were not the bound), 16 epilogue warps (101 to 103), a second set of scale columns (the same),
 // output lines of 64 bytes (the same), an evict-first hint on the stores (the same), token tiles of even width instead of whole
 // ones and a remainder (816 tokens: 28.3 to 30.3), the gated epilogue without its GELU (0.7 us of 28).
-#include <algorithm>
-#include <atomic>
-
-#include "fp4.cuh"
-#include "gemm_kernel.cuh"
+#include "fp4_mma.cuh"
 
 namespace qvla {
 namespace {
-
-// Descriptor of scales for tcgen05.cp: 32 rows of 16 bytes, 8-row groups 128 bytes apart, no swizzle.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128 >> 4) << 32) | (static_cast<uint64_t>(1) << 46);
-}
-// 128 rows' scales of four blocks (512 bytes) to four TMEM columns, for each of the four lane quadrants.
-__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-
-// Instruction descriptor: A = B = E2M1, both K-major, shape M x N, K = 64; scales E8M0 (MX) or E4M3.
-__host__ __device__ constexpr uint32_t idesc_e2m1_f32(int fmt, int m, int n) {
-  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (fmt == fp4::kMx ? 1u << 23 : 0u) |
-         (static_cast<uint32_t>(m >> 7) << 27);
-}
-
-// 64 codes of K.  MX: two scales a row, bytes `id` and id + 1 (id = 0 or 2) of the column; NV: all four.
-template <int kFmt>
-__device__ __forceinline__ void mma_e2m1(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                         uint32_t accumulate) {
-  if constexpr (kFmt == fp4::kMx) {
-    asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
-        : "memory");
-  } else {
-    asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
-        : "memory");
-  }
-}
-
-// gelu in its tanh form: g / (1 + exp(-2 u)), u = sqrt(2 / pi) (g + 0.044715 g^3); the exponential and the reciprocal by the
-// hardware's approximations (2^-22 and 2^-23 of their values), without the steps that would keep subnormal results.
-__device__ __forceinline__ float gelu_fast(float g) {
-  const float t = g * fmaf(-0.1029432397f, g * g, -2.3022081986f);  // -2 u log2(e)
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return g * r;
-}
 
 // ---- many tokens: CTA pairs, persistent -------------------------------------------------------------------------------
 
@@ -400,19 +352,6 @@ __global__ void __launch_bounds__(kPThreads, 1) fp4_pair_kernel(const __grid_con
   if (warp == kPMma) tmem_dealloc_pair<512>(tmem);
 }
 
-// Scale tiles [row groups][tiles of a row][512 bytes], read in boxes of kTiles tiles of `groups` row groups.
-cudaError_t make_tmap_scales(CUtensorMap* m, const void* base, int row_groups, int tiles, int box_tiles, int box_groups) {
-  PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
-  if (!enc) return cudaErrorNotSupported;
-  const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(tiles), static_cast<cuuint64_t>(row_groups)};
-  const cuuint64_t strides[2] = {512, static_cast<cuuint64_t>(tiles) * 512};
-  const cuuint32_t box[3] = {128, static_cast<cuuint32_t>(box_tiles), static_cast<cuuint32_t>(box_groups)};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
 // The output [M][width] of 16-bit values, written in boxes of 64 channels x 32 tokens from 128-byte swizzled rows.
 cudaError_t make_tmap_y(CUtensorMap* m, void* base, int rows, int width) {
   PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
@@ -425,23 +364,6 @@ cudaError_t make_tmap_y(CUtensorMap* m, void* base, int rows, int width) {
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
-const CUtensorMap& weight_map(const Fp4GemmArgs& a, int i) {
-  return *reinterpret_cast<const CUtensorMap*>(static_cast<const uint8_t*>(a.maps) + i * kFp4MapBytes);
-}
-
-// Raises the kernel's limit of dynamic shared memory once per device; `done` holds the devices where it is.
-cudaError_t raise_smem(const void* kern, int bytes, std::atomic<unsigned long long>* done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const unsigned long long bit = 1ull << (dev & 63);
-  if (done->load() & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-  if (e == cudaSuccess) done->fetch_or(bit);
-  return e;
 }
 
 template <int kBn, int kFmt, bool kGated, typename OutT>
@@ -840,6 +762,11 @@ cudaError_t fp4_weight_maps(const uint8_t* wq, const uint8_t* ws, int fmt, int N
   for (int i = 1; i < kFp4Maps && e == cudaSuccess; ++i)
     e = make_tmap_scales(reinterpret_cast<CUtensorMap*>(at + i * kFp4MapBytes), ws, groups, K / codes, i * 256 / codes, 1);
   return e;
+}
+
+int fp4_split(const Fp4GemmArgs& a) {
+  const F4Plan p = plan_gemm(a);
+  return p.bn == 32 ? p.split : 0;
 }
 
 cudaError_t launch_fp4_gemm(const Fp4GemmArgs& a) {

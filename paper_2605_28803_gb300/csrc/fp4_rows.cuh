@@ -358,14 +358,13 @@ __device__ __forceinline__ void block_sync() {
   }
 }
 
-// Thread j of a row holds v as Place<kLayout> says; `lines` is the row's shared memory.  Leaves codes, block scales and the row's.
-// write: the row and the thread's channels are there.  Every thread of the CTA calls this.  kNamed: the CTA has at most 512
-// threads, so that the 64 or 128 of a block of 2048 or 4096 have a barrier of their own.
-template <int kLayout, int kFmt, bool kNamed>
-__device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGroup& row, int slot, int j, int m, bool write, uint32_t lines,
-                                                float2 (&v)[16]) {
+// Thread j of a row holds v as Place<kLayout> says and leaves with its 32 consecutive channels, rotated; `lines` is the row's
+// shared memory, 128 bytes a thread.  kNamed: at most 512 threads, so that the 64 or 128 of a block of 2048 or 4096 have a barrier of
+// their own (1 and up); without, every thread of the CTA calls this.
+template <int kLayout, bool kNamed>
+__device__ __forceinline__ void rotate(int log_b, float inv_sqrt_b, int j, uint32_t lines, float2 (&v)[16]) {
   if constexpr (kLayout == kFour) {
-    if (a.log_b == 7) butterflies(v, 8);
+    if (log_b == 7) butterflies(v, 8);
     butterflies(v, 4);
     // quad i of line t at piece i ^ f(t), f = 0 2 4 6 1 3 5 7 over 8 lines: two groups' pieces fall on all eight
     const int g = (j >> 2) & 1;
@@ -428,20 +427,21 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
 #pragma unroll
     for (int i = 0; i < 8; ++i) lds_quad(own + ((i ^ q) << 4), v + 2 * i);
   }
-  if (a.log_b > 0) {
-    const int n = kLayout == kPlain ? a.log_b : 5;  // stages among a thread's 32 channels
+  if (log_b > 0) {
+    const int n = kLayout == kPlain ? log_b : 5;  // stages among a thread's 32 channels
     if (n > 4) butterflies(v, 8);
     if (n > 3) butterflies(v, 4);
     if (n > 2) butterflies(v, 2);
     if (n > 1) butterflies(v, 1);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      v[i] = __fmul2_rn(make_float2(v[i].x + v[i].y, v[i].x - v[i].y), both(a.inv_sqrt_b));
+      v[i] = __fmul2_rn(make_float2(v[i].x + v[i].y, v[i].x - v[i].y), both(inv_sqrt_b));
     }
   }
+}
 
-  // ---- scales and codes ----
-  float top[2];
+// The largest magnitude of each half of a thread's channels, NaN if one is.
+__device__ __forceinline__ void magnitudes(const float2 (&v)[16], float (&top)[2]) {
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     float t = 0.0f;
@@ -449,72 +449,91 @@ __device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGrou
     for (int i = 8 * b; i < 8 * b + 8; ++i) t = rq::max_nan(t, rq::max_nan(fabsf(v[i].x), fabsf(v[i].y)));
     top[b] = t;
   }
+}
+
+// A thread's MX block: its scale's byte.
+__device__ __forceinline__ uint32_t encode_mx(const float2 (&v)[16], const float (&top)[2], uint32_t (&code)[4]) {
+  const uint32_t t = __float_as_uint(rq::max_nan(top[0], top[1]));
+  uint32_t byte = 0;
+  float to_codes = 0.0f;  // 2^-e
+  if (t >= 0x7F800000u) {
+    byte = 255u;  // an infinity or NaN: the block has no values
+  } else if (t != 0u) {
+    // floor(log2) - 2, of a subnormal below the clamp at -127 anyway
+    const int e = max(static_cast<int>(t >> 23) - 127 - 2, -127);
+    byte = static_cast<uint32_t>(e + 127);
+    to_codes = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);  // (e <= 125; e = -127 gives 2^127)
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {  // the products are exact
+    float2 s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = __fmul2_rn(v[4 * c + i], both(to_codes));
+    code[c] = e2m1x8(s[0], s[1], s[2], s[3]);
+  }
+  return byte;
+}
+
+// A row's scale by its largest magnitude.
+__device__ __forceinline__ float row_scale(float most) {
+  const float delta = __fdiv_rn(most, kRowMax);
+  return isinf(delta) ? __int_as_float(0x7FC00000) : delta;
+}
+
+// A thread's two NV blocks: their scales' bytes, the first in the low one.
+__device__ __forceinline__ uint32_t encode_nv(const float2 (&v)[16], const float (&top)[2], float delta, uint32_t (&code)[4]) {
+  uint32_t bytes = 0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const uint32_t s = delta > 0.0f && !isinf(delta) ? block_scale_e4m3(top[b], delta) : 0u;
+    bytes |= s << (8 * b);
+    const float d = e4m3_value(s) * delta;
+    const bool easy = d >= 8.673617379884035e-19f && d <= 1.152921504606846976e18f;  // 2^-60 .. 2^60
+    const float r = easy ? near_reciprocal(d) : 0.0f;
+    // The float32 quotient is within 2^-22 of the exact one: where it rounds alike moved up and down by 2^-20 it decides.
+    const float up = r * 1.00000095367431640625f, dn = r * 0.99999904632568359375f;
+#pragma unroll
+    for (int c = 2 * b; c < 2 * b + 2; ++c) {
+      float2 h[4], l[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] = __fmul2_rn(v[4 * c + i], both(up));
+        l[i] = __fmul2_rn(v[4 * c + i], both(dn));
+      }
+      uint32_t w = e2m1x8(h[0], h[1], h[2], h[3]);
+      const uint32_t low = e2m1x8(l[0], l[1], l[2], l[3]);
+      if (w != low) w = decide_codes(low, w, v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3], d);
+      if (!easy && d > 0.0f) w = codes_exact(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3], d);
+      code[c] = w;
+    }
+  }
+  return bytes;
+}
+
+// Rotates v (as above) and leaves codes, block scales and the row's.  write: the row and the thread's channels are there.  Every thread
+// of the CTA calls this.
+template <int kLayout, int kFmt, bool kNamed>
+__device__ __forceinline__ void rotate_quantize(const RowsArgs& a, const RowGroup& row, int slot, int j, int m, bool write, uint32_t lines,
+                                                float2 (&v)[16]) {
+  rotate<kLayout, kNamed>(a.log_b, a.inv_sqrt_b, j, lines, v);
+  float top[2];
+  magnitudes(v, top);
   uint32_t code[4];
   if constexpr (kFmt == kMx) {
-    const uint32_t t = __float_as_uint(rq::max_nan(top[0], top[1]));
-    uint32_t byte = 0;
-    float to_codes = 0.0f;  // 2^-e
-    if (t >= 0x7F800000u) {
-      byte = 255u;  // an infinity or NaN: the block has no values
-    } else if (t != 0u) {
-      // floor(log2) - 2, of a subnormal below the clamp at -127 anyway
-      const int e = max(static_cast<int>(t >> 23) - 127 - 2, -127);
-      byte = static_cast<uint32_t>(e + 127);
-      to_codes = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);  // (e <= 125; e = -127 gives 2^127)
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {  // the products are exact
-      float2 s[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = __fmul2_rn(v[4 * c + i], both(to_codes));
-      code[c] = e2m1x8(s[0], s[1], s[2], s[3]);
-    }
     // the four threads of a tile's group hand their bytes to the first
-    uint32_t w = byte << (8 * (j & 3));
+    uint32_t w = encode_mx(v, top, code) << (8 * (j & 3));
     w |= __shfl_xor_sync(0xffffffffu, w, 1);
     w |= __shfl_xor_sync(0xffffffffu, w, 2);
     if (write && (j & 3) == 0) *reinterpret_cast<uint32_t*>(a.scales + scale_offset(m, j, a.K >> 7)) = w;
   } else {
-    float delta;
-    if (a.step_scale != nullptr) {
-      delta = *a.step_scale;
-    } else {
-      delta = __fdiv_rn(row.max(rq::max_nan(top[0], top[1]), slot), kRowMax);
-      if (isinf(delta)) delta = __int_as_float(0x7FC00000);
-    }
+    const float delta = a.step_scale != nullptr ? *a.step_scale : row_scale(row.max(rq::max_nan(top[0], top[1]), slot));
     if (write && j == 0) a.row_scale[m] = delta;
-    uint32_t bytes = 0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint32_t s = delta > 0.0f && !isinf(delta) ? block_scale_e4m3(top[b], delta) : 0u;
-      bytes |= s << (8 * b);
-      const float d = e4m3_value(s) * delta;
-      const bool easy = d >= 8.673617379884035e-19f && d <= 1.152921504606846976e18f;  // 2^-60 .. 2^60
-      const float r = easy ? near_reciprocal(d) : 0.0f;
-      // The float32 quotient is within 2^-22 of the exact one: where it rounds alike moved up and down by 2^-20 it decides.
-      const float up = r * 1.00000095367431640625f, dn = r * 0.99999904632568359375f;
-#pragma unroll
-      for (int c = 2 * b; c < 2 * b + 2; ++c) {
-        float2 h[4], l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[i] = __fmul2_rn(v[4 * c + i], both(up));
-          l[i] = __fmul2_rn(v[4 * c + i], both(dn));
-        }
-        uint32_t w = e2m1x8(h[0], h[1], h[2], h[3]);
-        const uint32_t low = e2m1x8(l[0], l[1], l[2], l[3]);
-        if (w != low) w = decide_codes(low, w, v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3], d);
-        if (!easy && d > 0.0f) w = codes_exact(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3], d);
-        code[c] = w;
-      }
-    }
-    uint32_t w = bytes << (16 * (j & 1));
+    uint32_t w = encode_nv(v, top, delta, code) << (16 * (j & 1));
     w |= __shfl_xor_sync(0xffffffffu, w, 1);
     if (write && (j & 1) == 0) *reinterpret_cast<uint32_t*>(a.scales + scale_offset(m, 2 * j, a.K >> 6)) = w;
   }
   if (write) *reinterpret_cast<uint4*>(a.codes + static_cast<size_t>(m) * (a.K >> 1) + j * 16) = make_uint4(code[0], code[1], code[2], code[3]);
 }
-
 
 template <typename T, int kLayout, int kFmt>
 __global__ void __launch_bounds__(kRowThreads, 2) quantize_rows_kernel(const RowsArgs a) {

@@ -271,6 +271,13 @@ cudaError_t launch_fp4_gemm(const Fp4GemmArgs& a);
 // Tensor maps of a layer's weights, made once: codes; scales by 256 codes of K; scales by 512.
 constexpr int kFp4Maps = 3, kFp4MapBytes = 128;
 cudaError_t fp4_weight_maps(const uint8_t* wq, const uint8_t* ws, int fmt, int N, int K, void* maps);
+// CTAs of a cluster of the split product, where that takes the call with tiles of 32 tokens; else 0.
+int fp4_split(const Fp4GemmArgs& a);
+// The linear of a few tokens x [M][K] of the output's type (fp4_token.cu), where one launch serves it: else not taken.  a's xq, xs and
+// xrow are not used.
+cudaError_t launch_fp4_token(const Fp4GemmArgs& a, const void* x, int log_b, float inv_sqrt_b, const float* step, bool* taken);
+cudaError_t read_and_clear_error_word_fp4_token(unsigned int* out, cudaStream_t stream);
+cudaError_t set_debug_hooks_fp4_token(unsigned long long wait_limit_ns, int hold_loads);
 cudaError_t read_and_clear_error_word_fp4(unsigned int* out, cudaStream_t stream);
 cudaError_t set_debug_hooks_fp4(unsigned long long wait_limit_ns, int hold_loads);
 
