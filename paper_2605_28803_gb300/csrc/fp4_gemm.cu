@@ -19,7 +19,8 @@
 // Tried and dropped: clusters of two pairs that share the tokens by multicast (102 us to 106: four-CTA clusters leave 8 of the
 // 152 SMs idle, and the loads were not the bound), 16 epilogue warps (101 to 103), a second set of scale columns (the same),
 // output lines of 64 bytes (the same), an evict-first hint on the stores (the same), token tiles of even width instead of whole
-// ones and a remainder (816 tokens: 28.3 to 30.3), the gated epilogue without its GELU (0.7 us of 28).
+// ones and a remainder (816 tokens: 28.3 to 30.3), two pairs a tile with half of K each (816 x 16384 -> 2048, NV, 15.4 to 18.4: fewer
+// stages a CTA, and the loads are the bound there), the gated epilogue without its GELU (0.7 us of 28).
 #include "fp4_mma.cuh"
 
 namespace qvla {
