@@ -19,7 +19,8 @@
 // Tried and dropped: clusters of two pairs that share the tokens by multicast (102 us to 106: four-CTA clusters leave 8 of the
 // 152 SMs idle, and the loads were not the bound), 16 epilogue warps (101 to 103), a second set of scale columns (the same),
 // output lines of 64 bytes (the same), an evict-first hint on the stores (the same), token tiles of even width instead of whole
-// ones and a remainder (816 tokens: 28.3 to 30.3), two pairs a tile with half of K each (816 x 16384 -> 2048, NV, 15.4 to 18.4: fewer
+// ones and a remainder (816 tokens: 28.3 to 30.3), weights held in shared memory over the token tiles (K 2048: 95 to 110; with 512 as
+// much faster as the order of units alone makes it), two pairs a tile with half of K each (816 x 16384 -> 2048, NV, 15.4 to 18.4: fewer
 // stages a CTA, and the loads are the bound there), the gated epilogue without its GELU (0.7 us of 28).
 #include "fp4_mma.cuh"
 
@@ -40,16 +41,18 @@ struct PairParams {
   int M, N, K;  // N weight rows
   int tiles_m, tiles_n;
   int bn_last;  // columns of the last token tile: its tokens rounded up to 16
-  // Work unit u: first the whole token tiles, weight tile by weight tile, then the last one's where it is narrower.  (In plain
-  // order a pair could meet whole tiles only: 816 tokens are 4 tiles of 256 or fewer, and 4 divides 76 pairs.)
+  int by_tokens;  // the order of work units
+  // Work unit u.  By weights: first the whole token tiles, weight tile by weight tile, then the last one's where it is narrower (in plain
+  // order a pair could meet whole tiles only: 816 tokens are 4 tiles of 256 or fewer, and 4 divides 76 pairs), so that weights come from
+  // memory once.  By tokens: what the pairs write at a time are whole rows of y nearly, so that outputs leave faster.
   __device__ __forceinline__ void unit(int u, int& ta, int& tb, int bn) const {
     const int whole = tiles_m - (bn_last < bn ? 1 : 0);
-    if (u < whole * tiles_n) {
-      ta = u % whole;
+    if (!by_tokens && u < whole * tiles_n) {
       tb = u / whole;
+      ta = u - tb * whole;
     } else {
-      ta = whole;
-      tb = u - whole * tiles_n;
+      ta = u / tiles_n;
+      tb = u - ta * tiles_n;
     }
   }
 };
@@ -382,7 +385,10 @@ cudaError_t launch_pair(const Fp4GemmArgs& a) {
   static_assert(C::kSmem >= 161 * 1024, "no CTA of a cluster of the split kernel beside this one (its launch says why)");
   if (e == cudaSuccess) e = make_tmap_y(&ty, a.y, a.M, kGated ? a.N / 2 : a.N);
   if (e != cudaSuccess) return e;
-  PairParams p = {a.xrow, a.wrow, a.bias, a.M, a.N, a.K, (a.M + kBn - 1) / kBn, (a.N + 255) / 256, 0};
+  // By tokens where the outputs are 8 times the weights: 8192 x 512 -> 16384, MX, 48 us against 56, 8192 x 2048 -> 16384 95 against 95
+  // to 96; but 816 x 2048 -> 2 x 16384 with other weights in every call, 29.2 against 28.4.
+  const bool by_tokens = 2ll * a.M * (kGated ? a.N / 2 : a.N) > 8ll * a.N * (a.K / 2);
+  PairParams p = {a.xrow, a.wrow, a.bias, a.M, a.N, a.K, (a.M + kBn - 1) / kBn, (a.N + 255) / 256, 0, by_tokens};
   p.bn_last = (a.M - (p.tiles_m - 1) * kBn + 15) / 16 * 16;
   const int units = p.tiles_m * p.tiles_n, pairs = a.num_sms / 2;
   cudaLaunchConfig_t cfg = {};

@@ -204,3 +204,13 @@ def test_a_wait_that_runs_out_is_reported(m):
     assert (y == 3.0).all()
     assert torch.equal(multiply(layer, x, m, "bf16"), want)
     layer.close()
+
+
+@pytest.mark.parametrize("fmt", [F.MX, F.NV])
+@pytest.mark.parametrize("m,n,k,dtype,gated", [(1025, 528, 128, "f16", False), (2100, 1040, 256, "bf16", False), (1800, 4096, 128, "bf16", False), (1111, 512, 128, "f16", True)])
+def test_outputs_far_larger_than_the_weights(fmt, m, n, k, dtype, gated):
+    """Here the work runs token tile by token tile."""
+    x, w = Matrix(21, m, k, fmt), Matrix(22, n, k, fmt, k ** -0.5)
+    layer = layer_of(w, dtype, gated=gated)
+    assert_product(multiply(layer, x, m, dtype), x, w, None, dtype, gated)
+    layer.close()
