@@ -12,7 +12,7 @@
 // tile's K.
 //
 // us in a graph of calls (MX unless noted), one 128 x 128 tile a CTA on one SM before and these: 8192 x 2048 -> 16384 342
-// and 96 (5.7 PFLOP/s); 816 x 2048 -> 2 x 16384 gated, NV, 81 and 28; 1187 x 4096 -> 2576 17.4 and 8.9; one token of 16384 ->
+// and 94 (5.8 PFLOP/s); 816 x 2048 -> 2 x 16384 gated, NV, 81 and 28; 1187 x 4096 -> 2576 17.4 and 8.9; one token of 16384 ->
 // 2048 24 and 5.5.  What bounds the large ones: without the epilogue's stores 8192 x 2048 -> 16384 takes 83 us, without the
 // epilogue 79 (27 tiles a pair, 5600 cycles each at 1.9 GHz against 4350 of tensor work, 700 of them the hand-over of
 // the one accumulator that fits); the 268 MB of outputs leave at 2.8 TB/s beside it.
