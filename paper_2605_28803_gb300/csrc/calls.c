@@ -16,6 +16,10 @@ static PyObject *g_check, *g_layer, *g_norm; /* callable(status): raises; the ty
 static int take(const char* call, const char* const* names, int n, int optional, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames,
                 PyObject** slots) {
   Py_ssize_t i, k;
+  if (!g_check) {
+    PyErr_Format(PyExc_RuntimeError, "%s(): not set up (import the package's qvla)", call);
+    return -1;
+  }
   if (nargs > n) {
     PyErr_Format(PyExc_TypeError, "%s() takes %d arguments but %zd were given", call, n, nargs);
     return -1;

@@ -119,3 +119,19 @@ def test_objects_of_another_kind():
     closed = qvla.Fp4Layer(None, 128, 128, 1, qvla.MXFP4, qvla.BF16, qvla.BF16, False)
     with pytest.raises(qvla.QvlaError, match="layer must not be NULL"):
         qvla.qvla_gemm_fp4(closed, Address(), Address(), None, 1, Address())
+
+
+def test_the_compiled_part_alone_refuses_calls():
+    """Without the rest of the binding it knows no types and no errors."""
+    import subprocess
+
+    run = subprocess.run([sys.executable, "-c", "\n".join([
+        "import importlib.util, sys",
+        f"spec = importlib.util.spec_from_file_location('_calls', {qvla._calls.__file__!r})",
+        "m = importlib.util.module_from_spec(spec); spec.loader.exec_module(m)",
+        "for call in ('qvla_gemm_fp4', 'qvla_block_norm', 'qvla_fp4_quantize_rows'):",
+        "    try:",
+        "        getattr(m, call)(*[None] * {'qvla_gemm_fp4': 7, 'qvla_block_norm': 11, 'qvla_fp4_quantize_rows': 12}[call])",
+        "    except RuntimeError as e:",
+        "        print(e)"])], capture_output=True, text=True)
+    assert run.returncode == 0 and run.stdout.count("not set up") == 3, run.stderr
