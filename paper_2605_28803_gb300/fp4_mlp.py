@@ -49,19 +49,20 @@ class Fp4Mlp:
         self.row_scales = empty(max_tokens, torch.float32)
         self.hidden, self.out, self.next = empty((max_tokens, gate_up.N), t), empty((max_tokens, k), t), empty((max_tokens, k), t)
         self.work = empty(Q.qvla_fp4_linear_workspace_bytes(down, max_tokens), torch.uint8)
-        self._last = None  # the stream of the latest call
+        # The stream of the latest call.  The buffers are the allocator's memory of this one, which its earlier work may still use.
+        self._last = torch.cuda.current_stream() if self.codes.is_cuda else None
 
     def _stream(self) -> torch.cuda.Stream:
-        """The current stream, behind the block's latest call.  (What a graph is captured from, or replayed beside, is ordered by
-        the one who replays it.)"""
+        """The current stream, behind the block's construction and latest call.  (What a graph is captured from, or replayed
+        beside, is ordered by the one who replays it, and the block has to outlive the replays.)"""
         stream = torch.cuda.current_stream()
         if torch.cuda.is_current_stream_capturing():
             return stream
-        if self._last is not None and stream != self._last:
+        if stream != self._last:
             stream.wait_stream(self._last)
             for t in (self.codes, self.scales, self.row_scales, self.hidden, self.out, self.next, self.work):
                 t.record_stream(stream)
-        self._last = stream
+            self._last = stream
         return stream
 
     def _check(self, residual, branch) -> int:
