@@ -22,7 +22,8 @@ _TORCH = {Q.F16: torch.float16, Q.BF16: torch.bfloat16, Q.F32: torch.float32}
 class Fp4Mlp:
     """``gate_up``: a gated Fp4Layer; ``down``: an Fp4Layer with K = gate_up.N and N = gate_up.K, of one 16-bit type.  ``before``
     and ``after``: the BlockNorm on either side, of that type.  Up to ``max_tokens`` tokens a call; the residual is kept in
-    ``residual_dtype`` (the layers' type, or F32)."""
+    ``residual_dtype`` (the layers' type, or F32).  Layers, norms, residual and branch lie on one device, the current one in every
+    call."""
 
     def __init__(self, gate_up: Q.Fp4Layer, down: Q.Fp4Layer, before: Q.BlockNorm, after: Q.BlockNorm, max_tokens: int,
                  residual_dtype: int | None = None, device=None):
@@ -38,10 +39,9 @@ class Fp4Mlp:
             raise ValueError("max_tokens must be positive")
         self.gate_up, self.down, self.before, self.after = gate_up, down, before, after
         self.dt, self.rdt, self.max_tokens, self.width = dt, residual_dtype, max_tokens, gate_up.K
-        self.device = torch.device("cuda") if device is None else torch.device(device)
 
         def empty(n, dtype):
-            return torch.empty(n, dtype=dtype, device=self.device)
+            return torch.empty(n, dtype=dtype, device="cuda" if device is None else device)
 
         k, t = self.width, _TORCH[dt]
         self.codes = empty((max_tokens, k // 2), torch.uint8)
@@ -49,13 +49,17 @@ class Fp4Mlp:
         self.row_scales = empty(max_tokens, torch.float32)
         self.hidden, self.out, self.next = empty((max_tokens, gate_up.N), t), empty((max_tokens, k), t), empty((max_tokens, k), t)
         self.work = empty(Q.qvla_fp4_linear_workspace_bytes(down, max_tokens), torch.uint8)
+        self.device = self.codes.device  # with its index
         # The stream of the latest call.  The buffers are the allocator's memory of this one, which its earlier work may still use.
-        self._last = torch.cuda.current_stream() if self.codes.is_cuda else None
+        self._last = torch.cuda.current_stream(self.device) if self.codes.is_cuda else None
+        for name, norm in (("before", before), ("after", after)):
+            if any(t is not None and t.device != self.device for t in norm.tensors):
+                raise ValueError(f"the tensors of `{name}` must lie on {self.device}")
 
     def _stream(self) -> torch.cuda.Stream:
         """The current stream, behind the block's construction and latest call.  (What a graph is captured from, or replayed
         beside, is ordered by the one who replays it, and the block has to outlive the replays.)"""
-        stream = torch.cuda.current_stream()
+        stream = torch.cuda.current_stream(self.device)
         if torch.cuda.is_current_stream_capturing():
             return stream
         if stream != self._last:
@@ -66,15 +70,18 @@ class Fp4Mlp:
         return stream
 
     def _check(self, residual, branch) -> int:
-        """The library takes sizes on trust where they lie on the device: an input of other sizes would be read past its end."""
+        """The library takes addresses and sizes on trust: an input of other sizes would be read past its end, one of another GPU
+        through an address that means nothing on this one."""
         m = residual.shape[0]
         if m > self.max_tokens:
             raise ValueError(f"{m} tokens are more than {self.max_tokens}")
         for name, x, dtype in (("residual", residual, _TORCH[self.rdt]), ("branch", branch, _TORCH[self.dt])):
             if tuple(x.shape) != (m, self.width) or x.dtype != dtype or not x.is_contiguous():
                 raise ValueError(f"{name} must be contiguous {dtype} [{m}, {self.width}]")
-            if x.device.type != self.device.type:
+            if x.device != self.device:
                 raise ValueError(f"{name} must lie on {self.device}")
+        if self.codes.is_cuda and torch.cuda.current_device() != self.device.index:  # the kernels run there
+            raise ValueError(f"the current device must be {self.device}")
         return m
 
     def __call__(self, residual: torch.Tensor, branch: torch.Tensor) -> torch.Tensor:
