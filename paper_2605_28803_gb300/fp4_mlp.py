@@ -55,6 +55,8 @@ class Fp4Mlp:
         for name, norm in (("before", before), ("after", after)):
             if any(t is not None and t.device != self.device for t in norm.tensors):
                 raise ValueError(f"the tensors of `{name}` must lie on {self.device}")
+            if any(t is not None and t.shape[-1] != k for t in norm.tensors[:-1]):  # (wider ones would be cut, silently)
+                raise ValueError(f"the vectors of `{name}` must have the layers' {k} channels")
 
     def _stream(self) -> torch.cuda.Stream:
         """The current stream, behind the block's construction and latest call.  (What a graph is captured from, or replayed
