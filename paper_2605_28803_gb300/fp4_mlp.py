@@ -52,7 +52,10 @@ class Fp4Mlp:
         self.device = self.codes.device  # with its index
         # The stream of the latest call.  The buffers are the allocator's memory of this one, which its earlier work may still use.
         self._last = torch.cuda.current_stream(self.device) if self.codes.is_cuda else None
+        self._tokens = {}  # that each norm's conditioning reaches over
         for name, norm in (("before", before), ("after", after)):
+            conditioned = norm.struct.mod_rows > 0 and norm.tensors[-1] is None
+            self._tokens[name] = norm.struct.mod_rows * norm.struct.mod_tokens if conditioned else norm.tokens
             if any(t is not None and t.device != self.device for t in norm.tensors):
                 raise ValueError(f"the tensors of `{name}` must lie on {self.device}")
             if any(t is not None and t.shape[-1] != k for t in norm.tensors[:-1]):  # (wider ones would be cut, silently)
@@ -77,6 +80,9 @@ class Fp4Mlp:
         m = residual.shape[0]
         if m > self.max_tokens:
             raise ValueError(f"{m} tokens are more than {self.max_tokens}")
+        for name, tokens in self._tokens.items():  # (the call itself would say so, of `after` when the residual has changed)
+            if m > tokens:
+                raise ValueError(f"{m} tokens are more than the {tokens} of the conditioning of `{name}`")
         for name, x, dtype in (("residual", residual, _TORCH[self.rdt]), ("branch", branch, _TORCH[self.dt])):
             if tuple(x.shape) != (m, self.width) or x.dtype != dtype or not x.is_contiguous():
                 raise ValueError(f"{name} must be contiguous {dtype} [{m}, {self.width}]")
