@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kTThreads, 1) fp4_token_kernel(const __grid_co
     int it = 0, s = 0;
     uint32_t ph = 0;
     for (int kb = ka; kb < kz && ok; ++kb, ++it) {
+      if (it == S) griddep_wait();  // (the ring is full until there are tokens: the wait's limit is not for the previous kernel)
       if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_empty[s]), ph ^ 1u))) break;
       if (elect_one()) {
         const uint32_t full = smem_u32(&bar_full[s]), dst = smem_u32(smem + s * C::kStage);
