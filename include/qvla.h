@@ -595,7 +595,8 @@ typedef struct {
  *   y  device, the block's output, rows of dt y_stride elements apart, or NULL: no block has run yet
  *   r_out  device, rows r_stride apart; may be r.  NULL where y is NULL and residual_scale is 1: r is left as it is
  *   h  device out [M][K] of dt (F16 or BF16), dense, or NULL: the residual alone
- * Pointers are 16-byte aligned; K % 8 == 0, K <= 16384, M in [0, 2^20].  h and r_out overlap no input (r_out may be r itself). */
+ * Pointers are 16-byte aligned; K % 8 == 0, K <= 16384, M in [0, 2^20].  h and r_out overlap no input, but r_out may be r
+ * itself, and h may be y itself where y_stride is K or M is 1 (QVLA_ERR_INVALID_ARG else). */
 qvla_status qvla_block_norm(const qvla_block_norm_params* norm, qvla_dtype dt, const void* r, qvla_dtype rdt, int64_t r_stride,
                             const void* y, int64_t y_stride, int M, int K, void* r_out, void* h, void* stream);
 

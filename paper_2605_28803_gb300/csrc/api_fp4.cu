@@ -224,6 +224,7 @@ qvla_status check_norm(const qvla_block_norm_params* n, qvla_dtype dt, const voi
   if (qvla_status s = check_matrix("r_out", r_out, M, r_stride, K, true)) return s;
   if (qvla_status s = check_matrix("y", y, M, y_stride, K, true)) return s;
   if (h && !aligned16(h)) return fail(QVLA_ERR_INVALID_ARG, "h must be 16-byte aligned");
+  if (h && h == y && y_stride != K && M > 1) return fail(QVLA_ERR_INVALID_ARG, "h is dense: it may be y only where y_stride is K=%d", K);
   if (!r_out && (y || n->residual_scale != 1.0f))
     return fail(QVLA_ERR_INVALID_ARG, "r_out may be NULL only without a branch and with residual_scale 1");
   if (!r_out && !h && !quant) return fail(QVLA_ERR_INVALID_ARG, "neither r_out nor h is given");

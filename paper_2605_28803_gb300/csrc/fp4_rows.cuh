@@ -287,7 +287,9 @@ __device__ __forceinline__ void norm_rows(const RowsArgs& a, const RowGroup& row
     }
     T* const ph = static_cast<T*>(a.h) + static_cast<size_t>(m) * a.K;
     m += step;
-    if (k + 1 < rows && m < a.M) fetch(m);  // (after this row's stores: a caller may update the residual in place)
+    // (A caller may update the residual in place, and have h where y is: a thread has its pieces of a row in registers before it writes
+    // them, another one reads them only where it has no channels and uses none, and other rows are other memory.)
+    if (k + 1 < rows && m < a.M) fetch(m);
     if (!norm_h) continue;
     const float2 s = both(norm_scale<N>(v, has, row, slot + 2, layer, width, a.norm.eps));
 #pragma unroll
