@@ -1,7 +1,8 @@
 """Build libqvla.so in-tree for sm_103a (GB300) with nvcc: one object per source, compiled in
 parallel, then linked into paper_2605_28803_gb300/libqvla.so.  The CUDA runtime is linked
-statically so the library needs nothing on LD_LIBRARY_PATH.  Beside it _calls.so, the part of the
-Python binding that is compiled (csrc/calls.c; it finds libqvla.so in its own folder)."""
+statically so the library needs nothing on LD_LIBRARY_PATH.  Beside it _calls, the part of the
+Python binding that is compiled (csrc/calls.c; it finds libqvla.so in its own folder), under the tag
+of the interpreter that it is compiled for."""
 
 from __future__ import annotations
 
@@ -16,7 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libqvla.so")
-CALLS = os.path.join(PKG, "_calls.so")
+CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -49,35 +50,40 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+def _stale(target: str) -> bool:
+    if not os.path.exists(target):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    t = os.path.getmtime(target)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
     deps.append(__file__)
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _link(cmd: list[str], target: str) -> None:
+    tmp = target + ".tmp"
+    r = subprocess.run([tmp if word is None else word for word in cmd], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"linking {os.path.basename(target)} failed:\n{' '.join(map(str, cmd))}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, target)
+
+
+def _build_calls() -> None:
+    _link([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.c"), "-o", None, LIB,
+           "-Wl,-rpath,$ORIGIN"], CALLS)
+    untagged = os.path.join(PKG, "_calls.so")  # as it was named once: every interpreter would import it
+    if os.path.exists(untagged):
+        os.remove(untagged)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile and link libqvla.so if any source is newer than it; return its path."""
-    if not force and not _stale():
-        return LIB
-    os.makedirs(BUILD, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
-        objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-    tmp = LIB + ".tmp"
-    cmd = [_nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-Xcompiler", "-pthread", "-Xlinker", "-soname=libqvla.so"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"linking libqvla.so failed:\n{' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, LIB)
-    tmp = CALLS + ".tmp"
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.c"), "-o", tmp, LIB,
-           "-Wl,-rpath,$ORIGIN"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"building _calls.so failed:\n{' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, CALLS)
+    """Compile and link what any source is newer than; return libqvla.so's path."""
+    if force or _stale(LIB):
+        os.makedirs(BUILD, exist_ok=True)
+        with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+            objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
+        _link([_nvcc(), *ARCH, "-shared", "-o", None, *objs, "-Xcompiler", "-pthread", "-Xlinker", "-soname=libqvla.so"], LIB)
+    if force or _stale(CALLS):
+        _build_calls()
     return LIB
 
 

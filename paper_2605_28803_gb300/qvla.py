@@ -4,7 +4,7 @@ floating-point operators and norms by the compiled _calls).
 Tensors are passed as raw pointers (``tensor.data_ptr()``) and streams as
 ``torch.cuda.Stream.cuda_stream``; every step of the computation runs in libqvla's kernels.
 A non-zero status raises QvlaError with the library's message.  Importing this module loads
-the in-tree libqvla.so and _calls.so and fails loudly if they have not been built.
+the in-tree libqvla.so and _calls and fails loudly if they have not been built.
 """
 
 from __future__ import annotations
