@@ -68,7 +68,11 @@ def _link(cmd: list[str], target: str) -> None:
 
 
 def _build_calls() -> None:
-    _link([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.c"), "-o", None, LIB,
+    include = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        sys.stderr.write(f"no Python.h in {include}: the calls of 4-bit floating point and of the norms are left out of the Python binding\n")
+        return
+    _link([os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", include, os.path.join(CSRC, "calls.c"), "-o", None, LIB,
            "-Wl,-rpath,$ORIGIN"], CALLS)
     untagged = os.path.join(PKG, "_calls.so")  # as it was named once: every interpreter would import it
     if os.path.exists(untagged):

@@ -4,7 +4,8 @@ floating-point operators and norms by the compiled _calls).
 Tensors are passed as raw pointers (``tensor.data_ptr()``) and streams as
 ``torch.cuda.Stream.cuda_stream``; every step of the computation runs in libqvla's kernels.
 A non-zero status raises QvlaError with the library's message.  Importing this module loads
-the in-tree libqvla.so and _calls and fails loudly if they have not been built.
+the in-tree libqvla.so and fails loudly if it has not been built; without _calls the calls that it
+has fail loudly, and the others work.
 """
 
 from __future__ import annotations
@@ -102,7 +103,10 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
 
 _lib = load_library()
 
-from . import _calls  # noqa: E402  (linked against libqvla.so, whose absence is reported above)
+try:
+    from . import _calls  # (linked against libqvla.so, whose absence is reported above)
+except ImportError as error:  # built without CPython's headers, say: reported by the calls that it has
+    _calls, _no_calls = None, str(error)
 
 
 def lib() -> ctypes.CDLL:
@@ -393,12 +397,23 @@ def qvla_attention_kv4(cache: Kv4Cache, q, dt: int, heads: int, q_stride: int, b
 
 # 4-bit floating point and the norms around a block.  The calls of a step come compiled (csrc/calls.c), as they cost no more than
 # their launch otherwise: what is optional is None or a tensor, a stream None, an address or a torch stream.
-qvla_fp4_quantize_rows = _calls.qvla_fp4_quantize_rows
-qvla_fp4_dequantize_rows = _calls.qvla_fp4_dequantize_rows
-qvla_gemm_fp4 = _calls.qvla_gemm_fp4
-qvla_fp4_linear = _calls.qvla_fp4_linear
-qvla_block_norm = _calls.qvla_block_norm
-qvla_block_norm_fp4 = _calls.qvla_block_norm_fp4
+def _compiled(name: str):
+    if _calls is not None:
+        return getattr(_calls, name)
+
+    def call(*args, **kwargs):
+        raise ImportError(f"{name}() is a compiled call, and _calls cannot be imported ({_no_calls}): run __graft_entry__.build() with CPython's headers")
+
+    call.__name__ = name
+    return call
+
+
+qvla_fp4_quantize_rows = _compiled("qvla_fp4_quantize_rows")
+qvla_fp4_dequantize_rows = _compiled("qvla_fp4_dequantize_rows")
+qvla_gemm_fp4 = _compiled("qvla_gemm_fp4")
+qvla_fp4_linear = _compiled("qvla_fp4_linear")
+qvla_block_norm = _compiled("qvla_block_norm")
+qvla_block_norm_fp4 = _compiled("qvla_block_norm_fp4")
 
 
 def qvla_fp4_scale_bytes(fmt: int, rows: int, K: int) -> int:
@@ -493,7 +508,8 @@ class BlockNorm:
         self.ref = ctypes.addressof(self.struct)
 
 
-_calls.setup(_check, Fp4Layer, BlockNorm)
+if _calls is not None:
+    _calls.setup(_check, Fp4Layer, BlockNorm)
 
 
 def qvla_check_device(stream=None) -> None:
