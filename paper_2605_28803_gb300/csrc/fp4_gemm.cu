@@ -14,7 +14,7 @@
 // us in a graph of calls (MX unless noted), one 128 x 128 tile a CTA on one SM before and these: 8192 x 2048 -> 16384 342
 // and 94 (5.8 PFLOP/s); 816 x 2048 -> 2 x 16384 gated, NV, 81 and 28; 1187 x 4096 -> 2576 17.4 and 8.9; one token of 16384 ->
 // 2048 24 and 5.5.  What bounds the large ones: without the epilogue's stores 8192 x 2048 -> 16384 takes 83 us, without the
-// epilogue 79 (27 tiles a pair, 5600 cycles each at 1.9 GHz against 4350 of tensor work, 700 of them the hand-over of
+// epilogue 79, at K = 64 an instruction (27 tiles a pair, 5600 cycles each at 1.9 GHz against 4350 of tensor work, 700 of them the hand-over of
 // the one accumulator that fits); the 268 MB of outputs leave at 2.8 TB/s beside it.
 // Tried and dropped: clusters of two pairs that share the tokens by multicast (102 us to 106: four-CTA clusters leave 8 of the
 // 152 SMs idle, and the loads were not the bound), 16 epilogue warps (101 to 103), a second set of scale columns (the same),
@@ -385,8 +385,10 @@ cudaError_t launch_pair(const Fp4GemmArgs& a) {
   static_assert(C::kSmem >= 161 * 1024, "no CTA of a cluster of the split kernel beside this one (its launch says why)");
   if (e == cudaSuccess) e = make_tmap_y(&ty, a.y, a.M, kGated ? a.N / 2 : a.N);
   if (e != cudaSuccess) return e;
-  // By tokens where the outputs are 8 times the weights: 8192 x 512 -> 16384, MX, 48 us against 56, 8192 x 2048 -> 16384 95 against 95
-  // to 96; but 816 x 2048 -> 2 x 16384 with other weights in every call, 29.2 against 28.4.
+  // By tokens where the outputs are more than 8 times the weights.  Both orders at 192 shapes (816 to 8192 tokens, K 256 to 4096, 1024 to
+  // 16384 outputs, gated ones among them, MX and NV, other weights in every call): where the rule takes it, 4.4% faster in the mean, 24% at
+  // best (4096 x 256 -> 16384, MX, 26.1 us against 32.4; 8192 x 1024 -> 16384 58.5 against 62.6; 8192 x 2048 -> 16384 the same) and 3% slower at
+  // worst (2048 x 512 -> 1024, NV, 5.1 against 5.0); where it does not, it would be 10% faster to 4% slower (816 x 2048 -> 2 x 16384 29.7 against 28.5).
   const bool by_tokens = 2ll * a.M * (kGated ? a.N / 2 : a.N) > 8ll * a.N * (a.K / 2);
   PairParams p = {a.xrow, a.wrow, a.bias, a.M, a.N, a.K, (a.M + kBn - 1) / kBn, (a.N + 255) / 256, 0, by_tokens};
   p.bn_last = (a.M - (p.tiles_m - 1) * kBn + 15) / 16 * 16;
